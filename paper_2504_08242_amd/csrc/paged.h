@@ -1,0 +1,24 @@
+// Internal declarations of the paged-cache operators (include/jupiter_paged.h): arguments as the kernels take them.
+#pragma once
+
+#include "bf16_common.h"
+#include "jupiter_paged.h"
+
+namespace jup {
+
+constexpr int kMaxPageSize = 65536;
+
+// page_size is a power of two
+inline int log2_of(int page_size) { return __builtin_ctz((unsigned)page_size); }
+
+// ---- tables and append (paged_tables.hip) -------------------------------------------------------------------------
+hipError_t launch_paged_extend(const jup_paged_extend_t& a, hipStream_t s);
+hipError_t launch_paged_append(const jup_paged_pool_t& pool, const jup_paged_append_t& a, hipStream_t s);
+
+// ---- attention (paged_attention.hip) --------------------------------------------------------------------------------
+hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_attention_t& a, hipStream_t s);
+
+// ---- verification (paged_verify.hip) --------------------------------------------------------------------------------
+hipError_t launch_verify_drafts(const jup_verify_drafts_t& a, hipStream_t s);
+
+}  // namespace jup
