@@ -1,17 +1,620 @@
 // Attention of the new tokens of a ragged batch over a paged cache (include/jupiter_paged.h).
+//
+// Rows.  A key/value head serves G = n_heads / n_kv_heads query heads, so the rows that read the same keys are (token, query
+// head of the group): row r of a request is token r / G, head r % G.  A workgroup has a TILE of such rows of one request and one
+// key/value head and a range of its keys.
+//
+// Who does what is found on the GPU: lengths are known nowhere else.  Every wave reads the lengths of all requests (64 lanes, a
+// prefix sum), so a launch needs no table of work and no launch before it: the host's grid is an upper bound, and the
+// workgroups past the last piece of work leave.  See find_work().
 #include "paged.h"
 
 namespace jup {
 namespace {
 
-__device__ __forceinline__ float to_f32(float x) { return x; }
-__device__ __forceinline__ float to_f32(u16 x) { return bf2f(x); }
-__device__ __forceinline__ void put(float* p, float x) { *p = x; }
-__device__ __forceinline__ void put(u16* p, float x) { *p = f2bf(x); }
+__device__ inline f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ inline f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-// One wave per (row, query head): 64 keys at a time, a lane has a key's score, then D / 64 columns of the output (rounded up).
-template <class T>
-__global__ __launch_bounds__(64) void attention_rows(const jup_paged_pool_t pool, const jup_paged_attention_t a, int shift) {
+constexpr int kKT = 32;                // keys per tile
+constexpr int kTileBytes = kKT * 256;  // a K or V tile: 32 rows of 128 bf16
+
+// A call, as the kernels take it.
+struct Attention {
+    const u16 *q, *k, *v;
+    u16* out;
+    long long q_row, q_head, out_row, out_head;   // strides
+    long long block, head, slot;
+    const int *row_start, *lengths, *table;
+    long long table_row;
+    int n_seqs, n_rows, n_kv_heads, n_blocks, shift, positions;  // positions: of a table row, table_width pages
+    Quotient group;                               // G
+    float scale_log2e;
+    int* count;                                   // arrival counters of rows whose keys are divided, zero between launches
+    float* partial;                               // [slot][kv head][row of the tile][kPartRow]
+    float chunk_factor;                           // 1 / pieces of work per key/value head that fill the chip (find_work); large: keys are not divided
+    int most_places;                              // of the scratch, per key/value head
+    int least_rows, most_rows;                    // requests with so many rows (tokens x G) are this launch's
+};
+// The arguments, read from memory where they are used: behind a main loop that needs the scalar registers itself.
+__device__ __forceinline__ Attention args_again() {
+    typedef const __attribute__((address_space(4))) char* kernarg;
+    kernarg p = (kernarg)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const Attention*)p;
+}
+constexpr int kPartRow = 132;  // 128 un-normalised outputs, maximum, sum, two unused
+
+// ---- who does what -------------------------------------------------------------------------------------------------------
+// A request of m new tokens has ceil(m G / R) tiles of R rows; a tile whose last row sees n keys has ceil(n / 32) key tiles,
+// and these are divided into pieces of at most `chunk`.  chunk = all key tiles of all rows / pieces wanted: about `pieces`
+// pieces per key/value head then fill the chip, however uneven the requests are, and no piece is longer than the others
+// by more than rounding.  Row tiles are numbered from the end: the longest first.
+struct Work {
+    int begin, tokens;    // rows of q of this request
+    int before;           // position of its first new token (negative: lengths shorter than the new tokens)
+    int seq, tile;        // request, tile of rows
+    int keys;             // that the last row of the tile sees
+    int tile_lo, tile_hi; // key tiles of this piece
+    int piece, pieces;    // of this tile of rows
+    int slot;             // of piece 0 in the scratch (pieces > 1)
+    // (every lane has the same; the compiler is told so)
+    __device__ __forceinline__ void make_uniform() {
+        for (int* x : {&begin, &tokens, &before, &seq, &tile, &keys, &tile_lo, &tile_hi, &piece, &pieces, &slot}) *x = __builtin_amdgcn_readfirstlane(*x);
+    }
+};
+
+__device__ __forceinline__ int pieces_of(int key_tiles, int chunk) { return max(1, (int)(((unsigned)key_tiles + (unsigned)chunk - 1) / (unsigned)chunk)); }
+
+template <int R>
+struct Request {
+    int begin, tokens, before, tiles, key_tiles;
+    __device__ __forceinline__ Request(const Attention& a, int i, int last) {
+        begin = tokens = before = tiles = key_tiles = 0;
+        if (i >= last) return;
+        begin = a.row_start[i];
+        const int end = a.row_start[i + 1], length = a.lengths[i];
+        if (begin < 0 || end <= begin) return;
+        tokens = min(end, a.n_rows) - begin;
+        const long long rows = (long long)tokens * a.group.d;
+        if (tokens <= 0 || rows < a.least_rows || rows > a.most_rows) {
+            tokens = 0;
+            return;
+        }
+        before = (int)max((long long)length - (end - begin), -(long long)INT32_MAX);
+        tiles = (int)((rows + R - 1) / R);
+        key_tiles = (keys_of(a, tokens - 1) + kKT - 1) / kKT;
+    }
+    // keys that token t sees
+    __device__ __forceinline__ int keys_of(const Attention& a, int t) const {
+        return (int)min(max((long long)before + t + 1, 0ll), (long long)a.positions);
+    }
+    __device__ __forceinline__ float cost() const { return (float)tiles * (float)key_tiles; }
+    __device__ __forceinline__ int pieces(int chunk) const { return tiles == 0 ? 0 : pieces_of(key_tiles, chunk); }
+};
+
+// Piece number `item` of a key/value head; false: there are fewer.  All lanes of a wave call it and get the same.  R: rows of a tile;
+// least: the shortest piece worth a workgroup, in key tiles.
+template <int R>
+__device__ bool find_work(const Attention& a, int item, int least, Work& w) {
+    const int lane = threadIdx.x & 63;
+    // the requests from `first` on are dealt to the lanes, `each` neighbours to a lane; the lane whose requests have the piece is gone
+    // into in the same way, until a lane has one request
+    int first = 0, last = a.n_seqs, each = (last + 63) / 64, chunk = 0, slots_before = 0;
+    for (;;) {
+        int items = 0, slots = 0;
+        Request<R> r(a, first + lane * each, last);
+        if (chunk == 0) {  // (first time round)
+            float cost = r.cost();
+            for (int j = 1; j < each; ++j) cost += Request<R>(a, first + lane * each + j, last).cost();
+            // (rounded up by more than the sums are off: at most as many pieces more than tiles as are wanted, as the grid says)
+            chunk = __builtin_amdgcn_readfirstlane((int)fminf(fmaxf(wave_sum(cost) * a.chunk_factor + 1.0f, (float)least), 1e9f));
+        }
+        for (int j = 0; j < each; ++j) {
+            const Request<R> x = j == 0 ? r : Request<R>(a, first + lane * each + j, min(last, first + (lane + 1) * each));
+            const int p = x.pieces(chunk);
+            items += x.tiles * p;
+            if (p > 1) slots += x.tiles * p;
+        }
+        int items_to = items, slots_to = slots;
+#pragma unroll
+        for (int by = 1; by < 64; by *= 2) {
+            const int i = __shfl_up(items_to, by, 64), s = __shfl_up(slots_to, by, 64);
+            if (lane >= by) {
+                items_to += i;
+                slots_to += s;
+            }
+        }
+        const unsigned long long there = __ballot(items_to > item);
+        if (!there) return false;
+        const int at = __builtin_ctzll(there);
+        item -= __builtin_amdgcn_readlane(items_to - items, at);
+        slots_before += __builtin_amdgcn_readlane(slots_to - slots, at);
+        first += at * each;
+        if (each == 1) {
+            r.begin = __builtin_amdgcn_readlane(r.begin, at);
+            r.tokens = __builtin_amdgcn_readlane(r.tokens, at);
+            r.before = __builtin_amdgcn_readlane(r.before, at);
+            r.tiles = __builtin_amdgcn_readlane(r.tiles, at);
+            r.key_tiles = __builtin_amdgcn_readlane(r.key_tiles, at);
+            const int most = r.pieces(chunk);
+            const int nth = (unsigned)item / (unsigned)max(most, 1);
+            // (sums of requests that overlap in a row_start that makes no sense can wrap)
+            if (item < 0 || nth >= r.tiles || slots_before < 0 || (most > 1 && slots_before + nth * most > a.most_places - most)) return false;
+            w.seq = first;
+            w.begin = r.begin;
+            w.tokens = r.tokens;
+            w.before = r.before;
+            w.tile = r.tiles - 1 - nth;
+            w.piece = item - nth * most;
+            w.slot = slots_before + nth * most;
+            const int last_token = min(a.group.of(min((w.tile + 1) * R, r.tokens * (int)a.group.d) - 1), r.tokens - 1);
+            w.keys = r.keys_of(a, last_token);
+            const int key_tiles = (w.keys + kKT - 1) / kKT;
+            w.pieces = pieces_of(key_tiles, chunk);
+            if (w.piece >= w.pieces) return false;  // (an earlier tile of a prompt: fewer keys than the last one)
+            const int even = (unsigned)key_tiles / (unsigned)w.pieces, over = key_tiles - even * w.pieces;
+            w.tile_lo = w.piece * even + min(w.piece, over);
+            w.tile_hi = w.tile_lo + even + (w.piece < over);
+            return true;
+        }
+        last = min(last, first + each);
+        each = (each + 63) / 64;
+    }
+}
+
+// ---- pages -----------------------------------------------------------------------------------------------------------------
+// Block numbers of a key tile's four groups of eight rows (a page has at least eight).  Read through the scalar cache:
+// the tables do not change during a launch.
+struct Blocks {
+    int id[4];
+};
+__device__ __forceinline__ Blocks blocks_of(const Attention& a, const int* table_row, int tile, int last_key) {
+    typedef const __attribute__((address_space(4))) int* scalar;
+    Blocks b;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) b.id[p] = ((scalar)table_row)[min(tile * kKT + 8 * p, last_key) >> a.shift];
+    return b;
+}
+// Address of the first of eight rows; of a place in block 0 where there is no such page (read, and not used).
+__device__ __forceinline__ const char* group_base(const Attention& a, const u16* pool, int block, int key) {
+    const int at = (unsigned)block < (unsigned)a.n_blocks ? block : 0;
+    return uniform_ptr((const char*)(pool + at * a.block + (key & ((1 << a.shift) - 1)) * a.slot));
+}
+// Which of a tile's 32 rows are keys: a page that is there, at or before the last key.
+__device__ __forceinline__ unsigned rows_there(const Attention& a, const Blocks& b, int tile, int last_key) {
+    unsigned rows = 0;
+#pragma unroll
+    for (int p = 0; p < 4; ++p)
+        if ((unsigned)b.id[p] < (unsigned)a.n_blocks) rows |= 0xFFu << (8 * p);
+    const int n = last_key + 1 - tile * kKT;
+    return n >= kKT ? rows : n <= 0 ? 0 : rows & ((1u << n) - 1);
+}
+
+__device__ inline float max_across_halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float max_across_rows(float x) {  // of 16 lanes, within each half
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// Transposing 8-byte LDS read: within each group of 16 lanes, lane i receives as element r element (i & 3) of the 8 bytes
+// addressed by lane 4r + (i >> 2) of the group.
+__device__ __forceinline__ u32x2 read_tr(unsigned lds_address) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(size_t)lds_address));
+}
+
+// ---- values that are no numbers --------------------------------------------------------------------------------------------
+// The products of a tile are sums over all its 32 keys, with probability 0 where a row does not see a key; 0 times an infinity
+// or a NaN is NaN.  Tiles in which some row does not see some key are looked through for such values (three operations per
+// dword; one tile in a few has a mask at all).  Where there is one, the products go without them, and a second pair of
+// products counts, for every row and feature, the infinities of either sign that the row does see.
+__device__ __forceinline__ unsigned not_finite(u32x4 v) {  // bits 15 and 31 of a dword: an exponent of ones
+    unsigned any = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) any |= (v[e] & 0x7F807F80u) + 0x00800080u;
+    return any & 0x80008000u;
+}
+// (one accumulator holds both counts: 1 for a positive infinity, 64 for a negative one, 65 for a NaN; a tile has 32 keys, and all of
+// it is exact in bf16 and fp32)
+__device__ __forceinline__ void split_values(u32x4 v, u32x4& finite, u32x4& code) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        unsigned f = 0, k = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const unsigned x = (v[e] >> (16 * h)) & 0xFFFFu;
+            const bool special = (x & 0x7F80u) == 0x7F80u;
+            const unsigned what = (x & 0x7Fu) ? 0x4282u : x & 0x8000u ? 0x4280u : 0x3F80u;  // bf16 65, 64, 1
+            f |= (special ? 0u : x) << (16 * h);
+            k |= (special ? what : 0u) << (16 * h);
+        }
+        finite[e] = f;
+        code[e] = k;
+    }
+}
+__device__ __forceinline__ float with_counts(float sum, float code) {
+    if (code >= 64.0f) sum -= INFINITY;
+    if (code != 0.0f && code != 64.0f * floorf(code * (1.0f / 64.0f))) sum += INFINITY;
+    return sum;
+}
+
+// ---- pieces of one tile put together ------------------------------------------------------------------------------------------
+// The workgroups of a tile's pieces leave un-normalised sums and their softmax statistics in the scratch; the one that
+// arrives last adds them in the order of the pieces (the result does not depend on who that is) and writes the rows.  Nobody
+// waits.  flag: an LDS word that nobody else uses any more; THREADS: of the workgroup, all of which call it.
+template <int R, int THREADS>
+__device__ __forceinline__ void join_pieces(const Work& w, int kv_head, int* flag) {
+    const Attention a = args_again();
+    const int tid = threadIdx.x;
+    wait_stores_performed();
+    __syncthreads();
+    if (tid == 0) {
+        int* count = a.count + (long long)w.slot * a.n_kv_heads + kv_head;
+        const int before = arrive_coherent(count);
+        *flag = before == w.pieces - 1;
+        if (before == w.pieces - 1) *count = 0;  // ready for the next launch
+    }
+    __syncthreads();
+    if (!*flag) return;
+    const long long step = (long long)a.n_kv_heads * R * kPartRow;
+    const float* base = a.partial + ((long long)w.slot * a.n_kv_heads + kv_head) * R * kPartRow;
+    const int rows = min(R, w.tokens * (int)a.group.d - w.tile * R);
+    for (int idx = tid; idx < rows * 16; idx += THREADS) {
+        const int r = idx >> 4, ch = idx & 15;
+        float m = -INFINITY, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int p0 = 0; p0 < w.pieces; p0 += 8) {  // eight pieces in flight: they come from memory
+            float2 stat[8], val[8][4];
+#pragma unroll
+            for (int p = 0; p < 8; ++p)
+                if (p0 + p < w.pieces) {
+                    const float* row = base + (p0 + p) * step + (long long)r * kPartRow;
+                    stat[p] = load_coherent2(row + 128);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) val[p][e] = load_coherent2(row + ch * 8 + 2 * e);
+                }
+            float top = m;
+#pragma unroll
+            for (int p = 0; p < 8; ++p)
+                if (p0 + p < w.pieces) top = fmaxf(top, stat[p].x);
+            if (top == -INFINITY) top = 0.f;
+            const float back = __builtin_amdgcn_exp2f(m - top);
+            l *= back;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] *= back;
+#pragma unroll
+            for (int p = 0; p < 8; ++p)
+                if (p0 + p < w.pieces && stat[p].y != 0.f) {  // (0: a piece this row sees nothing of)
+                    const float f = __builtin_amdgcn_exp2f(stat[p].x - top);
+                    l += stat[p].y * f;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        acc[2 * e] += val[p][e].x * f;
+                        acc[2 * e + 1] += val[p][e].y * f;
+                    }
+                }
+            m = top;
+        }
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+        const int token = a.group.of(w.tile * R + r);
+        const int in_group = w.tile * R + r - token * (int)a.group.d;
+        u32x4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = pack_bf16x2(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+        *(u32x4*)(a.out + (long long)(w.begin + token) * a.out_row + (long long)(kv_head * (int)a.group.d + in_group) * a.out_head + ch * 8) = o;
+    }
+}
+
+// ---- few rows ----------------------------------------------------------------------------------------------------------------
+// Decoding and verification: a handful of rows against a long cache, bound by reading keys and values.  A tile has QW = 16 or
+// 32 rows, and four waves divide the piece's key tiles: each works alone on the tiles wave, wave + 4, ..., with one LDS
+// slot for a K and one for a V tile, and refills the K slot as soon as the scores are out of it and the V slot as soon as the products
+// are.  Two workgroups share a CU, so 128 KB are in flight on it, and one's entry and merge lie under the other's loads.
+// Transposed products, S^T = K Q^T and O^T += V^T P^T: a lane owns a row, whose statistics are scalars of the lane.
+//   QW = 32, 32x32x16 (lane = 32 hh + c): A[m = c][k = 8 hh + e], B[k = 8 hh + e][n = c], D[m = 8 (i/4) + 4 hh + i%4][n = c].
+//   QW = 16, 16x16x32 (lane = 16 hh + c): A[m = c][k = 8 hh + e], B[k = 8 hh + e][n = c], D[m = 4 hh + i][n = c].
+// P^T is taken as the scores lie in the accumulators; V^T is read for exactly that order of keys.
+// LDS tiles, rows of 256 bytes in 16 chunks of 16:  K: chunk ch of row r at position ch ^ (r & 15);  V: at (((ch >> 2) ^ (r & 3)) << 2) | (ch & 3).
+constexpr int kFewWaves = 4;
+constexpr int kFewQ = kFewWaves * 2 * kTileBytes;                       // the tile of rows, K layout
+constexpr int few_stat(int QW) { return kFewQ + (QW == 32 ? 8192 : 4096); }  // [2][waves][QW] maxima and sums
+constexpr int few_lds(int QW) { return few_stat(QW) + 2 * kFewWaves * QW * 4; }
+static_assert(kFewWaves * 32 * 132 * 4 <= few_stat(32) && kFewWaves * 16 * 132 * 4 <= few_stat(16), "merge regions overlap the statistics");
+static_assert(2 * few_lds(32) <= 160 * 1024, "two workgroups share a CU");
+
+template <int QW>
+__global__ __launch_bounds__(64 * kFewWaves, 2) void attention_few(const Attention args, int least) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    constexpr int NW = kFewWaves;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & (QW - 1), hh = lane / QW;
+    // consecutive workgroups are the heads of a piece: a head's pieces meet on one XCD where the heads are a multiple of 8
+    const int kv_head = (int)(blockIdx.x % (unsigned)args.n_kv_heads), item = (int)(blockIdx.x / (unsigned)args.n_kv_heads);
+    Work w;
+    if (!find_work<QW>(args, item, least, w)) return;
+    w.make_uniform();
+    const Attention a = args_again();
+    const int G = a.group.d;
+    const int rows = min(QW, w.tokens * G - w.tile * QW);
+    const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_byte_address(lds));
+    const int lrow = lane >> 4, lp = lane & 15;
+
+    // the rows of q into LDS; past the last one, that one again
+    for (int r0 = 4 * wave; r0 < QW; r0 += 4 * NW) {
+        const int r = r0 + lrow;
+        const int row = w.tile * QW + min(r, rows - 1), token = a.group.of(row);
+        const u16* from = a.q + (long long)(w.begin + token) * a.q_row + (long long)(kv_head * G + row - token * G) * a.q_head;
+        load_to_lds_16(from + (lp ^ (r & 15)) * 8, lds0 + kFewQ + r0 * 256);
+    }
+    const int last_key = w.keys - 1;
+    const int my_token = a.group.of(w.tile * QW + min(c, rows - 1));
+    const int q_abs = w.before + my_token;                                          // the last key this lane's row sees
+    const int first_token = a.group.of(w.tile * QW);
+    const int first_masked = (int)max((long long)w.before + first_token + 1, 0ll) / kKT;  // tiles before it: every row sees every key
+    const int* table_row = (const int*)uniform_ptr((const char*)(a.table + w.seq * a.table_row));
+    const u16* k_pool = a.k + kv_head * a.head;
+    const u16* v_pool = a.v + kv_head * a.head;
+    const unsigned row_bytes = (unsigned)(a.slot * 2);
+
+    auto fill = [&](int tile, const Blocks& b, bool v_part) __attribute__((always_inline)) {
+        unsigned slot = lds0 + wave * 2 * kTileBytes + (v_part ? kTileBytes : 0);
+        asm volatile("" : "+v"(slot));  // (from a vector register on purpose: the compiler keeps it in one, and else hands that to the loads)
+        const unsigned dst = __builtin_amdgcn_readfirstlane(slot);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {  // four rows (1 KB): lane i lands at row 4j + (i >> 4), position i & 15
+            const char* base = group_base(a, v_part ? v_pool : k_pool, b.id[j >> 1], tile * kKT + 8 * (j >> 1));
+            const unsigned ch = v_part ? (((lp >> 2) ^ lrow) << 2) | (lp & 3) : lp ^ (4 * (j & 3) + lrow);
+            load_to_lds_16(base, (4 * (j & 1) + lrow) * row_bytes + ch * 16, dst + j * 1024);
+        }
+    };
+    int tile = w.tile_lo + wave;
+    Blocks here{}, next{};
+    if (tile < w.tile_hi) {
+        here = blocks_of(a, table_row, tile, last_key);
+        fill(tile, here, false);
+        fill(tile, here, true);
+        if (tile + NW < w.tile_hi) next = blocks_of(a, table_row, tile + NW, last_key);
+        asm volatile("s_waitcnt vmcnt(16)" ::: "memory");  // the rows of q have landed, the tiles are on their way
+    } else {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    __builtin_amdgcn_s_barrier();
+
+    constexpr int KS = QW == 16 ? 4 : 8;   // MFMA steps over the head's 128 features
+    constexpr int NS = QW == 16 ? 8 : 16;  // scores of a tile per lane
+    constexpr int DB = QW == 16 ? 8 : 4;   // output blocks of QW features
+    constexpr int NR = QW == 16 ? 4 : 16;  // registers of one
+    typedef float acc_t __attribute__((ext_vector_type(NR)));
+    constexpr unsigned kStep = QW == 16 ? 64 : 32;  // 16-byte chunk `hh` of a K row; the next MFMA step's is an XOR away
+    const unsigned k_lane = c * 256 + ((hh ^ (c & 15)) * 16);
+    bf16x8 qf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const bf16x8*)(lds + kFewQ + (k_lane ^ (kStep * ks)));
+    acc_t oacc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < NR; ++r) oacc[db][r] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+    const int quad = lane >> 4, s = lane & 15;
+    const int vt_row = QW == 16 ? 4 * quad + (s >> 2) : 4 * (quad >> 1) + (s >> 2);
+    const unsigned v_base = lds0 + wave * 2 * kTileBytes + kTileBytes;
+    unsigned v_lane[4];  // by 64-byte feature group
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+        v_lane[db] = v_base + vt_row * 256 + ((db ^ (vt_row & 3)) << 6) + ((QW == 16 ? 0 : 2 * (quad & 1)) + ((s & 3) >> 1)) * 16 + 8 * (s & 1);
+    auto product = [](u32x4 x, bf16x8 p, acc_t acc) {
+        if constexpr (QW == 16) return mfma16(__builtin_bit_cast(bf16x8, x), p, acc);
+        else return mfma32(__builtin_bit_cast(bf16x8, x), p, acc);
+    };
+    auto key_of = [](int r) { return (QW == 16 ? 16 : 8) * (r >> 2) + (r & 3); };  // of the lane's score r, less 4 hh
+    const unsigned char* k_base = lds + wave * 2 * kTileBytes;
+
+    for (; tile < w.tile_hi; tile += NW) {
+        const bool more = tile + NW < w.tile_hi;
+        const unsigned there = rows_there(a, here, tile, last_key);
+        asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // the K tile has landed; V may be in flight
+
+        // ---- S^T = K Q^T ----
+        bf16x8 kf[8];
+        float sv[NS];
+        if constexpr (QW == 16) {
+#pragma unroll
+            for (int f = 0; f < 8; ++f) kf[f] = *(const bf16x8*)(k_base + (f >> 2) * 4096 + (k_lane ^ (kStep * (f & 3))));
+            f32x4 sacc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+            for (int f = 0; f < 8; ++f) sacc[f & 1] = mfma16(kf[4 * (f & 1) + (f >> 1)], qf[f >> 1], sacc[f & 1]);
+#pragma unroll
+            for (int r = 0; r < NS; ++r) sv[r] = sacc[r >> 2][r & 3];
+        } else {
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) kf[ks] = *(const bf16x8*)(k_base + (k_lane ^ (kStep * ks)));
+            f32x16 sacc;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sacc[r] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) sacc = mfma32(kf[ks], qf[ks], sacc);
+#pragma unroll
+            for (int r = 0; r < NS; ++r) sv[r] = sacc[r];
+        }
+        if (more) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the K slot has been read
+            fill(tile + NW, next, false);
+        }
+
+        // ---- online softmax ----
+        const bool masked = tile >= first_masked || there != ~0u;
+        unsigned sees = ~0u;  // bit r: this lane's row sees the key of its score r
+        if (masked) {
+            // (opaque: keeps this a branch, as selects it would run for every tile, and its numbers out of the registers between tiles)
+            int quarter = 4 * hh;
+            asm volatile("" : "+v"(quarter));
+            sees = 0;
+#pragma unroll
+            for (int r = 0; r < NS; ++r) {
+                const int key = quarter + key_of(r);
+                const bool yes = tile * kKT + key <= q_abs && ((there >> key) & 1);
+                sv[r] = yes ? sv[r] : -INFINITY;
+                sees |= (unsigned)yes << r;
+            }
+        }
+        float mt = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < NS; ++r) mt = fmaxf(mt, sv[r]);
+        if constexpr (QW == 16) mt = max_across_rows(mt);
+        mt = max_across_halves(mt) * a.scale_log2e;  // the scale is positive
+        // The reference of the exponentials moves only when a tile's maximum exceeds it by 2^8: sums are rescaled a few times per
+        // piece, and the common factor goes with the normalisation.
+        const bool grow = mt > m_run + 8.0f;
+        const float m_new = grow ? mt : m_run;
+        const float m_safe = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = grow ? __builtin_amdgcn_exp2f(m_run - m_safe) : 1.0f;
+        const bool rescale = grow && m_run != -INFINITY;
+        float ps = 0.f;
+        bf16x8 pf[NS / 8];
+#pragma unroll
+        for (int r = 0; r < NS; ++r) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[r], a.scale_log2e, -m_safe));
+            ps += p;
+            pf[r >> 3][r & 7] = (__bf16)p;  // the operand of the second product: 2^-8 of each probability
+        }
+        l_run = l_run * alpha + ps;
+        m_run = m_new;
+        if (__any(rescale)) {
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int r = 0; r < NR; ++r) oacc[db][r] *= alpha;
+        }
+
+        // ---- O^T += V^T P^T ----
+        if (more) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // V has landed, the next K may be in flight
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        bool special = false;
+        if (masked) {
+            asm volatile("");
+            unsigned any = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                u32x4* piece = (u32x4*)(lds + wave * 2 * kTileBytes + kTileBytes + j * 1024 + lane * 16);  // of row 4j + lrow
+                if ((there >> (4 * j + lrow)) & 1) any |= not_finite(*piece);
+                else *piece = (u32x4){0, 0, 0, 0};  // no key: whatever lies there becomes 0
+            }
+            special = __any(any != 0);
+        }
+        // fragment f: QW = 32: feature block f / 2, key half f % 2; QW = 16: feature block f, all 32 keys
+        auto value = [&](int f) __attribute__((always_inline)) {
+            const unsigned at = v_lane[f / 2] + (QW == 16 ? (f % 2) * 32 : (f % 2) * 16 * 256);
+            const u32x2 lo = read_tr(at), hi = read_tr(at + (QW == 16 ? 16 * 256 : 8 * 256));
+            return (u32x4){lo[0], lo[1], hi[0], hi[1]};
+        };
+        if (special) {
+            bf16x8 seen[NS / 8];
+#pragma unroll
+            for (int r = 0; r < NS; ++r) seen[r >> 3][r & 7] = (__bf16)(float)((sees >> r) & 1);
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+                acc_t codes;
+#pragma unroll
+                for (int r = 0; r < NR; ++r) codes[r] = 0.f;
+#pragma unroll
+                for (int h = 0; h < 8 / DB; ++h) {
+                    u32x4 finite, code;
+                    split_values(value(db * (8 / DB) + h), finite, code);
+                    oacc[db] = product(finite, pf[h], oacc[db]);
+                    codes = product(code, seen[h], codes);
+                }
+#pragma unroll
+                for (int r = 0; r < NR; ++r) oacc[db][r] = with_counts(oacc[db][r], codes[r]);
+            }
+        } else {
+#pragma unroll
+            for (int f = 0; f < 8; ++f) oacc[f * DB / 8] = product(value(f), pf[f % (8 / DB)], oacc[f * DB / 8]);
+        }
+        if (more) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the V slot has been read
+            fill(tile + NW, next, true);
+            here = next;
+            if (tile + 2 * NW < w.tile_hi) next = blocks_of(a, table_row, tile + 2 * NW, last_key);
+        }
+    }
+
+    // ---- the waves' sums put together ----
+    const Attention e = args_again();
+    constexpr int kRow = 132;
+    constexpr int kRegion = QW * kRow;
+    float* obuf = (float*)lds;
+    float* stat_m = (float*)(lds + few_stat(QW));
+    float* stat_l = stat_m + NW * QW;
+    {
+        float l_tot = l_run + __shfl_xor(l_run, 32, 64);
+        if (QW == 16) l_tot += __shfl_xor(l_tot, 16, 64);
+        if (hh == 0) {
+            stat_m[wave * QW + c] = m_run;
+            stat_l[wave * QW + c] = l_tot;
+        }
+    }
+    __syncthreads();  // statistics visible; every wave is done with its slots
+    const long long part = ((long long)(w.slot + w.piece) * e.n_kv_heads + kv_head) * QW;
+    {
+        float sm[NW], sl[NW];
+#pragma unroll
+        for (int x = 0; x < NW; ++x) {
+            sm[x] = stat_m[x * QW + c];
+            sl[x] = stat_l[x * QW + c];
+        }
+        float m_all = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < NW; ++x) m_all = fmaxf(m_all, sm[x]);
+        const float m_ref = m_all == -INFINITY ? 0.f : m_all;  // (a row that sees nothing of this piece)
+        float l_all = 0.f;
+#pragma unroll
+        for (int x = 0; x < NW; ++x) l_all += sl[x] * __builtin_amdgcn_exp2f(sm[x] - m_ref);
+        // the only piece: normalised here; of several: left for join_pieces
+        const float f = __builtin_amdgcn_exp2f(m_run - m_ref) * (w.pieces > 1 ? 1.0f : l_all == 0.f ? 0.f : 1.0f / l_all);
+        float* mine = obuf + wave * kRegion + c * kRow;
+#pragma unroll
+        for (int x = 0; x < (QW == 16 ? 8 : 16); ++x) {  // four consecutive features per write
+            const int db = QW == 16 ? x : x >> 2, r = QW == 16 ? 0 : 4 * (x & 3);
+            *(float4*)(mine + (QW == 16 ? 16 * x : 8 * x) + 4 * hh) =
+                make_float4(oacc[db][r] * f, oacc[db][r + 1] * f, oacc[db][r + 2] * f, oacc[db][r + 3] * f);
+        }
+        if (w.pieces > 1 && wave == 0 && hh == 0 && c < rows) store_coherent2(e.partial + (part + c) * kPartRow + 128, m_all, l_all);
+    }
+    __syncthreads();
+    for (int idx = tid; idx < rows * 16; idx += 64 * NW) {
+        const int r = idx >> 4, ch = idx & 15;
+        const float* src = obuf + r * kRow + ch * 8;
+        float4 x = *(const float4*)src, y = *(const float4*)(src + 4);
+#pragma unroll
+        for (int i = 1; i < NW; ++i) {
+            const float4 x2 = *(const float4*)(src + i * kRegion), y2 = *(const float4*)(src + i * kRegion + 4);
+            x.x += x2.x; x.y += x2.y; x.z += x2.z; x.w += x2.w;
+            y.x += y2.x; y.y += y2.y; y.z += y2.z; y.w += y2.w;
+        }
+        if (w.pieces > 1) {
+            float* dst = e.partial + (part + r) * kPartRow + ch * 8;
+            store_coherent2(dst, x.x, x.y);
+            store_coherent2(dst + 2, x.z, x.w);
+            store_coherent2(dst + 4, y.x, y.y);
+            store_coherent2(dst + 6, y.z, y.w);
+            continue;
+        }
+        const int row = w.tile * QW + r, token = e.group.of(row);
+        u32x4 o;
+        o[0] = pack_bf16x2(x.x, x.y); o[1] = pack_bf16x2(x.z, x.w);
+        o[2] = pack_bf16x2(y.x, y.y); o[3] = pack_bf16x2(y.z, y.w);
+        *(u32x4*)(e.out + (long long)(w.begin + token) * e.out_row + (long long)((kv_head - token) * (int)e.group.d + row) * e.out_head + ch * 8) = o;
+    }
+    if (w.pieces > 1) join_pieces<QW, 64 * NW>(w, kv_head, (int*)(lds + few_stat(QW)));
+}
+
+// Check mode.  One wave per (row, query head): 64 keys at a time, a lane has a key's score, then D / 64 columns of the output (rounded up).
+__global__ __launch_bounds__(64) void attention_f32(const jup_paged_pool_t pool, const jup_paged_attention_t a, int shift) {
     __shared__ float q[256];
     const int lane = threadIdx.x, row = blockIdx.x / a.n_heads, head = blockIdx.x - row * a.n_heads;
     const int D = pool.head_dim, kv_head = head / (a.n_heads / pool.n_kv_heads);
@@ -26,7 +629,7 @@ __global__ __launch_bounds__(64) void attention_rows(const jup_paged_pool_t pool
     if (row >= end) return;
     const long long last = min((long long)a.lengths[lo] - (end - row), ((long long)a.table_width << shift) - 1);
     const int* table = a.table + lo * a.table_stride;
-    for (int i = lane; i < D; i += 64) q[i] = to_f32(((const T*)a.q)[row * a.q_row_stride + head * a.q_head_stride + i]);
+    for (int i = lane; i < D; i += 64) q[i] = ((const float*)a.q)[row * a.q_row_stride + head * a.q_head_stride + i];
     __syncthreads();
     float m = -INFINITY, l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
     for (long long first = 0; first <= last; first += 64) {
@@ -37,9 +640,9 @@ __global__ __launch_bounds__(64) void attention_rows(const jup_paged_pool_t pool
             const int block = table[key >> shift];
             if (block >= 0 && block < pool.n_blocks) {
                 at = block * pool.block_stride + kv_head * pool.head_stride + (key & ((1 << shift) - 1)) * pool.slot_stride;
-                const T* k = (const T*)pool.k + at;
+                const float* k = (const float*)pool.k + at;
                 float sum = 0.f;
-                for (int i = 0; i < D; ++i) sum = __builtin_fmaf(q[i], to_f32(k[i]), sum);
+                for (int i = 0; i < D; ++i) sum = __builtin_fmaf(q[i], k[i], sum);
                 s = sum * a.scale;
             }
         }
@@ -62,26 +665,75 @@ __global__ __launch_bounds__(64) void attention_rows(const jup_paged_pool_t pool
             if (from < 0) continue;
 #pragma unroll
             for (int c = 0; c < 4; ++c)
-                if (lane + 64 * c < D) acc[c] = __builtin_fmaf(w, to_f32(((const T*)pool.v)[from + lane + 64 * c]), acc[c]);
+                if (lane + 64 * c < D) acc[c] = __builtin_fmaf(w, ((const float*)pool.v)[from + lane + 64 * c], acc[c]);
         }
     }
 #pragma unroll
     for (int c = 0; c < 4; ++c)
-        if (lane + 64 * c < D) put((T*)a.out + row * a.out_row_stride + head * a.out_head_stride + lane + 64 * c, l == 0.f ? 0.f : acc[c] / l);
+        if (lane + 64 * c < D) ((float*)a.out)[row * a.out_row_stride + head * a.out_head_stride + lane + 64 * c] = l == 0.f ? 0.f : acc[c] / l;
 }
 
 }  // namespace
 
-hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_attention_t& a, hipStream_t s) {
-    const int shift = log2_of(pool.page_size);
-    const dim3 grid((unsigned)a.n_rows * (unsigned)a.n_heads);
-    if (pool.dtype == JUP_BF16)
-        hipLaunchKernelGGL(attention_rows<u16>, grid, dim3(64), 0, s, pool, a, shift);
-    else
-        hipLaunchKernelGGL(attention_rows<float>, grid, dim3(64), 0, s, pool, a, shift);
+// ---- launches ------------------------------------------------------------------------------------------------------------------
+namespace {
+
+// Scratch: counters, then pieces.  A launch has at most kPieces + n_kv_heads pieces wanted (find_work), a divided tile at least two, each of
+// which is at least half as long as a piece may be: at most twice as many places are used, of 32 rows.
+constexpr int kPieces = 1024;  // two rounds of two workgroups per CU
+constexpr int kMostHeads = kPieces;  // (more heads than that fill the chip without dividing keys)
+constexpr size_t kPlaces = 2 * (kPieces + kMostHeads);
+constexpr size_t kCountBytes = kPlaces * 4;
+constexpr size_t kPartialBytes = kPlaces * 32 * kPartRow * 4;
+
+template <class K>
+hipError_t with_lds(K* kernel, int bytes, bool* done) {  // once per device: a kernel's limit of dynamic LDS
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess || (dev < 64 && __atomic_load_n(done + dev, __ATOMIC_ACQUIRE))) return e;
+    e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess && dev < 64) __atomic_store_n(done + dev, true, __ATOMIC_RELEASE);
+    return e;
+}
+
+template <int QW>
+hipError_t launch_few(const Attention& a, int pieces, hipStream_t s) {
+    static bool done[64];
+    hipError_t e = with_lds(attention_few<QW>, few_lds(QW), done);
+    if (e != hipSuccess) return e;
+    const long long items = (long long)a.n_rows * a.group.d / QW + a.n_seqs + pieces;
+    const long long grid = items * a.n_kv_heads;
+    if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL(attention_few<QW>, dim3((unsigned)grid), dim3(64 * kFewWaves), few_lds(QW), s, a, 4);
     return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_attention_t& c, hipStream_t s) {
+    const int shift = log2_of(pool.page_size);
+    if (pool.dtype == JUP_F32) {
+        hipLaunchKernelGGL(attention_f32, dim3((unsigned)c.n_rows * (unsigned)c.n_heads), dim3(64), 0, s, pool, c, shift);
+        return hipGetLastError();
+    }
+    Attention a{};
+    a.q = (const u16*)c.q; a.k = (const u16*)pool.k; a.v = (const u16*)pool.v; a.out = (u16*)c.out;
+    a.q_row = c.q_row_stride; a.q_head = c.q_head_stride; a.out_row = c.out_row_stride; a.out_head = c.out_head_stride;
+    a.block = pool.block_stride; a.head = pool.head_stride; a.slot = pool.slot_stride;
+    a.row_start = c.row_start; a.lengths = c.lengths; a.table = c.table; a.table_row = c.table_stride;
+    a.n_seqs = c.n_seqs; a.n_rows = c.n_rows; a.n_kv_heads = pool.n_kv_heads; a.n_blocks = pool.n_blocks; a.shift = shift;
+    a.positions = c.table_width << shift;
+    a.group.set(c.n_heads / pool.n_kv_heads);
+    a.scale_log2e = c.scale * 1.4426950408889634f;
+    a.count = (int*)c.workspace;
+    a.partial = (float*)((char*)c.workspace + kCountBytes);
+    const int pieces = pool.n_kv_heads > kMostHeads ? 0 : (kPieces + pool.n_kv_heads - 1) / pool.n_kv_heads;
+    a.most_places = (int)(kPlaces / pool.n_kv_heads);
+    a.chunk_factor = pieces > 0 ? 1.0001f / pieces : 1e30f;
+    a.least_rows = 0; a.most_rows = INT32_MAX;
+    return (long long)c.max_new * a.group.d <= 16 ? launch_few<16>(a, pieces, s) : launch_few<32>(a, pieces, s);
 }
 
 }  // namespace jup
 
-extern "C" size_t jup_paged_workspace_bytes(void) { return 256; }
+extern "C" size_t jup_paged_workspace_bytes(void) { return jup::kCountBytes + jup::kPartialBytes; }
