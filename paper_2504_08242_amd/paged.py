@@ -57,6 +57,19 @@ class _Verify(ctypes.Structure):
         ("workspace_bytes", _sz)]
 
 
+# The structs as one pack() each: a ctypes object of 25 fields takes longer to fill than the GPU to answer a small call.
+_FORMATS = {_i32: "i", _i64: "q", _vp: "P", _f32: "f", _sz: "N"}
+
+
+def _packer(struct_type):
+    import struct
+    packer = struct.Struct("@" + "".join(_FORMATS[t] for _, t in struct_type._fields_) + "0q")
+    assert packer.size == ctypes.sizeof(struct_type), struct_type
+    return packer.pack
+
+
+_pack_pool, _pack_extend, _pack_append, _pack_attention, _pack_verify = map(_packer, (_Pool, _Extend, _Append, _Attention, _Verify))
+
 _bound = None
 
 
@@ -80,67 +93,81 @@ def _lib():
 Step = collections.namedtuple("Step", "row_start positions slots lengths owned free_count status")
 Verdict = collections.namedtuple("Verdict", "n_accepted next_token emitted lengths")
 
-_DTYPES = {torch.float32: jb.JUP_F32, torch.bfloat16: jb.JUP_BF16}
+_F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
+_DTYPES = {_F32: jb.JUP_F32, _BF16: jb.JUP_BF16}
 
 
-def _need(ok, message):
-    if not ok:
-        raise ValueError(message)
+# (messages are made where they are needed: in a call of a few microseconds they would be half of it)
 
 
-def _ints(name, t, device, *shape):
-    """An int32 tensor on the call's device; shape None: any length."""
-    _need(t.dtype == torch.int32 and t.device == device, f"{name} must be an int32 tensor on {device}")
-    _need(t.dim() == len(shape) and all(want is None or n == want for n, want in zip(t.shape, shape)),
-          f"{name} has shape {tuple(t.shape)}, {shape} wanted (None: any)")
-    _need(t.is_contiguous(), f"{name} must be contiguous")
+def _ints(name, t, at, *shape):
+    """Address of a contiguous int32 tensor on GPU number `at`, of that shape."""
+    if t.dtype is not _I32 or t.get_device() != at or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on cuda:{at}, not {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
 
 
-def _table(t, device, n):
-    _need(t.dtype == torch.int32 and t.device == device and t.dim() == 2 and t.shape[0] == n,
-          f"table must be an int32 tensor [{n}, width] on {device}")
-    _need(t.shape[1] < 2 or n == 0 or t.stride(1) == 1, "entries of a row of the table must be neighbours")
-    return max(t.stride(0), t.shape[1]) if n > 1 else t.shape[1]
+def _table(t, at, n):
+    """(address, width, stride) of block tables."""
+    if t.dtype is not _I32 or t.get_device() != at or t.dim() != 2 or t.shape[0] != n:
+        raise ValueError(f"table must be an int32 tensor [{n}, width] on cuda:{at}, not {t.dtype} {list(t.shape)} on {t.device}")
+    width, (stride, step) = t.shape[1], t.stride()
+    if n < 2:
+        stride = width
+    if (step != 1 and width > 1 and n > 0) or stride < width:
+        raise ValueError("entries of a row of the table must be neighbours, and rows must not overlap")
+    return t.data_ptr(), width, stride
 
 
-def _heads(name, t, dtype, device, n_heads, head_dim, rows=None):
-    """[rows, heads, head_dim], elements of a head neighbours; (row stride, head stride)."""
-    _need(t.dtype == dtype and t.device == device, f"{name} must be a {dtype} tensor on {device}")
-    _need(t.dim() == 3 and (n_heads is None or t.shape[1] == n_heads) and t.shape[2] == head_dim and (rows is None or t.shape[0] == rows),
-          f"{name} has shape {tuple(t.shape)}, [{rows}, {n_heads}, {head_dim}] wanted (None: any)")
-    _need(t.stride(2) == 1 or t.numel() == 0, f"elements of a head of {name} must be neighbours")
+def _heads(name, t, dtype, at, rows, heads, dim, written=False):
+    """(address, row stride, head stride) of a tensor [rows, heads, dim] whose heads are contiguous."""
+    if t.dtype is not dtype or t.get_device() != at or t.shape != (rows, heads, dim):
+        raise ValueError(f"{name} must be a {dtype} tensor [{rows}, {heads}, {dim}] on cuda:{at}, not {t.dtype} {list(t.shape)} on {t.device}")
+    row, head, step = t.stride()
+    if step != 1 and dim > 1 and t.numel():
+        raise ValueError(f"elements of a head of {name} must be neighbours")
     # (the stride of an axis of one entry is not used, and says nothing)
-    return t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0
+    row, head = row if rows > 1 else 0, head if heads > 1 else 0
+    if written and ((row < dim and rows > 1) or (head < dim and heads > 1)) and t.numel():
+        raise ValueError(f"heads of {name} overlap")
+    return t.data_ptr(), row, head
 
 
 def _pool(k_pool, v_pool):
-    _need(k_pool.dtype in _DTYPES and k_pool.dim() == 4 and k_pool.device.type == "cuda",
-          "k_pool must be a float32 or bfloat16 tensor [n_blocks, n_kv_heads, page_size, head_dim] on the GPU")
-    _need(v_pool.dtype == k_pool.dtype and v_pool.shape == k_pool.shape and v_pool.device == k_pool.device,
-          "v_pool must have the type, shape and device of k_pool")
-    strides = [n if size > 1 else 0 for n, size in zip(k_pool.stride(), k_pool.shape)]
-    _need(strides == [n if size > 1 else 0 for n, size in zip(v_pool.stride(), v_pool.shape)] and strides[3] == 1,
-          "k_pool and v_pool must have the same strides, the last one 1")
-    n_blocks, heads, page, dim = k_pool.shape
-    return _Pool(k_pool.data_ptr(), v_pool.data_ptr(), strides[0], strides[1], strides[2], n_blocks, page, heads, dim, _DTYPES[k_pool.dtype])
+    """(struct, dtype, GPU number, heads, head size) of a pool."""
+    dtype, at, shape = k_pool.dtype, k_pool.get_device(), k_pool.shape
+    if dtype not in _DTYPES or len(shape) != 4 or at < 0:
+        raise ValueError("k_pool must be a float32 or bfloat16 tensor [n_blocks, n_kv_heads, page_size, head_dim] on the GPU")
+    if v_pool.dtype is not dtype or v_pool.shape != shape or v_pool.get_device() != at:
+        raise ValueError("v_pool must have the type, shape and device of k_pool")
+    strides = k_pool.stride()
+    if v_pool.stride() != strides or strides[3] != 1:
+        raise ValueError("k_pool and v_pool must have the same strides, the last one 1")
+    blocks, heads, page, dim = shape
+    return (_pack_pool(k_pool.data_ptr(), v_pool.data_ptr(), strides[0], strides[1], strides[2], blocks, page, heads, dim, _DTYPES[dtype]),
+            dtype, at, heads, dim)
 
 
-def _call(fn, device, stream, made, *structs):
-    """The call on `stream`, with the tensors' device current; made: tensors that were allocated for it."""
+_current_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
+
+
+def _call(fn, at, stream, made, *structs):
+    """The call on `stream`, with the tensors' device current; made: the tensor that was allocated for it, or None."""
     if stream is None:
-        handle = torch.cuda.current_stream(device).cuda_stream
+        handle = _current_stream(at)
     else:
-        _need(stream.device == device, f"the stream is on {stream.device}, the tensors on {device}")
+        if stream.device.index != at:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on cuda:{at}")
         handle = stream.cuda_stream
-        for t in made:
-            if t is not None:
-                t.record_stream(stream)
-    structs = [ctypes.byref(s) for s in structs]
-    if device.index == torch.cuda.current_device():
-        jb._check(fn(*structs, handle))
+        if made is not None:
+            made.record_stream(stream)
+    if at == _current_device():
+        status = fn(*structs, handle)
     else:
-        with torch.cuda.device(device):
-            jb._check(fn(*structs, handle))
+        with torch.cuda.device(at):
+            status = fn(*structs, handle)
+    if status:
+        jb._check(status)
 
 
 class Workspace:
@@ -148,63 +175,68 @@ class Workspace:
 
     def __init__(self, device="cuda:0"):
         self.buf = torch.zeros(_lib().jup_paged_workspace_bytes(), dtype=torch.uint8, device=device)
+        self.args = self.buf.data_ptr(), self.buf.numel()
+        self.at = self.buf.get_device()
 
 
-def _scratch(workspace, device):
-    _need(isinstance(workspace, Workspace) and workspace.buf.device == device, f"workspace must be a Workspace on {device}")
-    return workspace.buf.data_ptr(), workspace.buf.numel()
+def _scratch(workspace, at):
+    if not isinstance(workspace, Workspace) or workspace.at != at:
+        raise ValueError(f"workspace must be a Workspace on cuda:{at}")
+    return workspace.args
 
 
 def extend(lengths, n_new, owned, table, free_blocks, free_count, page_size, max_rows, in_place=False, stream=None):
     """Pages, positions and slots of a step (jup_paged_extend): ``Step(row_start, positions, slots, lengths, owned, free_count,
     status)``, int32 tensors; ``table`` gets the new pages.  in_place: lengths, owned and free_count are updated themselves."""
-    device, n = lengths.device, lengths.numel()
-    _need(device.type == "cuda", "lengths must be on the GPU")
-    for name, t in (("lengths", lengths), ("n_new", n_new), ("owned", owned)):
-        _ints(name, t, device, n)
-    _ints("free_blocks", free_blocks, device, None)
-    _ints("free_count", free_count, device, 1)
-    stride = _table(table, device, n)
+    at, n = lengths.get_device(), lengths.numel()
+    if at < 0:
+        raise ValueError("lengths must be on the GPU")
     max_rows = int(max_rows)
-    _need(max_rows >= 0, "max_rows must not be negative")
-    made = torch.empty(n + 1 + 2 * max_rows + 1 + (0 if in_place else 2 * n + 1), dtype=torch.int32, device=device)
-    sizes = [n + 1, max_rows, max_rows, 1] + ([] if in_place else [n, n, 1])
+    if max_rows < 0:
+        raise ValueError("max_rows must not be negative")
+    n_free = free_blocks.numel()
+    inputs = (_ints("lengths", lengths, at, n), _ints("n_new", n_new, at, n), _ints("owned", owned, at, n))
+    tables, width, stride = _table(table, at, n)
+    free = (_ints("free_blocks", free_blocks, at, n_free), _ints("free_count", free_count, at, 1))
+    sizes = [n + 1, max_rows, max_rows, 1] if in_place else [n + 1, max_rows, max_rows, 1, n, n, 1]
+    made = torch.empty(sum(sizes), dtype=_I32, device=lengths.device)
     row_start, positions, slots, status, *new = made.split(sizes)
     new_lengths, new_owned, new_count = (lengths, owned, free_count) if in_place else new
-    args = _Extend(n, int(page_size), table.shape[1], free_blocks.numel(), max_rows, stride, lengths.data_ptr(), n_new.data_ptr(),
-                   owned.data_ptr(), table.data_ptr(), free_blocks.data_ptr(), free_count.data_ptr(), row_start.data_ptr(),
-                   positions.data_ptr(), slots.data_ptr(), new_lengths.data_ptr(), new_owned.data_ptr(), new_count.data_ptr(),
-                   status.data_ptr())
-    _call(_lib().jup_paged_extend, device, stream, (made,), args)
+    base = made.data_ptr()
+    ends = base + 4 * (n + 1), base + 4 * (n + 1 + max_rows), base + 4 * (n + 1 + 2 * max_rows)
+    after = (inputs[0], inputs[2], free[1]) if in_place else (ends[2] + 4, ends[2] + 4 * (n + 1), ends[2] + 4 * (2 * n + 1))
+    _call(_lib().jup_paged_extend, at, stream, made,
+          _pack_extend(n, int(page_size), width, n_free, max_rows, stride, *inputs, tables, *free, base, ends[0], ends[1], *after, ends[2]))
     return Step(row_start, positions, slots, new_lengths, new_owned, new_count, status)
 
 
 def append(k, v, slots, k_pool, v_pool, positions=None, rope_theta=None, q=None, q_out=None, stream=None):
     """Rows k, v [rows, n_kv_heads, head_dim] into their slots (jup_paged_append), k rotated at ``positions`` if rope_theta is
     given; q [rows, n_heads, head_dim] is rotated into q_out (may be q; default: a new tensor), which is returned."""
-    pool = _pool(k_pool, v_pool)
-    dtype, device, rows = k_pool.dtype, k_pool.device, k.shape[0]
-    a = _Append(n_rows=rows, k=k.data_ptr(), v=v.data_ptr(), slots=slots.data_ptr())
-    a.k_row_stride, a.k_head_stride = _heads("k", k, dtype, device, pool.n_kv_heads, pool.head_dim)
-    a.v_row_stride, a.v_head_stride = _heads("v", v, dtype, device, pool.n_kv_heads, pool.head_dim, rows)
-    _ints("slots", slots, device, rows)
-    made = None
+    pool, dtype, at, kv_heads, dim = _pool(k_pool, v_pool)
+    rows = k.shape[0]
+    k_at, *k_strides = _heads("k", k, dtype, at, rows, kv_heads, dim)
+    v_at, *v_strides = _heads("v", v, dtype, at, rows, kv_heads, dim)
+    slots_at = _ints("slots", slots, at, rows)
     if rope_theta is None:
-        _need(q is None and q_out is None and positions is None, "q and positions go with rope_theta")
+        if q is not None or q_out is not None or positions is not None:
+            raise ValueError("q and positions go with rope_theta")
+        theta, positions_at = 0.0, 0
     else:
-        _need(positions is not None, "rope_theta goes with positions")
-        _need(rope_theta > 0, "rope_theta must be positive")
-        _ints("positions", positions, device, rows)
-        a.rope_theta, a.positions = rope_theta, positions.data_ptr()
+        if positions is None or not rope_theta > 0:
+            raise ValueError("rope_theta must be positive, and goes with positions")
+        theta, positions_at = rope_theta, _ints("positions", positions, at, rows)
+    made, heads, q_at, q_strides, out_at, out_strides = None, 0, 0, (0, 0), 0, (0, 0)
     if q is not None:
-        a.q_row_stride, a.q_head_stride = _heads("q", q, dtype, device, None, pool.head_dim, rows)
+        heads = q.shape[1] if q.dim() == 3 else -1
+        q_at, *q_strides = _heads("q", q, dtype, at, rows, heads, dim)
         if q_out is None:
-            q_out = made = torch.empty(q.shape, dtype=dtype, device=device)
-        a.q_out_row_stride, a.q_out_head_stride = _heads("q_out", q_out, dtype, device, q.shape[1], pool.head_dim, rows)
-        a.n_heads, a.q, a.q_out = q.shape[1], q.data_ptr(), q_out.data_ptr()
-    else:
-        _need(q_out is None, "q_out goes with q")
-    _call(_lib().jup_paged_append, device, stream, (made,), pool, a)
+            q_out = made = torch.empty(q.shape, dtype=dtype, device=q.device)
+        out_at, *out_strides = _heads("q_out", q_out, dtype, at, rows, heads, dim, written=True)
+    elif q_out is not None:
+        raise ValueError("q_out goes with q")
+    _call(_lib().jup_paged_append, at, stream, made, pool,
+          _pack_append(rows, heads, q_at, k_at, v_at, out_at, *q_strides, *k_strides, *v_strides, *out_strides, positions_at, slots_at, theta))
     return q_out
 
 
@@ -212,58 +244,65 @@ def attention(q, k_pool, v_pool, table, row_start, lengths, max_new, workspace=N
     """Attention of the rows q [rows, n_heads, head_dim] of a ragged batch over the pages (jup_paged_attention): out, of q's
     shape (default: a new tensor, whose rows outside the batch are not set).  lengths count the new tokens.  max_new: the most new tokens
     a request is expected to have.  workspace: a ``Workspace`` (not needed by float32 pools); scale: 1 / sqrt(head_dim) if None."""
-    pool = _pool(k_pool, v_pool)
-    dtype, device, n = k_pool.dtype, k_pool.device, lengths.numel()
-    a = _Attention(n_seqs=n, n_rows=q.shape[0], max_new=int(max_new), table_width=table.shape[-1])
-    a.q_row_stride, a.q_head_stride = _heads("q", q, dtype, device, None, pool.head_dim)
-    a.n_heads = q.shape[1]
+    pool, dtype, at, kv_heads, dim = _pool(k_pool, v_pool)
+    n = lengths.numel()
+    if q.dim() != 3:
+        raise ValueError("q must be a tensor [rows, n_heads, head_dim]")
+    rows, heads = q.shape[0], q.shape[1]
+    q_at, *q_strides = _heads("q", q, dtype, at, rows, heads, dim)
     made = None
     if out is None:
-        out = made = torch.empty(q.shape, dtype=dtype, device=device)
-    a.out_row_stride, a.out_head_stride = _heads("out", out, dtype, device, q.shape[1], pool.head_dim, q.shape[0])
-    _ints("lengths", lengths, device, None)
-    _ints("row_start", row_start, device, n + 1)
-    a.table_stride = _table(table, device, n)
-    a.q, a.out, a.row_start, a.lengths, a.table = q.data_ptr(), out.data_ptr(), row_start.data_ptr(), lengths.data_ptr(), table.data_ptr()
-    a.scale = 1.0 / math.sqrt(pool.head_dim) if scale is None else scale
-    if workspace is not None or dtype != torch.float32:
-        a.workspace, a.workspace_bytes = _scratch(workspace, device)
-    _call(_lib().jup_paged_attention, device, stream, (made,), pool, a)
+        out = made = torch.empty(q.shape, dtype=dtype, device=q.device)
+    out_at, *out_strides = _heads("out", out, dtype, at, rows, heads, dim, written=True)
+    tables, width, stride = _table(table, at, n)
+    _call(_lib().jup_paged_attention, at, stream, made, pool,
+          _pack_attention(n, rows, heads, int(max_new), width, stride, q_at, out_at, *q_strides, *out_strides,
+                          _ints("row_start", row_start, at, n + 1), _ints("lengths", lengths, at, n), tables,
+                          1.0 / math.sqrt(dim) if scale is None else scale,
+                          *(_scratch(workspace, at) if workspace is not None or dtype is not _F32 else (0, 0))))
     return out
+
+
+def _probs(name, t, dtype, at, rows, vocab):
+    if t.dtype is not dtype or t.get_device() != at or t.shape != (rows, vocab):
+        raise ValueError(f"{name} must be a {dtype} tensor [{rows}, {vocab}] on cuda:{at}, not {t.dtype} {list(t.shape)} on {t.device}")
+    row, step = t.stride()
+    if step != 1 and vocab > 1 and rows > 0:
+        raise ValueError(f"probabilities of a row of {name} must be neighbours")
+    return t.data_ptr(), row if rows > 1 else 0
+
+
+def _uniforms(name, t, at, n):
+    if t.dtype is not _F32 or t.get_device() != at or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous float32 tensor [{n}] on cuda:{at}, not {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
 
 
 def verify(tokens, target_probs, row_start, u_accept, u_sample, workspace, draft_probs=None, lengths=None, in_place=False, stream=None):
     """Verification of drafted tokens (jup_verify_drafts): ``Verdict(n_accepted, next_token, emitted, lengths)``, int32 tensors.
     tokens, u_accept [rows], probabilities [rows, vocab] (float32 or bfloat16), u_sample [n]; lengths: cached positions before the
     step (Verdict.lengths: those behind it, None without; in_place: in the same tensor)."""
-    device, n, rows = row_start.device, row_start.numel() - 1, tokens.numel()
-    _need(device.type == "cuda" and n >= 0, "row_start must be on the GPU and have an entry more than there are requests")
-    _ints("row_start", row_start, device, n + 1)
-    _ints("tokens", tokens, device, rows)
-    dtype = target_probs.dtype
-    _need(dtype in _DTYPES, "target_probs must be float32 or bfloat16")
-    a = _Verify(n_seqs=n, n_rows=rows, vocab=target_probs.shape[-1], probs_dtype=_DTYPES[dtype])
-    for name, t in (("target", target_probs), ("draft", draft_probs)):
-        if t is None:
-            continue
-        _need(t.dtype == dtype and t.device == device and t.dim() == 2 and tuple(t.shape) == (rows, a.vocab),
-              f"{name}_probs must be a {dtype} tensor [{rows}, {a.vocab}] on {device}")
-        _need(t.shape[1] < 2 or rows == 0 or t.stride(1) == 1, f"probabilities of a row of {name}_probs must be neighbours")
-        setattr(a, name + "_probs", t.data_ptr())
-        setattr(a, name + "_row_stride", t.stride(0) if rows > 1 else 0)
-    for name, t, size in (("u_accept", u_accept, rows), ("u_sample", u_sample, n)):
-        _need(t.dtype == torch.float32 and t.device == device and t.is_contiguous() and tuple(t.shape) == (size,),
-              f"{name} must be a contiguous float32 tensor [{size}] on {device}")
-        setattr(a, name, t.data_ptr())
+    at, n, rows, dtype = row_start.get_device(), row_start.numel() - 1, tokens.numel(), target_probs.dtype
+    if at < 0 or n < 0:
+        raise ValueError("row_start must be on the GPU and have an entry more than there are requests")
+    if dtype not in _DTYPES or target_probs.dim() != 2:
+        raise ValueError("target_probs must be a float32 or bfloat16 tensor [rows, vocab]")
+    vocab = target_probs.shape[1]
+    target, target_stride = _probs("target_probs", target_probs, dtype, at, rows, vocab)
+    draft, draft_stride = (0, 0) if draft_probs is None else _probs("draft_probs", draft_probs, dtype, at, rows, vocab)
+    sizes = [n, n, rows] if lengths is None or in_place else [n, n, rows, n]
+    made = torch.empty(sum(sizes), dtype=_I32, device=row_start.device)
+    n_accepted, next_token, emitted, *new = made.split(sizes)
+    base = made.data_ptr()
+    lengths_at = after_at = 0
     new_lengths = None
-    made = torch.empty(2 * n + rows + (n if lengths is not None and not in_place else 0), dtype=torch.int32, device=device)
-    n_accepted, next_token, emitted, rest = made.split([n, n, rows, made.numel() - 2 * n - rows])
     if lengths is not None:
-        _ints("lengths", lengths, device, n)
-        new_lengths = lengths if in_place else rest
-        a.lengths, a.new_lengths = lengths.data_ptr(), new_lengths.data_ptr()
-    a.tokens, a.row_start = tokens.data_ptr(), row_start.data_ptr()
-    a.n_accepted, a.next_token, a.emitted = n_accepted.data_ptr(), next_token.data_ptr(), emitted.data_ptr()
-    a.workspace, a.workspace_bytes = _scratch(workspace, device)
-    _call(_lib().jup_verify_drafts, device, stream, (made,), a)
+        lengths_at = after_at = _ints("lengths", lengths, at, n)
+        new_lengths = lengths
+        if not in_place:
+            new_lengths, after_at = new[0], base + 4 * (2 * n + rows)
+    _call(_lib().jup_verify_drafts, at, stream, made,
+          _pack_verify(n, rows, vocab, _DTYPES[dtype], _ints("tokens", tokens, at, rows), _ints("row_start", row_start, at, n + 1), target,
+                       draft, target_stride, draft_stride, _uniforms("u_accept", u_accept, at, rows), _uniforms("u_sample", u_sample, at, n),
+                       base, base + 4 * n, base + 8 * n, lengths_at, after_at, *_scratch(workspace, at)))
     return Verdict(n_accepted, next_token, emitted, new_lengths)
