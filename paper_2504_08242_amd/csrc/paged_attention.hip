@@ -67,7 +67,7 @@ __device__ __forceinline__ int pieces_of(int key_tiles, int chunk) { return max(
 
 template <int R>
 struct Request {
-    int begin, tokens, before, tiles, key_tiles;
+    int begin, tokens, before, tiles, key_tiles;  // key_tiles: of the last tile
     __device__ __forceinline__ Request(const Attention& a, int i, int last) {
         begin = tokens = before = tiles = key_tiles = 0;
         if (i >= last) return;
@@ -88,12 +88,18 @@ struct Request {
     __device__ __forceinline__ int keys_of(const Attention& a, int t) const {
         return (int)min(max((long long)before + t + 1, 0ll), (long long)a.positions);
     }
-    __device__ __forceinline__ float cost() const { return (float)tiles * (float)key_tiles; }
+    __device__ __forceinline__ float cost(const Attention& a) const {
+        if (R > 32 && tiles > 1)  // (half as much for a prompt from its first token on; at least half of tiles x key_tiles)
+            return (float)tiles * 0.5f * (float)(key_tiles + (keys_of(a, a.group.of(R - 1)) + kKT - 1) / kKT);
+        return (float)tiles * (float)key_tiles;
+    }
     __device__ __forceinline__ int pieces(int chunk) const { return tiles == 0 ? 0 : pieces_of(key_tiles, chunk); }
 };
 
 // Piece number `item` of a key/value head; false: there are fewer.  All lanes of a wave call it and get the same.  R: rows of a tile;
 // least: the shortest piece worth a workgroup, in key tiles.
+constexpr int kOrdered = 16;  // requests that are put in order of their lengths
+
 template <int R>
 __device__ bool find_work(const Attention& a, int item, int least, Work& w) {
     const int lane = threadIdx.x & 63;
@@ -104,8 +110,8 @@ __device__ bool find_work(const Attention& a, int item, int least, Work& w) {
         int items = 0, slots = 0;
         Request<R> r(a, first + lane * each, last);
         if (chunk == 0) {  // (first time round)
-            float cost = r.cost();
-            for (int j = 1; j < each; ++j) cost += Request<R>(a, first + lane * each + j, last).cost();
+            float cost = r.cost(a);
+            for (int j = 1; j < each; ++j) cost += Request<R>(a, first + lane * each + j, last).cost(a);
             // (rounded up by more than the sums are off: at most as many pieces more than tiles as are wanted, as the grid says)
             chunk = __builtin_amdgcn_readfirstlane((int)fminf(fmaxf(wave_sum(cost) * a.chunk_factor + 1.0f, (float)least), 1e9f));
         }
@@ -116,15 +122,25 @@ __device__ bool find_work(const Attention& a, int item, int least, Work& w) {
             if (p > 1) slots += x.tiles * p;
         }
         int items_to = items, slots_to = slots;
+        if (R > 32 && last - first <= kOrdered) {
+            // whole prompts: the requests with the most keys first, so that what is left for the end is short
+            for (int j = 0; j < last - first; ++j) {
+                const int keys = __builtin_amdgcn_readlane(r.key_tiles, j);
+                const bool before = keys > r.key_tiles || (keys == r.key_tiles && j < lane);
+                items_to += before ? __builtin_amdgcn_readlane(items, j) : 0;
+                slots_to += before ? __builtin_amdgcn_readlane(slots, j) : 0;
+            }
+        } else {
 #pragma unroll
-        for (int by = 1; by < 64; by *= 2) {
-            const int i = __shfl_up(items_to, by, 64), s = __shfl_up(slots_to, by, 64);
-            if (lane >= by) {
-                items_to += i;
-                slots_to += s;
+            for (int by = 1; by < 64; by *= 2) {
+                const int i = __shfl_up(items_to, by, 64), s = __shfl_up(slots_to, by, 64);
+                if (lane >= by) {
+                    items_to += i;
+                    slots_to += s;
+                }
             }
         }
-        const unsigned long long there = __ballot(items_to > item);
+        const unsigned long long there = __ballot(item < items_to && item >= items_to - items);
         if (!there) return false;
         const int at = __builtin_ctzll(there);
         item -= __builtin_amdgcn_readlane(items_to - items, at);
@@ -209,50 +225,110 @@ __device__ __forceinline__ u32x2 read_tr(unsigned lds_address) {
 
 // ---- values that are no numbers --------------------------------------------------------------------------------------------
 // The products of a tile are sums over all its 32 keys, with probability 0 where a row does not see a key; 0 times an infinity
-// or a NaN is NaN.  Tiles in which some row does not see some key are looked through for such values (three operations per
-// dword; one tile in a few has a mask at all).  Where there is one, the products go without them, and a second pair of
-// products counts, for every row and feature, the infinities of either sign that the row does see.
-__device__ __forceinline__ unsigned not_finite(u32x4 v) {  // bits 15 and 31 of a dword: an exponent of ones
+// or a NaN is NaN.  In tiles in which some row does not see some key (masked ones: a few per workgroup) such values are
+// therefore set to 0 in LDS, and what they do to the rows that do see them is added to the sums at the end, from memory.
+__device__ __forceinline__ unsigned not_finite(unsigned v) {  // bits 15 and 31: an exponent of ones
+    return ((v & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+}
+// A 16-byte piece of a row of values in a masked tile; there: the row is a key.  True: something was taken out of it.
+__device__ __forceinline__ bool clean_piece(unsigned char* at, bool there) {
+    u32x4 v = *(const u32x4*)at;
     unsigned any = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) any |= (v[e] & 0x7F807F80u) + 0x00800080u;
-    return any & 0x80008000u;
-}
-// (one accumulator holds both counts: 1 for a positive infinity, 64 for a negative one, 65 for a NaN; a tile has 32 keys, and all of
-// it is exact in bf16 and fp32)
-__device__ __forceinline__ void split_values(u32x4 v, u32x4& finite, u32x4& code) {
+    for (int e = 0; e < 4; ++e) any |= not_finite(v[e]);
+    if (there && !any) return false;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        unsigned f = 0, k = 0;
+        const unsigned bad = not_finite(v[e]);
+        v[e] = there ? v[e] & ~((bad & 0x8000u ? 0xFFFFu : 0u) | (bad & 0x80000000u ? 0xFFFF0000u : 0u)) : 0u;
+    }
+    *(u32x4*)at = v;
+    return there;
+}
+// What was taken out of a key's values, for four features from `feature` on (registers r .. r + 3 of sums), if the row sees the key.
+template <class V>
+__device__ __forceinline__ void add_not_finite(V& sums, int r, const char* row, int feature, bool sees) {
+    const u32x2 v = *(const u32x2*)(row + feature * 2);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const unsigned x = (v[e] >> (16 * h)) & 0xFFFFu;
-            const bool special = (x & 0x7F80u) == 0x7F80u;
-            const unsigned what = (x & 0x7Fu) ? 0x4282u : x & 0x8000u ? 0x4280u : 0x3F80u;  // bf16 65, 64, 1
-            f |= (special ? 0u : x) << (16 * h);
-            k |= (special ? what : 0u) << (16 * h);
-        }
-        finite[e] = f;
-        code[e] = k;
+    for (int e = 0; e < 2; ++e) {
+        const unsigned bad = not_finite(v[e]);
+        if (sees && (bad & 0x8000u)) sums[r + 2 * e] += bf2f((u16)v[e]);
+        if (sees && (bad >> 31)) sums[r + 2 * e + 1] += bf2f((u16)(v[e] >> 16));
     }
 }
-__device__ __forceinline__ float with_counts(float sum, float code) {
-    if (code >= 64.0f) sum -= INFINITY;
-    if (code != 0.0f && code != 64.0f * floorf(code * (1.0f / 64.0f))) sum += INFINITY;
-    return sum;
+// Whether a row of values in memory has any (all lanes get the same).
+__device__ __forceinline__ bool row_not_finite(const char* row) {
+    return __any(not_finite(*(const unsigned*)(row + 4 * (threadIdx.x & 63))) != 0);
 }
 
 // ---- pieces of one tile put together ------------------------------------------------------------------------------------------
 // The workgroups of a tile's pieces leave un-normalised sums and their softmax statistics in the scratch; the one that
 // arrives last adds them in the order of the pieces (the result does not depend on who that is) and writes the rows.  Nobody
-// waits.  flag: an LDS word that nobody else uses any more; THREADS: of the workgroup, all of which call it.
-template <int R, int THREADS>
+// waits.  A wave has a row, a lane two neighbouring features: whole lines go to memory and back (8 bytes at 32-byte steps, as the
+// sums lie in the registers, are a partial write each).
+
+// N rows per wave, PC pieces of each in flight at once: they come from memory, microseconds away.
+template <int WAVES, int N, int PC>
+__device__ __forceinline__ void join_rows(const Attention& a, const Work& w, int R, int kv_head, int rows, const float* base, long long step) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    float m[N], l[N];
+    float2 acc[N];
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+        m[x] = -INFINITY;
+        l[x] = acc[x].x = acc[x].y = 0.f;
+    }
+    for (int p0 = 0; p0 < w.pieces; p0 += PC) {
+        float2 stat[N][PC], val[N][PC];
+#pragma unroll
+        for (int x = 0; x < N; ++x)
+#pragma unroll
+            for (int p = 0; p < PC; ++p) {
+                if (wave + x * WAVES >= rows || p0 + p >= w.pieces) continue;
+                const float* from = base + (p0 + p) * step + (long long)(wave + x * WAVES) * kPartRow;
+                stat[x][p] = load_coherent2(from + 128);
+                val[x][p] = load_coherent2(from + 2 * lane);
+            }
+#pragma unroll
+        for (int x = 0; x < N; ++x) {
+            if (wave + x * WAVES >= rows) continue;
+            float top = m[x];
+#pragma unroll
+            for (int p = 0; p < PC; ++p)
+                if (p0 + p < w.pieces) top = fmaxf(top, stat[x][p].x);
+            if (top == -INFINITY) top = 0.f;
+            const float back = __builtin_amdgcn_exp2f(m[x] - top);
+            l[x] *= back;
+            acc[x].x *= back;
+            acc[x].y *= back;
+#pragma unroll
+            for (int p = 0; p < PC; ++p)
+                if (p0 + p < w.pieces && stat[x][p].y != 0.f) {  // (0: a piece this row sees nothing of)
+                    const float f = __builtin_amdgcn_exp2f(stat[x][p].x - top);
+                    l[x] += stat[x][p].y * f;
+                    acc[x].x += val[x][p].x * f;
+                    acc[x].y += val[x][p].y * f;
+                }
+            m[x] = top;
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+        if (wave + x * WAVES >= rows) continue;
+        const float inv = l[x] == 0.f ? 0.f : 1.0f / l[x];
+        const int row = w.tile * R + wave + x * WAVES, token = a.group.of(row);
+        *(unsigned*)(a.out + (long long)(w.begin + token) * a.out_row + (long long)((kv_head - token) * (int)a.group.d + row) * a.out_head + 2 * lane) =
+            pack_bf16x2(acc[x].x * inv, acc[x].y * inv);
+    }
+}
+
+// flag: an LDS word that nobody else uses any more; all waves of the workgroup call it.
+template <int R, int WAVES>
 __device__ __forceinline__ void join_pieces(const Work& w, int kv_head, int* flag) {
     const Attention a = args_again();
-    const int tid = threadIdx.x;
     wait_stores_performed();
     __syncthreads();
-    if (tid == 0) {
+    if (threadIdx.x == 0) {
         int* count = a.count + (long long)w.slot * a.n_kv_heads + kv_head;
         const int before = arrive_coherent(count);
         *flag = before == w.pieces - 1;
@@ -263,48 +339,23 @@ __device__ __forceinline__ void join_pieces(const Work& w, int kv_head, int* fla
     const long long step = (long long)a.n_kv_heads * R * kPartRow;
     const float* base = a.partial + ((long long)w.slot * a.n_kv_heads + kv_head) * R * kPartRow;
     const int rows = min(R, w.tokens * (int)a.group.d - w.tile * R);
-    for (int idx = tid; idx < rows * 16; idx += THREADS) {
-        const int r = idx >> 4, ch = idx & 15;
-        float m = -INFINITY, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        for (int p0 = 0; p0 < w.pieces; p0 += 8) {  // eight pieces in flight: they come from memory
-            float2 stat[8], val[8][4];
+    constexpr int N = R / WAVES;
+    if (rows <= WAVES) join_rows<WAVES, 1, 24>(a, w, R, kv_head, rows, base, step);
+    else join_rows<WAVES, N, (N >= 32 ? 1 : 32 / N)>(a, w, R, kv_head, rows, base, step);
+}
+// A workgroup's sums of row r, in LDS as `PARTS` partial ones `region` bytes apart, into their place in the scratch.
+template <int PARTS, int WAVES>
+__device__ __forceinline__ void store_pieces(const unsigned char* sums, int row_bytes, int region, float* place, int rows) {
+    const int lane = threadIdx.x & 63;
+    for (int r = threadIdx.x >> 6; r < rows; r += WAVES) {
+        float2 x = *(const float2*)(sums + r * row_bytes + lane * 8);
 #pragma unroll
-            for (int p = 0; p < 8; ++p)
-                if (p0 + p < w.pieces) {
-                    const float* row = base + (p0 + p) * step + (long long)r * kPartRow;
-                    stat[p] = load_coherent2(row + 128);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) val[p][e] = load_coherent2(row + ch * 8 + 2 * e);
-                }
-            float top = m;
-#pragma unroll
-            for (int p = 0; p < 8; ++p)
-                if (p0 + p < w.pieces) top = fmaxf(top, stat[p].x);
-            if (top == -INFINITY) top = 0.f;
-            const float back = __builtin_amdgcn_exp2f(m - top);
-            l *= back;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) acc[e] *= back;
-#pragma unroll
-            for (int p = 0; p < 8; ++p)
-                if (p0 + p < w.pieces && stat[p].y != 0.f) {  // (0: a piece this row sees nothing of)
-                    const float f = __builtin_amdgcn_exp2f(stat[p].x - top);
-                    l += stat[p].y * f;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        acc[2 * e] += val[p][e].x * f;
-                        acc[2 * e + 1] += val[p][e].y * f;
-                    }
-                }
-            m = top;
+        for (int k = 1; k < PARTS; ++k) {
+            const float2 y = *(const float2*)(sums + k * region + r * row_bytes + lane * 8);
+            x.x += y.x;
+            x.y += y.y;
         }
-        const float inv = l == 0.f ? 0.f : 1.0f / l;
-        const int token = a.group.of(w.tile * R + r);
-        const int in_group = w.tile * R + r - token * (int)a.group.d;
-        u32x4 o;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = pack_bf16x2(acc[2 * e] * inv, acc[2 * e + 1] * inv);
-        *(u32x4*)(a.out + (long long)(w.begin + token) * a.out_row + (long long)(kv_head * (int)a.group.d + in_group) * a.out_head + ch * 8) = o;
+        store_coherent2(place + (long long)r * kPartRow + 2 * lane, x.x, x.y);
     }
 }
 
@@ -407,12 +458,9 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void attention_few(const Attenti
 #pragma unroll
     for (int db = 0; db < 4; ++db)
         v_lane[db] = v_base + vt_row * 256 + ((db ^ (vt_row & 3)) << 6) + ((QW == 16 ? 0 : 2 * (quad & 1)) + ((s & 3) >> 1)) * 16 + 8 * (s & 1);
-    auto product = [](u32x4 x, bf16x8 p, acc_t acc) {
-        if constexpr (QW == 16) return mfma16(__builtin_bit_cast(bf16x8, x), p, acc);
-        else return mfma32(__builtin_bit_cast(bf16x8, x), p, acc);
-    };
     auto key_of = [](int r) { return (QW == 16 ? 16 : 8) * (r >> 2) + (r & 3); };  // of the lane's score r, less 4 hh
     const unsigned char* k_base = lds + wave * 2 * kTileBytes;
+    bool special = false;  // values that are no numbers were taken out of a tile (of this lane's pieces)
 
     for (; tile < w.tile_hi; tile += NW) {
         const bool more = tile + NW < w.tile_hi;
@@ -448,18 +496,14 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void attention_few(const Attenti
 
         // ---- online softmax ----
         const bool masked = tile >= first_masked || there != ~0u;
-        unsigned sees = ~0u;  // bit r: this lane's row sees the key of its score r
         if (masked) {
             // (opaque: keeps this a branch, as selects it would run for every tile, and its numbers out of the registers between tiles)
             int quarter = 4 * hh;
             asm volatile("" : "+v"(quarter));
-            sees = 0;
 #pragma unroll
             for (int r = 0; r < NS; ++r) {
                 const int key = quarter + key_of(r);
-                const bool yes = tile * kKT + key <= q_abs && ((there >> key) & 1);
-                sv[r] = yes ? sv[r] : -INFINITY;
-                sees |= (unsigned)yes << r;
+                if (tile * kKT + key > q_abs || !((there >> key) & 1)) sv[r] = -INFINITY;
             }
         }
         float mt = -INFINITY;
@@ -494,52 +538,44 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void attention_few(const Attenti
         // ---- O^T += V^T P^T ----
         if (more) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // V has landed, the next K may be in flight
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        bool special = false;
         if (masked) {
             asm volatile("");
-            unsigned any = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                u32x4* piece = (u32x4*)(lds + wave * 2 * kTileBytes + kTileBytes + j * 1024 + lane * 16);  // of row 4j + lrow
-                if ((there >> (4 * j + lrow)) & 1) any |= not_finite(*piece);
-                else *piece = (u32x4){0, 0, 0, 0};  // no key: whatever lies there becomes 0
-            }
-            special = __any(any != 0);
+            for (int j = 0; j < 8; ++j)  // rows 4j .. 4j + 3
+                special |= clean_piece(lds + wave * 2 * kTileBytes + kTileBytes + j * 1024 + lane * 16, (there >> (4 * j + lrow)) & 1);
         }
-        // fragment f: QW = 32: feature block f / 2, key half f % 2; QW = 16: feature block f, all 32 keys
-        auto value = [&](int f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int f = 0; f < 8; ++f) {
+            // QW = 32: feature block f / 2, key half f % 2; QW = 16: feature block f, all 32 keys
             const unsigned at = v_lane[f / 2] + (QW == 16 ? (f % 2) * 32 : (f % 2) * 16 * 256);
             const u32x2 lo = read_tr(at), hi = read_tr(at + (QW == 16 ? 16 * 256 : 8 * 256));
-            return (u32x4){lo[0], lo[1], hi[0], hi[1]};
-        };
-        if (special) {
-            bf16x8 seen[NS / 8];
-#pragma unroll
-            for (int r = 0; r < NS; ++r) seen[r >> 3][r & 7] = (__bf16)(float)((sees >> r) & 1);
-#pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                acc_t codes;
-#pragma unroll
-                for (int r = 0; r < NR; ++r) codes[r] = 0.f;
-#pragma unroll
-                for (int h = 0; h < 8 / DB; ++h) {
-                    u32x4 finite, code;
-                    split_values(value(db * (8 / DB) + h), finite, code);
-                    oacc[db] = product(finite, pf[h], oacc[db]);
-                    codes = product(code, seen[h], codes);
-                }
-#pragma unroll
-                for (int r = 0; r < NR; ++r) oacc[db][r] = with_counts(oacc[db][r], codes[r]);
-            }
-        } else {
-#pragma unroll
-            for (int f = 0; f < 8; ++f) oacc[f * DB / 8] = product(value(f), pf[f % (8 / DB)], oacc[f * DB / 8]);
+            const bf16x8 v = __builtin_bit_cast(bf16x8, (u32x4){lo[0], lo[1], hi[0], hi[1]});
+            if constexpr (QW == 16) oacc[f] = mfma16(v, pf[0], oacc[f]);
+            else oacc[f / 2] = mfma32(v, pf[f % 2], oacc[f / 2]);
         }
         if (more) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the V slot has been read
             fill(tile + NW, next, true);
             here = next;
             if (tile + 2 * NW < w.tile_hi) next = blocks_of(a, table_row, tile + 2 * NW, last_key);
+        }
+    }
+
+    if (__any(special)) {  // once in a blue moon
+        for (tile = w.tile_lo + wave; tile < w.tile_hi; tile += NW) {
+            const Blocks b = blocks_of(a, table_row, tile, last_key);
+            const unsigned there = rows_there(a, b, tile, last_key);
+            if (tile < first_masked && there == ~0u) continue;
+            for (int k = 0; k < kKT; ++k) {
+                if (!((there >> k) & 1)) continue;
+                const char* row = group_base(a, v_pool, b.id[k >> 3], tile * kKT + (k & ~7)) + (k & 7) * row_bytes;
+                if (!row_not_finite(row)) continue;
+#pragma unroll
+                for (int x = 0; x < (QW == 16 ? 8 : 16); ++x) {
+                    const int db = QW == 16 ? x : x >> 2, r = QW == 16 ? 0 : 4 * (x & 3);
+                    add_not_finite(oacc[db], r, row, (QW == 16 ? 16 * x : 8 * x) + 4 * hh, tile * kKT + k <= q_abs);
+                }
+            }
         }
     }
 
@@ -586,6 +622,11 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void attention_few(const Attenti
         if (w.pieces > 1 && wave == 0 && hh == 0 && c < rows) store_coherent2(e.partial + (part + c) * kPartRow + 128, m_all, l_all);
     }
     __syncthreads();
+    if (w.pieces > 1) {
+        store_pieces<NW, NW>(lds, kRow * 4, kRegion * 4, e.partial + part * kPartRow, rows);
+        join_pieces<QW, NW>(w, kv_head, (int*)(lds + few_stat(QW)));
+        return;
+    }
     for (int idx = tid; idx < rows * 16; idx += 64 * NW) {
         const int r = idx >> 4, ch = idx & 15;
         const float* src = obuf + r * kRow + ch * 8;
@@ -596,21 +637,376 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void attention_few(const Attenti
             x.x += x2.x; x.y += x2.y; x.z += x2.z; x.w += x2.w;
             y.x += y2.x; y.y += y2.y; y.z += y2.z; y.w += y2.w;
         }
-        if (w.pieces > 1) {
-            float* dst = e.partial + (part + r) * kPartRow + ch * 8;
-            store_coherent2(dst, x.x, x.y);
-            store_coherent2(dst + 2, x.z, x.w);
-            store_coherent2(dst + 4, y.x, y.y);
-            store_coherent2(dst + 6, y.z, y.w);
-            continue;
-        }
         const int row = w.tile * QW + r, token = e.group.of(row);
         u32x4 o;
         o[0] = pack_bf16x2(x.x, x.y); o[1] = pack_bf16x2(x.z, x.w);
         o[2] = pack_bf16x2(y.x, y.y); o[3] = pack_bf16x2(y.z, y.w);
         *(u32x4*)(e.out + (long long)(w.begin + token) * e.out_row + (long long)((kv_head - token) * (int)e.group.d + row) * e.out_head + ch * 8) = o;
     }
-    if (w.pieces > 1) join_pieces<QW, 64 * NW>(w, kv_head, (int*)(lds + few_stat(QW)));
+}
+
+// ---- many rows -----------------------------------------------------------------------------------------------------------------
+// Prompts and long chunks, bound by the matrix cores.  Eight waves of 32 rows each; keys come in steps, K and V in LDS for all
+// waves, and the waves meet once per step.  Two waves share a SIMD: one's exponentials lie under the other's products.
+// KP parts of the keys: a workgroup has 256 / KP rows, and KP waves divide the keys of 32 of them and add up through LDS at the
+// end.  One part reads a key for the most rows; more parts make more workgroups of fewer rows, where rows are few or
+// where triangles of different sizes are to be dealt to the CUs.
+template <int NW, int KP, int NT, int SUB, int RING>
+struct Many {
+    static constexpr int kWaves = NW;
+    static constexpr int kRows = 32 * NW / KP;
+    static constexpr int kSubTiles = KP * NT;                // a wave works through NT tiles at a time, SUB times between two meetings
+    static constexpr int kStepTiles = SUB * kSubTiles;
+    static constexpr int kStep = kStepTiles * kKT;           // keys of a step
+    static constexpr int kHalf = kStepTiles * kTileBytes;    // K tiles, then V tiles
+    static constexpr int kRing = RING;                       // steps in LDS
+    static constexpr int kGroups = kStepTiles * 4 / kWaves;  // groups of eight rows that a wave fetches per step: wave, wave + NW
+    static_assert(kGroups * kWaves == kStepTiles * 4);
+    static constexpr int kRowBytes = 132 * 4;                // a row of a part's sums
+    static constexpr int kSteps = kRing * 2 * kHalf, kSums = KP > 1 ? 32 * NW * kRowBytes : 0, kQ = 32 * NW * 256;
+    static constexpr int kThere = (kSteps > kSums ? kSteps > kQ ? kSteps : kQ : kSums);  // [kRing][kStepTiles * 4] bytes: which rows of a step's groups are keys
+    static constexpr int kFlag = kThere + 64;
+    static constexpr int kStat = kFlag + 64;                 // [2][waves][32] maxima and sums
+    static constexpr int kLds = kStat + (KP > 1 ? 2 * 32 * NW * 4 : 0);
+    static_assert(kLds <= 160 * 1024 && kRing * kStepTiles * 4 <= 64);
+    // queries go through the last places of the ring, the first kFirst steps are fetched beside them
+    static constexpr int kFirst = (kThere - kQ) / (2 * kHalf) < kRing - 1 ? (kThere - kQ) / (2 * kHalf) : kRing - 1;
+    static constexpr int kQAt = kThere - kQ;
+    // Only the shape with the fewest rows divides keys among workgroups: the sums of 64 rows are 34 KB per piece, and one CU reads them all.
+    static constexpr bool kSplits = KP == 4;
+};
+
+// Waits until at most `steps` steps' loads of this wave (four or eight each) are in flight.
+template <int LOADS>
+__device__ __forceinline__ void wait_steps(int steps) {
+    if (steps >= 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * LOADS) : "memory");
+    else if (steps == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS) : "memory");
+    else if (steps == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+template <int NW, int KP, int NT, int SUB, int RING, int OCC>
+__global__ __launch_bounds__(64 * NW, OCC) void attention_many(const Attention args, int least) {
+    typedef Many<NW, KP, NT, SUB, RING> L;
+    constexpr int kRing = L::kRing, kHalf = L::kHalf, kStep = L::kStep, kRows = L::kRows;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 31, hh = lane >> 5;
+    const int part = wave % KP, r_wave = wave / KP * 32;  // this wave's keys of a step, and its rows
+    const int kv_head = (int)(blockIdx.x % (unsigned)args.n_kv_heads), item = (int)(blockIdx.x / (unsigned)args.n_kv_heads);
+    Work w;
+    if (!find_work<kRows>(args, item, least, w)) return;
+    w.make_uniform();
+    const Attention a = args_again();
+    const int G = a.group.d;
+    const int rows = min(kRows, w.tokens * G - w.tile * kRows);
+    const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_byte_address(lds));
+    const int lrow = lane >> 4, lp = lane & 15;
+
+    // this wave's eight rows of a step: group `wave` (and wave + 8)
+    const int last_key = w.keys - 1, first_key = w.tile_lo * kKT;
+    const int n = (w.tile_hi - w.tile_lo + L::kStepTiles - 1) / L::kStepTiles;
+    const int* table_row = (const int*)uniform_ptr((const char*)(a.table + w.seq * a.table_row));
+    typedef const __attribute__((address_space(4))) int* scalar;
+    const u16* k_pool = a.k + kv_head * a.head;
+    const u16* v_pool = a.v + kv_head * a.head;
+    // keys of this piece: up to the last key, or where the next piece begins
+    const int end_key = min(last_key + 1, w.tile_hi * kKT);
+    unsigned k_off[2], v_off[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const unsigned row = (unsigned)(a.slot * 2) * (4 * j + lrow);
+        k_off[j] = row + (lp ^ ((8 * wave + 4 * j + lrow) & 15)) * 16;
+        v_off[j] = row + ((((lp >> 2) ^ lrow) << 2) | (lp & 3)) * 16;
+    }
+    struct Ids {
+        int id[L::kGroups];
+    };
+    auto ids_of = [&](int i) {
+        Ids x;
+#pragma unroll
+        for (int g = 0; g < L::kGroups; ++g) x.id[g] = ((scalar)table_row)[min(first_key + i * kStep + 8 * NW * g + 8 * wave, last_key) >> a.shift];
+        return x;
+    };
+    unsigned hole = 0;  // bit: in that slot, some of this wave's rows are no keys
+    // K of step i, or V, and which rows are keys
+    auto fill = [&](int i, const Ids& ids, bool v_part) __attribute__((always_inline)) {
+        if (v_part) hole &= ~(1u << (i % kRing));
+#pragma unroll
+        for (int g = 0; g < L::kGroups; ++g) {
+            const int mine = first_key + i * kStep + 8 * NW * g + 8 * wave, key = min(mine, last_key & ~7);  // (groups behind the last key repeat its own)
+            unsigned slot = lds0 + (unsigned)(i % kRing) * 2 * kHalf + (v_part ? kHalf : 0) + (NW * g + wave) * 2048;
+            asm volatile("" : "+v"(slot));  // (see attention_few)
+            const unsigned dst = __builtin_amdgcn_readfirstlane(slot);
+            const char* base = group_base(a, v_part ? v_pool : k_pool, ids.id[g], key);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) load_to_lds_16(base, v_part ? v_off[j] : k_off[j], dst + j * 1024);
+            if (!v_part) continue;
+            const int left = end_key - mine;
+            const unsigned there = (unsigned)ids.id[g] >= (unsigned)a.n_blocks || left <= 0 ? 0u : left >= 8 ? 0xFFu : (1u << left) - 1;
+            hole |= there == 0xFFu ? 0u : 1u << (i % kRing);
+            if (lane == 0) lds[L::kThere + (i % kRing) * L::kStepTiles * 4 + NW * g + wave] = (unsigned char)there;
+        }
+    };
+    // Queries: this wave's 32 rows go through LDS (the second half of the steps' places) into B operands; rows past the last one repeat it.
+    // (As plain loads they would be waited for with everything issued behind them: the compiler does not know of the tiles.)
+    unsigned char* q_lds = lds + L::kQAt + wave * 8192;
+    const unsigned q_at = lds0 + L::kQAt + wave * 8192;
+    for (int r0 = 0; r0 < 32; r0 += 4) {
+        const int row = w.tile * kRows + min(r_wave + r0 + lrow, rows - 1), token = a.group.of(row);
+        const u16* from = a.q + (long long)(w.begin + token) * a.q_row + (long long)(kv_head * G + row - token * G) * a.q_head;
+        load_to_lds_16(from + (lp ^ ((r0 + lrow) & 15)) * 8, __builtin_amdgcn_readfirstlane(q_at + r0 * 256));
+    }
+    if (tid == 0) lds[L::kFlag] = 0;
+    Ids ids{};
+    if (n > 0) ids = ids_of(0);
+    auto fill_next = [&](int i, bool k_part, bool v_part) __attribute__((always_inline)) {  // step i, then the block numbers of the one behind it
+        if (i >= n) return;
+        if (k_part) fill(i, ids, false);
+        if (v_part) {
+            const Ids next = ids_of(i + 1);
+            fill(i, ids, true);
+            ids = next;
+        }
+    };
+    for (int i = 0; i < L::kFirst; ++i) fill_next(i, true, true);
+
+    // Sub-steps (NT tiles per part) before this one: every row of the workgroup sees all their keys.
+    constexpr int kSub = L::kSubTiles * kKT;
+    const int open = __builtin_amdgcn_readfirstlane((int)min(max(max((long long)w.before + a.group.of(w.tile * kRows) + 1, 0ll) - first_key, 0ll) / kSub, (long long)n * SUB));
+    // Behind the wait for this wave's rows of step i: rows that are no keys become 0, and where some row sees some key and another
+    // does not, values that are no numbers do.
+    bool special = false;
+    auto clean = [&](int i) __attribute__((always_inline)) {
+        if ((i + 1) * SUB <= open && !((hole >> (i % kRing)) & 1)) return;
+#pragma unroll
+        for (int g = 0; g < L::kGroups; ++g) {
+            const unsigned there = lds[L::kThere + (i % kRing) * L::kStepTiles * 4 + NW * g + wave];
+            unsigned char* at = lds + (i % kRing) * 2 * kHalf + kHalf + (NW * g + wave) * 2048 + lane * 16;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const bool key = (there >> (4 * j + lrow)) & 1;
+                if (i * SUB + (NW * g + wave) / (4 * L::kSubTiles) >= open || !key) special |= clean_piece(at + j * 1024, key);
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    };
+    // the last key that this lane's row sees; sub-steps that some row of this wave sees
+    const int sees_to = w.before + a.group.of(w.tile * kRows + min(r_wave + c, rows - 1));
+    const long long seen = (long long)w.before + a.group.of(w.tile * kRows + min(r_wave + 31, rows - 1)) + 1 - first_key;
+    const int mine = __builtin_amdgcn_readfirstlane(r_wave >= rows ? 0 : (int)min(max((seen + kSub - 1) / kSub, 0ll), (long long)n * SUB));
+
+    f32x16 o[4];
+    float m_run = -INFINITY, l_run = 0.f;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[db][r] = 0.f;
+    const unsigned k_lane = c * 256 + ((hh ^ (c & 15)) * 16);
+    const int quad = lane >> 4, sl = lane & 15;
+    const int vt_row = 4 * (quad >> 1) + (sl >> 2);
+    unsigned v_lane[4];
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+        v_lane[db] = lds0 + kHalf + vt_row * 256 + ((db ^ (vt_row & 3)) << 6) + (2 * (quad & 1) + ((sl & 3) >> 1)) * 16 + 8 * (sl & 1);
+    bf16x8 qf[8];
+    wait_steps<4 * L::kGroups>(min(n, L::kFirst));  // the queries have landed
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const bf16x8*)(q_lds + (k_lane ^ (32 * ks)));
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();  // every wave has its queries: steps may go there
+    asm volatile("" ::: "memory");
+    for (int i = L::kFirst; i < kRing - 1; ++i) fill_next(i, true, true);
+
+    for (int i = 0; i < n; ++i) {
+        // step i is there for all, and step i - 1 has been read by all
+        wait_steps<4 * L::kGroups>(min(n - 1 - i, kRing - 2));
+        clean(i);
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        // Step i + kRing - 1 goes where step i - 1 was.  (Its loads are put between the products: the address path of a CU takes 64 bytes per
+        // clock, and with all waves' loads behind the meeting every wave would wait for it there.)
+#pragma unroll
+      for (int u = 0; u < SUB; ++u) {
+        if (i * SUB + u >= mine) {
+            fill_next(i + kRing - 1, u == 0, u == SUB - 1);
+            continue;
+        }
+        const int first_tile = (u * KP + part) * NT;  // of this wave's keys of the sub-step
+        const unsigned char* k_base = lds + (i % kRing) * 2 * kHalf + first_tile * kTileBytes;
+        const unsigned v_slot = (unsigned)(i % kRing) * 2 * kHalf + first_tile * kTileBytes;
+        const int key0 = first_key + i * kStep + first_tile * kKT;
+        unsigned there[NT], whole = ~0u;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) there[t] = *(const unsigned*)(lds + L::kThere + (i % kRing) * L::kStepTiles * 4 + (first_tile + t) * 4);
+
+        // ---- S^T = K Q^T ----
+        f32x16 s[NT];
+        bf16x8 kf[NT][8];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) kf[t][ks] = *(const bf16x8*)(k_base + t * kTileBytes + (k_lane ^ (32 * ks)));
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[t][r] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) s[t] = mfma32(kf[t][ks], qf[ks], s[t]);
+        }
+        // the first tile's values are on their way under the exponentials
+        u32x4 vf[8];
+        auto read_v = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+            for (int f = 0; f < 8; ++f) {  // feature block f / 2, key half f % 2
+                const unsigned at = v_slot + t * kTileBytes + v_lane[f / 2] + (f % 2) * 16 * 256;
+                const u32x2 lo = read_tr(at), hi = read_tr(at + 8 * 256);
+                vf[f] = (u32x4){lo[0], lo[1], hi[0], hi[1]};
+            }
+        };
+        read_v(0);
+
+        fill_next(i + kRing - 1, u == 0, false);
+
+        // ---- online softmax (see attention_few) ----
+        float sv[16 * NT];
+#pragma unroll
+        for (int r = 0; r < 16 * NT; ++r) sv[r] = s[r >> 4][r & 15];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) whole &= there[t] = __builtin_amdgcn_readfirstlane(there[t]);
+        if (i * SUB + u >= open || whole != ~0u) {
+            int quarter = 4 * hh;
+            asm volatile("" : "+v"(quarter));
+#pragma unroll
+            for (int r = 0; r < 16 * NT; ++r) {
+                const int key = quarter + 8 * ((r & 15) >> 2) + (r & 3);
+                if (key0 + 32 * (r >> 4) + key > sees_to || !((there[r >> 4] >> key) & 1)) sv[r] = -INFINITY;
+            }
+        }
+        float mt = sv[0];
+#pragma unroll
+        for (int r = 1; r < 16 * NT; ++r) mt = fmaxf(mt, sv[r]);
+        mt = max_across_halves(mt) * a.scale_log2e;
+        const bool grow = mt > m_run + 8.0f;
+        const float m_new = grow ? mt : m_run;
+        const float m_safe = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = grow ? __builtin_amdgcn_exp2f(m_run - m_safe) : 1.0f;
+        if (__any(grow && m_run != -INFINITY)) {
+#pragma unroll
+            for (int db = 0; db < 4; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
+        }
+        float ps = 0.f;
+        bf16x8 p[2 * NT];
+#pragma unroll
+        for (int r = 0; r < 16 * NT; ++r) {
+            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[r], a.scale_log2e, -m_safe));
+            ps += x;
+            p[r >> 3][r & 7] = (__bf16)x;
+        }
+        l_run = l_run * alpha + ps;
+        m_run = m_new;
+
+        fill_next(i + kRing - 1, false, u == SUB - 1);
+
+        // ---- O^T += V^T P^T ----
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int f = 0; f < 8; ++f) o[f / 2] = mfma32(__builtin_bit_cast(bf16x8, vf[f]), p[2 * t + f % 2], o[f / 2]);
+            if (t + 1 < NT) read_v(t + 1);
+        }
+      }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the step has been read
+    }
+    if (__any(special)) lds[L::kFlag] = 1;
+
+    // ---- results -------------------------------------------------------------------------------------------------------------
+    const Attention e = args_again();
+    __syncthreads();  // every wave is done with the steps
+    if (lds[L::kFlag]) {  // once in a blue moon: what clean() took out
+        for (int tile = w.tile_lo + L::kSubTiles * open; tile < min(w.tile_hi, w.tile_lo + L::kSubTiles * mine); ++tile) {
+            if ((tile - w.tile_lo) / NT % KP != part) continue;
+            const Blocks ids = blocks_of(a, table_row, tile, last_key);
+            const unsigned there = rows_there(a, ids, tile, last_key);
+            for (int k = 0; k < kKT; ++k) {
+                if (!((there >> k) & 1)) continue;
+                const char* row = group_base(a, v_pool, ids.id[k >> 3], tile * kKT + (k & ~7)) + (k & 7) * (unsigned)(a.slot * 2);
+                if (!row_not_finite(row)) continue;
+#pragma unroll
+                for (int x = 0; x < 16; ++x) add_not_finite(o[x >> 2], 4 * (x & 3), row, 8 * x + 4 * hh, tile * kKT + k <= sees_to);
+            }
+        }
+    }
+    float l = l_run + __shfl_xor(l_run, 32, 64), m = m_run;
+    float f = 1.0f;  // what this wave's sums are multiplied by
+    if (KP > 1) {
+        float* stat = (float*)(lds + L::kStat);
+        if (hh == 0) {
+            stat[wave * 32 + c] = m_run;
+            stat[32 * NW + wave * 32 + c] = l;
+        }
+        __syncthreads();
+        const int first = wave / KP * KP;
+        m = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < KP; ++x) m = fmaxf(m, stat[(first + x) * 32 + c]);
+        const float ref = m == -INFINITY ? 0.f : m;
+        l = 0.f;
+#pragma unroll
+        for (int x = 0; x < KP; ++x) l += stat[32 * NW + (first + x) * 32 + c] * __builtin_amdgcn_exp2f(stat[(first + x) * 32 + c] - ref);
+        f = __builtin_amdgcn_exp2f(m_run - ref);
+    }
+    const bool pieces = L::kSplits && w.pieces > 1;
+    if (!pieces) f *= l == 0.f ? 0.f : 1.0f / l;
+    const long long place = ((long long)(w.slot + w.piece) * e.n_kv_heads + kv_head) * kRows;
+    if (pieces && part == 0 && hh == 0 && r_wave + c < rows) store_coherent2(e.partial + (place + r_wave + c) * kPartRow + 128, m, l);
+    if (KP == 1) {  // rows as they are, through LDS to whole lines (a wave reads its own rows only)
+        unsigned char* to = lds + (r_wave + c) * 256;  // 16-byte pieces as in a K tile
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+            u32x2 y;
+            y[0] = pack_bf16x2(o[x >> 2][4 * (x & 3)] * f, o[x >> 2][4 * (x & 3) + 1] * f);
+            y[1] = pack_bf16x2(o[x >> 2][4 * (x & 3) + 2] * f, o[x >> 2][4 * (x & 3) + 3] * f);
+            *(u32x2*)(to + (x ^ (c & 15)) * 16 + 8 * hh) = y;
+        }
+        for (int r0 = 0; r0 < 32; r0 += 4) {
+            const int r = r_wave + r0 + lrow, row = w.tile * kRows + r;
+            if (r >= rows) break;
+            const int token = e.group.of(row);
+            *(u32x4*)(e.out + (long long)(w.begin + token) * e.out_row + (long long)((kv_head - token) * (int)e.group.d + row) * e.out_head + lp * 8) =
+                *(const u32x4*)(lds + r * 256 + (lp ^ (r & 15)) * 16);
+        }
+        return;
+    }
+    float* to = (float*)(lds + (part * kRows + r_wave + c) * L::kRowBytes);
+#pragma unroll
+    for (int x = 0; x < 16; ++x)
+        *(float4*)(to + 8 * x + 4 * hh) = make_float4(o[x >> 2][4 * (x & 3)] * f, o[x >> 2][4 * (x & 3) + 1] * f, o[x >> 2][4 * (x & 3) + 2] * f, o[x >> 2][4 * (x & 3) + 3] * f);
+    __syncthreads();
+    if (pieces) {
+        store_pieces<KP, NW>(lds, L::kRowBytes, kRows * L::kRowBytes, e.partial + place * kPartRow, rows);
+        join_pieces<kRows, NW>(w, kv_head, (int*)(lds + L::kFlag));
+        return;
+    }
+    for (int idx = tid; idx < rows * 16; idx += 64 * NW) {
+        const int r = idx >> 4, ch = idx & 15;
+        const char* from = (const char*)lds + r * L::kRowBytes + ch * 32;
+        float4 x = *(const float4*)from, y = *(const float4*)(from + 16);
+#pragma unroll
+        for (int k = 1; k < KP; ++k) {
+            const float4 x2 = *(const float4*)(from + k * kRows * L::kRowBytes), y2 = *(const float4*)(from + k * kRows * L::kRowBytes + 16);
+            x.x += x2.x; x.y += x2.y; x.z += x2.z; x.w += x2.w;
+            y.x += y2.x; y.y += y2.y; y.z += y2.z; y.w += y2.w;
+        }
+        const int row = w.tile * kRows + r, token = e.group.of(row);
+        u32x4 z;
+        z[0] = pack_bf16x2(x.x, x.y); z[1] = pack_bf16x2(x.z, x.w);
+        z[2] = pack_bf16x2(y.x, y.y); z[3] = pack_bf16x2(y.z, y.w);
+        *(u32x4*)(e.out + (long long)(w.begin + token) * e.out_row + (long long)((kv_head - token) * (int)e.group.d + row) * e.out_head + ch * 8) = z;
+    }
 }
 
 // Check mode.  One wave per (row, query head): 64 keys at a time, a lane has a key's score, then D / 64 columns of the output (rounded up).
@@ -678,13 +1074,18 @@ __global__ __launch_bounds__(64) void attention_f32(const jup_paged_pool_t pool,
 // ---- launches ------------------------------------------------------------------------------------------------------------------
 namespace {
 
-// Scratch: counters, then pieces.  A launch has at most kPieces + n_kv_heads pieces wanted (find_work), a divided tile at least two, each of
-// which is at least half as long as a piece may be: at most twice as many places are used, of 32 rows.
-constexpr int kPieces = 1024;  // two rounds of two workgroups per CU
-constexpr int kMostHeads = kPieces;  // (more heads than that fill the chip without dividing keys)
-constexpr size_t kPlaces = 2 * (kPieces + kMostHeads);
-constexpr size_t kCountBytes = kPlaces * 4;
-constexpr size_t kPartialBytes = kPlaces * 32 * kPartRow * 4;
+// Scratch: counters, then pieces.  Pieces wanted are P per chip, so at most P + n_kv_heads in all (find_work); a divided tile of
+// attention_few has at least two, each of which is at least half as long as a piece may be: at most twice as many places are
+// used.  attention_many counts a request's pieces as if all its tiles had the keys of the last one, at most twice what they
+// have on average: four times.
+constexpr int kFewRows = 32;       // a request's rows up to which attention_few has it
+constexpr int kFewPieces = 512;    // two workgroups per CU
+constexpr int kLeast16 = 24, kLeast32 = 16, kLeastMany = 24;  // key tiles that are worth a piece
+constexpr int kManyPieces = 222;   // a workgroup per CU, less what the longest may be longer than the average
+constexpr int kMostSplitHeads = 128;  // (more heads than that fill the chip without dividing keys)
+constexpr int kFewPlaces = 2 * (kFewPieces + kMostSplitHeads), kManyPlaces = 4 * (kManyPieces + kMostSplitHeads);
+constexpr size_t kCountBytes = ((size_t)(kFewPlaces > kManyPlaces ? kFewPlaces : kManyPlaces) * 4 + 255) / 256 * 256;
+constexpr size_t kPartialBytes = (size_t)(kFewPlaces * 32 > kManyPlaces * 64 ? kFewPlaces * 32 : kManyPlaces * 64) * kPartRow * 4;
 
 template <class K>
 hipError_t with_lds(K* kernel, int bytes, bool* done) {  // once per device: a kernel's limit of dynamic LDS
@@ -696,15 +1097,17 @@ hipError_t with_lds(K* kernel, int bytes, bool* done) {  // once per device: a k
     return e;
 }
 
-template <int QW>
-hipError_t launch_few(const Attention& a, int pieces, hipStream_t s) {
-    static bool done[64];
-    hipError_t e = with_lds(attention_few<QW>, few_lds(QW), done);
+// tiles: at most so many tiles of rows per key/value head
+template <class K>
+hipError_t launch(K* kernel, int threads, int lds, bool* done, Attention a, long long tiles, int pieces, int places, int least, hipStream_t s) {
+    hipError_t e = with_lds(kernel, lds, done);
     if (e != hipSuccess) return e;
-    const long long items = (long long)a.n_rows * a.group.d / QW + a.n_seqs + pieces;
-    const long long grid = items * a.n_kv_heads;
+    pieces = a.n_kv_heads > kMostSplitHeads || pieces == 0 ? 0 : (pieces + a.n_kv_heads - 1) / a.n_kv_heads;
+    a.chunk_factor = pieces > 0 ? 1.0001f / pieces : 1e30f;
+    a.most_places = places / a.n_kv_heads;
+    const long long grid = (tiles + 2 * pieces) * a.n_kv_heads;
     if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL(attention_few<QW>, dim3((unsigned)grid), dim3(64 * kFewWaves), few_lds(QW), s, a, 4);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), lds, s, a, least);
     return hipGetLastError();
 }
 
@@ -727,11 +1130,27 @@ hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_
     a.scale_log2e = c.scale * 1.4426950408889634f;
     a.count = (int*)c.workspace;
     a.partial = (float*)((char*)c.workspace + kCountBytes);
-    const int pieces = pool.n_kv_heads > kMostHeads ? 0 : (kPieces + pool.n_kv_heads - 1) / pool.n_kv_heads;
-    a.most_places = (int)(kPlaces / pool.n_kv_heads);
-    a.chunk_factor = pieces > 0 ? 1.0001f / pieces : 1e30f;
     a.least_rows = 0; a.most_rows = INT32_MAX;
-    return (long long)c.max_new * a.group.d <= 16 ? launch_few<16>(a, pieces, s) : launch_few<32>(a, pieces, s);
+    const long long rows = (long long)c.n_rows * a.group.d, most = (long long)c.max_new * a.group.d;
+    static bool done16[64], done32[64], done_many[64];
+    auto few = [&](Attention x, long long tiles16, long long tiles32) {
+        return most <= 16 ? launch(attention_few<16>, 64 * kFewWaves, few_lds(16), done16, x, tiles16, kFewPieces, kFewPlaces, kLeast16, s)
+                          : launch(attention_few<32>, 64 * kFewWaves, few_lds(32), done32, x, tiles32, kFewPieces, kFewPlaces, kLeast32, s);
+    };
+    if (most <= kFewRows) return few(a, rows / 16 + c.n_seqs, rows / 32 + c.n_seqs);
+    Attention longer = a;
+    // A few requests go to attention_many whatever their rows: a launch of attention_few for none of them costs as much as it saves.
+    const bool all = c.n_seqs <= 4;
+    longer.least_rows = all ? 0 : kFewRows + 1;
+    static bool done2[64], done4[64];
+        const long long groups = (rows / 256 + c.n_seqs) * pool.n_kv_heads;
+    hipError_t e = groups >= 384   ? launch(attention_many<8, 1, 2, 2, 2, 2>, 512, Many<8, 1, 2, 2, 2>::kLds, done_many, longer, rows / 256 + c.n_seqs, 0, 0, 8, s)
+                   : groups >= 112 ? launch(attention_many<8, 2, 2, 1, 2, 2>, 512, Many<8, 2, 2, 1, 2>::kLds, done2, longer, rows / 128 + c.n_seqs, 0, 0, 8, s)
+                                   : launch(attention_many<8, 4, 1, 1, 2, 2>, 512, Many<8, 4, 1, 1, 2>::kLds, done4, longer, rows / 64 + c.n_seqs, kManyPieces, kManyPlaces, kLeastMany, s);
+    if (e != hipSuccess || all) return e;
+    a.most_rows = kFewRows;
+    const long long tiles = (long long)c.n_seqs * (kFewRows / 32);
+    return few(a, 0, tiles < rows / 32 + c.n_seqs ? tiles : rows / 32 + c.n_seqs);
 }
 
 }  // namespace jup
