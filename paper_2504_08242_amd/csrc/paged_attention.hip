@@ -1084,8 +1084,8 @@ constexpr int kLeast16 = 24, kLeast32 = 16, kLeastMany = 24;  // key tiles that 
 constexpr int kManyPieces = 222;   // a workgroup per CU, less what the longest may be longer than the average
 constexpr int kMostSplitHeads = 128;  // (more heads than that fill the chip without dividing keys)
 constexpr int kFewPlaces = 2 * (kFewPieces + kMostSplitHeads), kManyPlaces = 4 * (kManyPieces + kMostSplitHeads);
-constexpr size_t kCountBytes = ((size_t)(kFewPlaces > kManyPlaces ? kFewPlaces : kManyPlaces) * 4 + 255) / 256 * 256;
 constexpr size_t kPartialBytes = (size_t)(kFewPlaces * 32 > kManyPlaces * 64 ? kFewPlaces * 32 : kManyPlaces * 64) * kPartRow * 4;
+static_assert(kFewPlaces * 4 <= kCountBytes && kManyPlaces * 4 <= kCountBytes);
 
 template <class K>
 hipError_t with_lds(K* kernel, int bytes, bool* done) {  // once per device: a kernel's limit of dynamic LDS
@@ -1155,4 +1155,6 @@ hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_
 
 }  // namespace jup
 
-extern "C" size_t jup_paged_workspace_bytes(void) { return jup::kCountBytes + jup::kPartialBytes; }
+extern "C" size_t jup_paged_workspace_bytes(void) {
+    return jup::kCountBytes + (jup::kPartialBytes > jup::kVerifyBytes ? jup::kPartialBytes : jup::kVerifyBytes);
+}

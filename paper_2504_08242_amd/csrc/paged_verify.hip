@@ -9,21 +9,44 @@
 namespace jup {
 namespace {
 
-constexpr int kVerifyThreads = 1024;
-constexpr int kVerifyWaves = kVerifyThreads / 64;
-
-__device__ __forceinline__ float prob(const float* p, long long i) { return p[i]; }
-__device__ __forceinline__ float prob(const u16* p, long long i) { return bf2f(p[i]); }
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr int kEach = 32;                        // probabilities of a thread at a time
+constexpr int kBlock = kThreads * kEach;         // and of a workgroup: the shortest slice
+constexpr int kMostSlices = kVerifySlices;
 
 // What the next token is drawn from: a row of the target's probabilities, less the draft's, or without one token.
 template <class T>
 struct Weights {
     const T *p, *q;
     int without;  // -1: nothing
-    __device__ __forceinline__ double at(int j) const {
-        double w = prob(p, j);
-        if (q) w -= (double)prob(q, j);
+    static __device__ __forceinline__ float value(float x) { return x; }
+    static __device__ __forceinline__ float value(u16 x) { return bf2f(x); }
+    __device__ __forceinline__ double weight(T pj, T qj, int j) const {
+        double w = value(pj);
+        if (q) w -= (double)value(qj);
         return j != without && w > 0.0 && w < INFINITY ? w : 0.0;
+    }
+    __device__ __forceinline__ bool aligned() const { return (((uintptr_t)p | (uintptr_t)q) & 15) == 0; }
+    // f(w_j, j) for N consecutive j from `first` on, those below `end`; vector: first is a multiple of N and the rows are aligned
+    template <int N, class F>
+    __device__ __forceinline__ void run(int first, int end, bool vector, F f) const {
+        if (vector && first + N <= end) {
+            constexpr int V = 16 / sizeof(T);
+            typedef T vec __attribute__((ext_vector_type(V)));
+            vec a[N / V], b[N / V];
+#pragma unroll
+            for (int k = 0; k < N / V; ++k) a[k] = *(const vec*)(p + first + k * V);
+            if (q) {
+#pragma unroll
+                for (int k = 0; k < N / V; ++k) b[k] = *(const vec*)(q + first + k * V);
+            }
+#pragma unroll
+            for (int k = 0; k < N; ++k) f(weight(a[k / V][k % V], q ? b[k / V][k % V] : T(0), first + k), first + k);
+        } else {
+            for (int k = 0; k < N; ++k)
+                if (first + k < end) f(weight(p[first + k], q ? q[first + k] : T(0), first + k), first + k);
+        }
     }
 };
 
@@ -33,108 +56,182 @@ __device__ __forceinline__ double wave_total(double v) {
     return v;
 }
 
-// The lowest j with w_0 + .. + w_j > u * sum(w) (the last j with w_j > 0 where rounding or u leaves none); -1 if all w are 0.
-// A wave owns a contiguous range, kRun columns at a time; its runs' sums say which one holds the border, and that one is
-// gone through again.
+struct Shared {
+    double sum[kMostSlices > kWaves ? kMostSlices : kWaves];
+    int top[kMostSlices > kWaves ? kMostSlices : kWaves];
+    int first_rejected, found, flag;
+};
+
+// Sum of w over [lo, hi) and the last j with w_j > 0, or -1; the same in all threads.
 template <class T>
-__device__ int draw(const Weights<T>& w, int vocab, float u, double* wave_sum_lds, int* found, int* last) {
+__device__ void add_up(const Weights<T>& w, int lo, int hi, Shared& s, double& sum, int& top) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int each = ((vocab + kVerifyWaves - 1) / kVerifyWaves + 63) / 64 * 64;
-    const int lo = min(wave * each, vocab), hi = min(lo + each, vocab);
-    double sum = 0.0;
-    int top = -1;
-    for (int j = lo + lane; j < hi; j += 64) {
-        const double x = w.at(j);
-        sum += x;
-        if (x > 0.0) top = j;
+    constexpr int V = 16 / sizeof(T);
+    const bool vector = w.aligned();
+    double mine = 0.0;
+    int last = -1;
+    for (int j0 = lo; j0 < hi; j0 += kBlock) {
+#pragma unroll
+        for (int k = 0; k < kEach / V; ++k)  // neighbouring threads have neighbouring pieces of 16 bytes
+            w.template run<V>(j0 + (k * kThreads + tid) * V, hi, vector, [&](double x, int j) {
+                mine += x;
+                if (x > 0.0) last = j;
+            });
     }
-    sum = wave_total(sum);
-    for (int by = 32; by > 0; by >>= 1) top = max(top, __shfl_xor(top, by, 64));
-    __syncthreads();
-    if (tid == 0) {
-        *found = INT32_MAX;
-        *last = -1;
-    }
+    mine = wave_total(mine);
+#pragma unroll
+    for (int by = 32; by > 0; by >>= 1) last = max(last, __shfl_xor(last, by, 64));
     __syncthreads();
     if (lane == 0) {
-        wave_sum_lds[wave] = sum;
-        atomicMax(last, top);
+        s.sum[wave] = mine;
+        s.top[wave] = last;
     }
     __syncthreads();
-    double all = 0.0, before = 0.0;
-    for (int i = 0; i < kVerifyWaves; ++i) {
-        if (i == wave) before = all;
-        all += wave_sum_lds[i];
+    sum = 0.0;
+    top = -1;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+        sum += s.sum[i];
+        top = max(top, s.top[i]);
     }
-    if (*last < 0) return -1;
-    const double border = u < 0.0f ? 0.0 : (double)u * all;
-    if (before <= border && before + sum > border) {
-        double run = before;
-        bool none = true;
-        for (int j0 = lo; j0 < hi; j0 += 64) {
-            const int j = j0 + lane;
-            double x = j < hi ? w.at(j) : 0.0;
-            const bool some = x > 0.0;
-            for (int by = 1; by < 64; by *= 2) {
-                const double left = __shfl_up(x, by, 64);
-                if (lane >= by) x += left;
-            }
-            const unsigned long long over = __ballot(some && run + x > border);
-            if (over) {
-                if (lane == 0) *found = j0 + __builtin_ctzll(over);
-                none = false;
-                break;
-            }
-            run += __shfl(x, 63, 64);
-        }
-        if (none && lane == 0) *found = top;  // (added up in this order the wave ends on the border)
-    }
-    __syncthreads();
-    return *found == INT32_MAX ? *last : *found;
 }
 
-// One workgroup per request.
+// The lowest j of [lo, hi) with before + w_lo + .. + w_j > border, or -1.  A thread has 32 neighbours.
 template <class T>
-__global__ __launch_bounds__(kVerifyThreads) void verify(const jup_verify_drafts_t a) {
-    __shared__ double sums[kVerifyWaves];
-    __shared__ int first_rejected, found, last;
-    const int i = blockIdx.x, tid = threadIdx.x;
+__device__ int search(const Weights<T>& w, int lo, int hi, double before, double border, Shared& s) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const bool vector = w.aligned();
+    for (int j0 = lo; j0 < hi; j0 += kBlock) {
+        double mine = 0.0;
+        w.template run<kEach>(j0 + tid * kEach, hi, vector, [&](double x, int) { mine += x; });
+        double upto = mine;
+#pragma unroll
+        for (int by = 1; by < 64; by *= 2) {
+            const double left = __shfl_up(upto, by, 64);
+            if (lane >= by) upto += left;
+        }
+        __syncthreads();
+        if (tid == 0) s.found = INT32_MAX;
+        if (lane == 63) s.sum[wave] = upto;
+        __syncthreads();
+        double run = before, all = before;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+            if (i == wave) run = all;
+            all += s.sum[i];
+        }
+        run += upto - mine;
+        if (mine > 0.0 && run + mine > border) {
+            // (threads behind the one that has the border get here too, and find something later)
+            int at = INT32_MAX;
+            w.template run<kEach>(j0 + tid * kEach, hi, vector, [&](double x, int j) {
+                run += x;
+                if (x > 0.0 && run > border) at = min(at, j);
+            });
+            if (at < INT32_MAX) atomicMin(&s.found, at);
+        }
+        __syncthreads();
+        if (s.found < INT32_MAX) return s.found;
+        before = all;
+    }
+    return -1;
+}
+
+// `slices` workgroups per request, each with `length` tokens of the vocabulary.  All of them find the row (a few loads); the one that
+// is done last knows where the border is and goes through its slice again.
+template <class T>
+__global__ __launch_bounds__(kThreads) void verify(const jup_verify_drafts_t a, int slices, int length, int* count, double* scratch) {
+    __shared__ Shared s;
+    const int i = blockIdx.x / slices, slice = blockIdx.x - i * slices, tid = threadIdx.x;
     const int begin = a.row_start[i], end = min(a.row_start[i + 1], a.n_rows);
     if (begin < 0 || begin >= end) {
-        if (tid == 0) {
+        if (tid == 0 && slice == 0) {
             a.n_accepted[i] = 0;
             a.next_token[i] = -1;
             if (a.new_lengths) a.new_lengths[i] = a.lengths[i];
         }
         return;
     }
-    if (tid == 0) first_rejected = end - 1;
+    if (tid == 0) s.first_rejected = end - 1;
     __syncthreads();
-    for (int row = begin + tid; row < end - 1; row += kVerifyThreads) {
+    for (int row = begin + tid; row < end - 1; row += kThreads) {
         const int x = a.tokens[row + 1];
         bool accepted = false;
         if (x >= 0 && x < a.vocab) {
-            const double p = prob((const T*)a.target_probs + row * a.target_row_stride, x);
-            const double q = a.draft_probs ? prob((const T*)a.draft_probs + row * a.draft_row_stride, x) : 1.0f;
+            const double p = Weights<T>::value(((const T*)a.target_probs)[row * a.target_row_stride + x]);
+            const double q = a.draft_probs ? Weights<T>::value(((const T*)a.draft_probs)[row * a.draft_row_stride + x]) : 1.0f;
             accepted = (double)a.u_accept[row] * q < p;
         }
-        if (!accepted) atomicMin(&first_rejected, row);
+        if (!accepted) atomicMin(&s.first_rejected, row);
     }
     __syncthreads();
-    const int row = first_rejected, n = row - begin;
+    const int row = s.first_rejected, n = row - begin;
     Weights<T> w{(const T*)a.target_probs + row * a.target_row_stride, nullptr, -1};
     if (row < end - 1) {
         if (a.draft_probs) w.q = (const T*)a.draft_probs + row * a.draft_row_stride;
         else w.without = a.tokens[row + 1];
     }
-    int next = draw(w, a.vocab, a.u_sample[i], sums, &found, &last);
-    if (next < 0 && row < end - 1) {
+    double sum;
+    int top;
+    add_up(w, min(slice * length, a.vocab), min((slice + 1) * length, a.vocab), s, sum, top);
+    if (slices > 1) {
+        double* mine = scratch + ((long long)i * slices + slice) * 2;
+        if (tid == 0) {
+            const unsigned long long bits = __builtin_bit_cast(unsigned long long, sum);
+            store_coherent2((float*)mine, __uint_as_float((unsigned)bits), __uint_as_float((unsigned)(bits >> 32)));
+            store_coherent2((float*)(mine + 1), __int_as_float(top), 0.f);
+            wait_stores_performed();
+            const int before = arrive_coherent(count + i);
+            s.flag = before == slices - 1;
+            if (before == slices - 1) count[i] = 0;  // ready for the next launch
+        }
+        __syncthreads();
+        if (!s.flag) return;
+        if (tid < slices) {
+            const float* from = (const float*)(scratch + ((long long)i * slices + tid) * 2);
+            const float2 x = load_coherent2(from), y = load_coherent2(from + 2);
+            s.sum[tid] = __builtin_bit_cast(double, (unsigned long long)__float_as_uint(x.x) | ((unsigned long long)__float_as_uint(x.y) << 32));
+            s.top[tid] = __float_as_int(y.x);
+        }
+        __syncthreads();
+    } else {
+        __syncthreads();
+        if (tid == 0) {
+            s.sum[0] = sum;
+            s.top[0] = top;
+        }
+        __syncthreads();
+    }
+    const float u = a.u_sample[i];
+    int next = -1, at = -1;  // at: the slice with the border
+    double all = 0.0, before = 0.0;
+    for (int k = 0; k < slices; ++k) {
+        all += s.sum[k];
+        next = max(next, s.top[k]);  // (where rounding or u leaves no token: the last one there is)
+    }
+    const double border = u < 0.0f ? 0.0 : (double)u * all;
+    double run = 0.0;
+    for (int k = 0; k < slices; ++k) {
+        if (at < 0 && run + s.sum[k] > border) {
+            at = k;
+            before = run;
+        }
+        run += s.sum[k];
+    }
+    if (next < 0 && row < end - 1) {  // a rejected row whose weights are all 0: the target itself (this workgroup alone)
         w.q = nullptr;
         w.without = -1;
-        next = draw(w, a.vocab, a.u_sample[i], sums, &found, &last);
+        add_up(w, 0, a.vocab, s, all, next);
+        const double again = u < 0.0f ? 0.0 : (double)u * all;
+        const int x = next < 0 ? -1 : search(w, 0, a.vocab, 0.0, again, s);
+        if (x >= 0) next = x;
+    } else if (at >= 0) {
+        const int last = s.top[at];
+        const int x = search(w, min(at * length, a.vocab), min((at + 1) * length, a.vocab), before, border, s);
+        next = x >= 0 ? x : last;  // (added up in this order the slice ends on the border)
     }
     if (a.emitted)
-        for (int r = begin + tid; r < end; r += kVerifyThreads) a.emitted[r] = r < row ? a.tokens[r + 1] : r == row ? next : -1;
+        for (int r = begin + tid; r < end; r += kThreads) a.emitted[r] = r < row ? a.tokens[r + 1] : r == row ? next : -1;
     if (tid == 0) {
         a.n_accepted[i] = n;
         a.next_token[i] = next;
@@ -145,8 +242,14 @@ __global__ __launch_bounds__(kVerifyThreads) void verify(const jup_verify_drafts
 }  // namespace
 
 hipError_t launch_verify_drafts(const jup_verify_drafts_t& a, hipStream_t s) {
-    if (a.probs_dtype == JUP_BF16) hipLaunchKernelGGL(verify<u16>, dim3(a.n_seqs), dim3(kVerifyThreads), 0, s, a);
-    else hipLaunchKernelGGL(verify<float>, dim3(a.n_seqs), dim3(kVerifyThreads), 0, s, a);
+    int length = kBlock;
+    if ((long long)length * kMostSlices < a.vocab) length = (int)(((long long)a.vocab + kMostSlices * kBlock - 1) / (kMostSlices * kBlock)) * kBlock;
+    const int slices = (a.vocab + length - 1) / length;
+    int* count = (int*)a.workspace;
+    double* scratch = (double*)((char*)a.workspace + kCountBytes);
+    const dim3 grid((unsigned)a.n_seqs * (unsigned)slices);
+    if (a.probs_dtype == JUP_BF16) hipLaunchKernelGGL(verify<u16>, grid, dim3(kThreads), 0, s, a, slices, length, count, scratch);
+    else hipLaunchKernelGGL(verify<float>, grid, dim3(kThreads), 0, s, a, slices, length, count, scratch);
     return hipGetLastError();
 }
 
