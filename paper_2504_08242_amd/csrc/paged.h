@@ -11,7 +11,7 @@ constexpr int kMaxPageSize = 65536;
 // A workspace: arrival counters, zero between launches, then what the workgroups of a launch leave for each other.
 constexpr size_t kCountBytes = (size_t)JUP_PAGED_MAX_SEQS * 4;
 constexpr int kVerifySlices = 64;  // of the vocabulary
-constexpr size_t kVerifyBytes = (size_t)JUP_PAGED_MAX_SEQS * kVerifySlices * 16;
+constexpr size_t kVerifyBytes = (size_t)JUP_PAGED_MAX_SEQS * kVerifySlices * 8;
 
 // page_size is a power of two
 inline int log2_of(int page_size) { return __builtin_ctz((unsigned)page_size); }

@@ -28,7 +28,7 @@ struct Weights {
         return j != without && w > 0.0 && w < INFINITY ? w : 0.0;
     }
     __device__ __forceinline__ bool aligned() const { return (((uintptr_t)p | (uintptr_t)q) & 15) == 0; }
-    // f(w_j, j) for N consecutive j from `first` on, those below `end`; vector: first is a multiple of N and the rows are aligned
+    // f(p_j, q_j, j) for N consecutive j from `first` on, those below `end`; vector: first is a multiple of N and the rows are aligned
     template <int N, class F>
     __device__ __forceinline__ void run(int first, int end, bool vector, F f) const {
         if (vector && first + N <= end) {
@@ -42,10 +42,10 @@ struct Weights {
                 for (int k = 0; k < N / V; ++k) b[k] = *(const vec*)(q + first + k * V);
             }
 #pragma unroll
-            for (int k = 0; k < N; ++k) f(weight(a[k / V][k % V], q ? b[k / V][k % V] : T(0), first + k), first + k);
+            for (int k = 0; k < N; ++k) f(a[k / V][k % V], q ? b[k / V][k % V] : T(0), first + k);
         } else {
             for (int k = 0; k < N; ++k)
-                if (first + k < end) f(weight(p[first + k], q ? q[first + k] : T(0), first + k), first + k);
+                if (first + k < end) f(p[first + k], q ? q[first + k] : T(0), first + k);
         }
     }
 };
@@ -58,42 +58,52 @@ __device__ __forceinline__ double wave_total(double v) {
 
 struct Shared {
     double sum[kMostSlices > kWaves ? kMostSlices : kWaves];
-    int top[kMostSlices > kWaves ? kMostSlices : kWaves];
     int first_rejected, found, flag;
 };
 
-// Sum of w over [lo, hi) and the last j with w_j > 0, or -1; the same in all threads.
+// Sum of w over [lo, hi), the same in all threads.  64-bit operations are what this costs (half the rate of 32-bit ones, five per
+// token): the maximum with 0 takes care of negative differences and of NaN; an infinity shows in the sum, which is then made again
+// with every weight looked at.
 template <class T>
-__device__ void add_up(const Weights<T>& w, int lo, int hi, Shared& s, double& sum, int& top) {
+__device__ double add_up(const Weights<T>& w, int lo, int hi, Shared& s) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     constexpr int V = 16 / sizeof(T);
     const bool vector = w.aligned();
-    double mine = 0.0;
+    double sum = 0.0;
+    for (int careful = 0; careful < 2; ++careful) {
+        double mine = 0.0;
+        for (int j0 = lo; j0 < hi; j0 += kBlock) {
+#pragma unroll
+            for (int k = 0; k < kEach / V; ++k)  // neighbouring threads have neighbouring pieces of 16 bytes
+                w.template run<V>(j0 + (k * kThreads + tid) * V, hi, vector, [&](T p, T q, int j) {
+                    mine += careful ? w.weight(p, q, j) : fmax((double)(j == w.without ? 0.0f : w.value(p)) - (double)w.value(q), 0.0);
+                });
+        }
+        mine = wave_total(mine);
+        __syncthreads();
+        if (lane == 0) s.sum[wave] = mine;
+        __syncthreads();
+        sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) sum += s.sum[i];
+        if (sum < INFINITY) break;
+    }
+    return sum;
+}
+
+// The last j with w_j > 0, or -1.
+template <class T>
+__device__ int last_weight(const Weights<T>& w, int vocab, Shared& s) {
+    const int tid = threadIdx.x;
     int last = -1;
-    for (int j0 = lo; j0 < hi; j0 += kBlock) {
-#pragma unroll
-        for (int k = 0; k < kEach / V; ++k)  // neighbouring threads have neighbouring pieces of 16 bytes
-            w.template run<V>(j0 + (k * kThreads + tid) * V, hi, vector, [&](double x, int j) {
-                mine += x;
-                if (x > 0.0) last = j;
-            });
-    }
-    mine = wave_total(mine);
-#pragma unroll
-    for (int by = 32; by > 0; by >>= 1) last = max(last, __shfl_xor(last, by, 64));
+    for (int j = tid; j < vocab; j += kThreads)
+        if (w.weight(w.p[j], w.q ? w.q[j] : T(0), j) > 0.0) last = j;
     __syncthreads();
-    if (lane == 0) {
-        s.sum[wave] = mine;
-        s.top[wave] = last;
-    }
+    if (tid == 0) s.found = -1;
     __syncthreads();
-    sum = 0.0;
-    top = -1;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-        sum += s.sum[i];
-        top = max(top, s.top[i]);
-    }
+    atomicMax(&s.found, last);
+    __syncthreads();
+    return s.found;
 }
 
 // The lowest j of [lo, hi) with before + w_lo + .. + w_j > border, or -1.  A thread has 32 neighbours.
@@ -103,7 +113,7 @@ __device__ int search(const Weights<T>& w, int lo, int hi, double before, double
     const bool vector = w.aligned();
     for (int j0 = lo; j0 < hi; j0 += kBlock) {
         double mine = 0.0;
-        w.template run<kEach>(j0 + tid * kEach, hi, vector, [&](double x, int) { mine += x; });
+        w.template run<kEach>(j0 + tid * kEach, hi, vector, [&](T p, T q, int j) { mine += w.weight(p, q, j); });
         double upto = mine;
 #pragma unroll
         for (int by = 1; by < 64; by *= 2) {
@@ -124,7 +134,8 @@ __device__ int search(const Weights<T>& w, int lo, int hi, double before, double
         if (mine > 0.0 && run + mine > border) {
             // (threads behind the one that has the border get here too, and find something later)
             int at = INT32_MAX;
-            w.template run<kEach>(j0 + tid * kEach, hi, vector, [&](double x, int j) {
+            w.template run<kEach>(j0 + tid * kEach, hi, vector, [&](T p, T q, int j) {
+                const double x = w.weight(p, q, j);
                 run += x;
                 if (x > 0.0 && run > border) at = min(at, j);
             });
@@ -171,15 +182,12 @@ __global__ __launch_bounds__(kThreads) void verify(const jup_verify_drafts_t a, 
         if (a.draft_probs) w.q = (const T*)a.draft_probs + row * a.draft_row_stride;
         else w.without = a.tokens[row + 1];
     }
-    double sum;
-    int top;
-    add_up(w, min(slice * length, a.vocab), min((slice + 1) * length, a.vocab), s, sum, top);
+    const double sum = add_up(w, min(slice * length, a.vocab), min((slice + 1) * length, a.vocab), s);
     if (slices > 1) {
-        double* mine = scratch + ((long long)i * slices + slice) * 2;
+        float* mine = (float*)(scratch + (long long)i * slices + slice);
         if (tid == 0) {
             const unsigned long long bits = __builtin_bit_cast(unsigned long long, sum);
-            store_coherent2((float*)mine, __uint_as_float((unsigned)bits), __uint_as_float((unsigned)(bits >> 32)));
-            store_coherent2((float*)(mine + 1), __int_as_float(top), 0.f);
+            store_coherent2(mine, __uint_as_float((unsigned)bits), __uint_as_float((unsigned)(bits >> 32)));
             wait_stores_performed();
             const int before = arrive_coherent(count + i);
             s.flag = before == slices - 1;
@@ -188,29 +196,20 @@ __global__ __launch_bounds__(kThreads) void verify(const jup_verify_drafts_t a, 
         __syncthreads();
         if (!s.flag) return;
         if (tid < slices) {
-            const float* from = (const float*)(scratch + ((long long)i * slices + tid) * 2);
-            const float2 x = load_coherent2(from), y = load_coherent2(from + 2);
+            const float2 x = load_coherent2((const float*)(scratch + (long long)i * slices + tid));
             s.sum[tid] = __builtin_bit_cast(double, (unsigned long long)__float_as_uint(x.x) | ((unsigned long long)__float_as_uint(x.y) << 32));
-            s.top[tid] = __float_as_int(y.x);
         }
         __syncthreads();
     } else {
         __syncthreads();
-        if (tid == 0) {
-            s.sum[0] = sum;
-            s.top[0] = top;
-        }
+        if (tid == 0) s.sum[0] = sum;
         __syncthreads();
     }
     const float u = a.u_sample[i];
     int next = -1, at = -1;  // at: the slice with the border
-    double all = 0.0, before = 0.0;
-    for (int k = 0; k < slices; ++k) {
-        all += s.sum[k];
-        next = max(next, s.top[k]);  // (where rounding or u leaves no token: the last one there is)
-    }
+    double all = 0.0, before = 0.0, run = 0.0;
+    for (int k = 0; k < slices; ++k) all += s.sum[k];
     const double border = u < 0.0f ? 0.0 : (double)u * all;
-    double run = 0.0;
     for (int k = 0; k < slices; ++k) {
         if (at < 0 && run + s.sum[k] > border) {
             at = k;
@@ -218,17 +217,16 @@ __global__ __launch_bounds__(kThreads) void verify(const jup_verify_drafts_t a, 
         }
         run += s.sum[k];
     }
-    if (next < 0 && row < end - 1) {  // a rejected row whose weights are all 0: the target itself (this workgroup alone)
-        w.q = nullptr;
-        w.without = -1;
-        add_up(w, 0, a.vocab, s, all, next);
-        const double again = u < 0.0f ? 0.0 : (double)u * all;
-        const int x = next < 0 ? -1 : search(w, 0, a.vocab, 0.0, again, s);
-        if (x >= 0) next = x;
-    } else if (at >= 0) {
-        const int last = s.top[at];
-        const int x = search(w, min(at * length, a.vocab), min((at + 1) * length, a.vocab), before, border, s);
-        next = x >= 0 ? x : last;  // (added up in this order the slice ends on the border)
+    if (at >= 0) next = search(w, min(at * length, a.vocab), min((at + 1) * length, a.vocab), before, border, s);
+    if (next < 0) {  // hardly ever, and this workgroup alone: u leaves no token (or rounding does), or there is none
+        next = last_weight(w, a.vocab, s);
+        if (next < 0 && row < end - 1) {  // a rejected row whose weights are all 0: the target itself
+            w.q = nullptr;
+            w.without = -1;
+            const double whole = add_up(w, 0, a.vocab, s);
+            next = search(w, 0, a.vocab, 0.0, u < 0.0f ? 0.0 : (double)u * whole, s);
+            if (next < 0) next = last_weight(w, a.vocab, s);
+        }
     }
     if (a.emitted)
         for (int r = begin + tid; r < end; r += kThreads) a.emitted[r] = r < row ? a.tokens[r + 1] : r == row ? next : -1;
