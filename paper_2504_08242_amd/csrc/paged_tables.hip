@@ -3,7 +3,8 @@
 // Tables.  Request i of n needs fresh_i = max(0, ceil((L_i + m_i) / P) - owned_i) pages; prefix sums over the requests of m and
 // of fresh give every request its rows and its place in the stack of free blocks.  One workgroup goes through the requests
 // 1024 at a time, twice: the sums alone (does the step fit?), then with the sums of the parts before it the writes.
-// Sums are in 64 bits: what the arrays hold is the caller's, and a sum that wraps would pass the checks.
+// Sums saturate: what the arrays hold is the caller's, and a sum that wraps would pass the checks.
+// Bound by latencies (loads, prefix sum, search, loads, stores): pages and rows are looked up four at a time.
 #include "paged.h"
 
 namespace jup {
@@ -12,11 +13,12 @@ namespace {
 constexpr int kPart = 1024;  // requests (and threads) of one part
 
 struct Pair {
-    long long rows, fresh;
+    unsigned rows, fresh;
 };
-__device__ __forceinline__ Pair operator+(Pair a, Pair b) { return {a.rows + b.rows, a.fresh + b.fresh}; }
+__device__ __forceinline__ unsigned sum(unsigned a, unsigned b) { return __builtin_elementwise_add_sat(a, b); }
+__device__ __forceinline__ Pair operator+(Pair a, Pair b) { return {sum(a.rows, b.rows), sum(a.fresh, b.fresh)}; }
 
-// Sums of the threads before this one, and of all; lds: one entry per wave and one for the whole.
+// Sums of the threads before this one, and of all; lds: one entry per wave.  (What is before a thread is of use where nothing is saturated.)
 __device__ Pair scan_part(Pair mine, Pair& all, Pair* lds) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Pair run = mine;
@@ -71,6 +73,20 @@ __device__ __forceinline__ int last_not_above(const int* at, int n, int x) {
     return lo;
 }
 
+// The same for four numbers at once, neighbours in the part by 1024, those below `end`; at[0] = 0.
+__device__ __forceinline__ void find4(const int* at, int n, int first, int end, int* found) {
+    int lo[4] = {0, 0, 0, 0}, size = n;
+    while (size > 1) {  // the same size for all: the last not above lies in [lo, lo + size)
+        const int half = size >> 1;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (at[lo[k] + half] <= min(first + k * kPart, end - 1)) lo[k] += half;
+        size -= half;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) found[k] = lo[k];
+}
+
 // Slot of a position in a request's table row; -1 where there is none (a block number that no pool has).
 __device__ __forceinline__ int slot_of(const int* table_row, int shift, int width, int position) {
     const int page = position >> shift;
@@ -89,18 +105,23 @@ __global__ __launch_bounds__(kPart) void extend_tables(const jup_paged_extend_t 
     const int tid = threadIdx.x;
     if (tid == 0) worst = 5;
     const int F = *a.free_count;
-    Pair total{0, 0};
+    Pair total{0, 0}, first_at{0, 0};
+    Request first{0, 0, 0, 0, 0};
     int why = 5;
     if (F < 0 || F > a.n_free) why = 1;
     for (int part = 0; part < a.n_seqs; part += kPart) {
         const Request r = request_of(a, shift, part + tid);
         if (r.why) why = min(why, r.why);
         Pair all;
-        scan_part({r.rows, r.fresh}, all, sums);
+        const Pair at = scan_part({(unsigned)max(r.rows, 0), (unsigned)r.fresh}, all, sums);
         total = total + all;
+        if (part == 0) {
+            first = r;
+            first_at = at;
+        }
     }
-    if (total.rows > a.max_rows) why = min(why, 3);
-    if (total.fresh > F) why = min(why, 4);
+    if (total.rows > (unsigned)a.max_rows) why = min(why, 3);
+    if (F >= 0 && total.fresh > (unsigned)F) why = min(why, 4);
     __syncthreads();
     if (why < 5) atomicMin(&worst, why);
     __syncthreads();
@@ -113,15 +134,16 @@ __global__ __launch_bounds__(kPart) void extend_tables(const jup_paged_extend_t 
     Pair done{0, 0};
     for (int part = 0; part < a.n_seqs; part += kPart) {
         const int i = part + tid, here = min(kPart, a.n_seqs - part);
-        Request r{0, 0, 0, 0, 0};
-        if (i < a.n_seqs && !fits) {  // nothing happens to it
-            r.length = a.lengths[i];
-            r.owned = a.owned[i];
-        } else {
-            r = request_of(a, shift, i);
+        Request r = first;
+        Pair all = total, at = first_at;
+        if (!fits) {  // nothing happens to any
+            if (part > 0) r = request_of(a, shift, i);
+            r.rows = r.fresh = 0;
+            all = at = {0, 0};
+        } else if (a.n_seqs > kPart) {
+            if (part > 0) r = request_of(a, shift, i);
+            at = scan_part({(unsigned)r.rows, (unsigned)r.fresh}, all, sums);
         }
-        Pair all;
-        const Pair at = scan_part({r.rows, r.fresh}, all, sums);
         if (i < a.n_seqs) {
             a.row_start[i] = (int)(done.rows + at.rows);
             a.new_lengths[i] = r.length + r.rows;
@@ -133,20 +155,33 @@ __global__ __launch_bounds__(kPart) void extend_tables(const jup_paged_extend_t 
         owned_at[tid] = r.owned;
         __syncthreads();
         // the part's pages, dealt to the threads one by one (a prompt needs hundreds where a decoding request needs none)
-        for (int p = tid; p < (int)all.fresh; p += kPart) {
-            const int q = last_not_above(fresh_at, here, p);
-            a.table[(long long)(part + q) * a.table_stride + owned_at[q] + p - fresh_at[q]] = a.free_blocks[F - 1 - (int)done.fresh - p];
+        for (int p = tid; p < (int)all.fresh; p += 4 * kPart) {
+            int q[4], block[4];
+            find4(fresh_at, here, p, (int)all.fresh, q);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (p + k * kPart < (int)all.fresh) block[k] = a.free_blocks[F - 1 - (int)done.fresh - p - k * kPart];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (p + k * kPart < (int)all.fresh)
+                    a.table[(long long)(part + q[k]) * a.table_stride + owned_at[q[k]] + p + k * kPart - fresh_at[q[k]]] = block[k];
         }
         if (ROWS) {
             __syncthreads();  // the entries are there
-            for (int row = tid; row < (int)all.rows; row += kPart) {
-                const int q = last_not_above(row_at, here, row);
-                const int position = length_at[q] + row - row_at[q];
-                const int to = (int)done.rows + row;
-                a.positions[to] = position;
-                a.slots[to] = slot_of(a.table + (long long)(part + q) * a.table_stride, shift, a.table_width, position);
+            for (int row = tid; row < (int)all.rows; row += 4 * kPart) {
+                int q[4];
+                find4(row_at, here, row, (int)all.rows, q);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (row + k * kPart >= (int)all.rows) continue;
+                    const int position = length_at[q[k]] + row + k * kPart - row_at[q[k]];
+                    const int to = (int)done.rows + row + k * kPart;
+                    a.positions[to] = position;
+                    a.slots[to] = slot_of(a.table + (long long)(part + q[k]) * a.table_stride, shift, a.table_width, position);
+                }
             }
         }
+        __syncthreads();  // (the part's arrays are free again)
         done = done + all;
     }
     if (ROWS) {
@@ -157,18 +192,39 @@ __global__ __launch_bounds__(kPart) void extend_tables(const jup_paged_extend_t 
     }
 }
 
-// Positions and slots of steps with many rows, from what extend_tables left.
+// Positions and slots of steps with many rows, from what extend_tables left.  A wave has 64 neighbouring rows: it finds the request of the
+// first of them 64 probes at a time, and the others' among the 64 requests from there on.
 __global__ __launch_bounds__(256) void extend_rows(const jup_paged_extend_t a, int shift) {
-    const int row = blockIdx.x * 256 + threadIdx.x;
-    if (row >= a.max_rows) return;
+    const int lane = threadIdx.x & 63, row = blockIdx.x * 256 + threadIdx.x;
+    const int total = a.n_seqs > 0 ? a.row_start[a.n_seqs] : 0;
+    const int row0 = row - lane;
     int position = 0, slot = -1;
-    if (a.n_seqs > 0 && row < a.row_start[a.n_seqs]) {
-        const int i = last_not_above(a.row_start, a.n_seqs, row);
-        position = a.new_lengths[i] - (a.row_start[i + 1] - row);
-        slot = slot_of(a.table + (long long)i * a.table_stride, shift, a.table_width, position);
+    if (row0 < total) {
+        int first = 0, size = a.n_seqs;
+        while (size > 1) {
+            const int step = (size + 63) / 64, at = first + lane * step;
+            const bool below = lane * step < size && a.row_start[min(at, a.n_seqs)] <= row0;
+            const int n = __popcll(__ballot(below));  // (row_start does not fall: the lanes below are the first n, and n > 0)
+            first += (n - 1) * step;
+            size = min(step, size - (n - 1) * step);
+        }
+        const int mine = min(first + lane, a.n_seqs);
+        const int start = a.row_start[mine];
+        int lo = 0;  // the last of the 64 that begins at or before the row
+#pragma unroll
+        for (int half = 32; half > 0; half >>= 1)
+            if (__shfl(start, lo + half, 64) <= row) lo += half;
+        int i = min(first + lo, a.n_seqs - 1);
+        if (row < total) {
+            if (lo == 63) i = first + 63 + last_not_above(a.row_start + first + 63, a.n_seqs - first - 63, row);  // (idle requests lie between)
+            position = a.new_lengths[i] - (a.row_start[i + 1] - row);
+            slot = slot_of(a.table + (long long)i * a.table_stride, shift, a.table_width, position);
+        }
     }
-    a.positions[row] = position;
-    a.slots[row] = slot;
+    if (row < a.max_rows) {
+        a.positions[row] = position;
+        a.slots[row] = slot;
+    }
 }
 
 // ---- rows into their slots -----------------------------------------------------------------------------------------------
