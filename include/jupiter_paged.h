@@ -9,8 +9,9 @@
  * Jupiter paper Sec. V-B) that share a prefix name the same pages.  A speculative step (Sec. V-A) is
  *
  *     jup_paged_extend     lengths -> pages, positions, slots                       (once per step)
- *     jup_paged_append     rotary embedding, keys and values into their slots       (every layer)
- *     jup_paged_attention  the new tokens over the pages                            (every layer)
+ *     jup_paged_append     rotary embedding, keys and values into their slots       (every layer; or, for a stage of
+ *     jup_paged_attention  the new tokens over the pages                             this library, all of its layers:
+ *                                                                                    jup_stage_prefill_paged)
  *     jup_verify_drafts    drafted tokens against the target's probabilities, the requests' new lengths (once per step)
  *
  * Lengths, tables and tokens stay on the GPU: the host waits for nothing, and a captured step can be replayed.
@@ -127,6 +128,30 @@ JUP_API jup_status_t jup_paged_attention(const jup_paged_pool_t *pool, const jup
 
 /* Bytes of a workspace that serves every call of jup_paged_attention() and jup_verify_drafts(). */
 JUP_API size_t jup_paged_workspace_bytes(void);
+
+/*
+ * The forward of a stage (steps 1-6 of jupiter_stage.h) over the rows of a ragged batch, with a pool in place of the caches: what
+ * jup_stage_prefill_chunk() computes for every request's new tokens on its own cache, the weights read once for all of
+ * them.  Enqueues what jup_paged_append() and jup_paged_attention() do in every layer.
+ *   hidden_in, hidden_out   [n_rows, d_model], stage dtype; hidden_out may be hidden_in.  n_rows <= the stage's max_chunk_tokens.
+ *                   Rows behind the last request's may be there (a captured step of fixed size): hidden_out is then unspecified in them
+ *   pool            of the stage's first layer: n_kv_heads = n_heads, head_dim as the stage's; JUP_BF16 for the bf16 and 4-bit stages.
+ *                   A layer's k and v lie layer_stride elements behind the one's before it
+ *   others          as in jup_paged_extend() and jup_paged_attention()
+ * Results are those of the calls on caches up to the summation order of fp32 sums and the rounding of probabilities to bf16.
+ * Errors: JUP_EINVAL, JUP_ECAP, JUP_EDEVICE.
+ */
+typedef struct {
+    jup_paged_pool_t pool;
+    int64_t layer_stride;
+    int32_t n_seqs, max_new, table_width;
+    int64_t table_stride;
+    const int32_t *row_start, *lengths, *table, *positions, *slots;
+    void *workspace;
+    size_t workspace_bytes;
+} jup_paged_batch_t;
+JUP_API jup_status_t jup_stage_prefill_paged(jup_stage_t *stage, const void *hidden_in, int32_t n_rows, const jup_paged_batch_t *batch,
+                                             void *hidden_out, void *stream);
 
 /*
  * Verification of drafted tokens (Sec. V-A step 4).  Row r of request i holds an input token of the step: the last one

@@ -405,6 +405,7 @@ struct BeginArgs {
 void launch_begin_chunk(const BeginArgs& a, int pos0, hipStream_t s);
 void launch_begin_tree(const BeginArgs& a, int pos0, const TreeTable& t, TreeTable* dst, hipStream_t s);
 void launch_begin_branches(const BeginArgs& a, const BranchTable& t, BranchTable* dst, hipStream_t s);
+void launch_begin_paged(const BeginArgs& a, const int* positions, hipStream_t s);  // positions of the rows, on the GPU
 // v = (hidden_in, or x32 if null) + sum_s partial[s];  x32 <- v, or with out: out <- bf16(v), row-major;  if g: xn <- rmsnorm(v) * g
 // (tiled layout), or with factor xn <- v * g and factor <- 1 / rms of the rows
 void launch_reduce_norm(float* x32, const u16* hidden_in, const float* partial, int splits, size_t split_stride, const u16* g,

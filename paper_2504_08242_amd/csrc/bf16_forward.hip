@@ -11,6 +11,7 @@
 // The projections back to d_model are too narrow to fill 256 CUs with tall tiles, so they split K and
 // write fp32 partial tiles; the next reduce+norm pass adds them to the fp32 residual stream in a fixed
 // order (bitwise reproducible) on its way to the normalised bf16 rows it has to produce anyway.
+#include "paged.h"
 #include "w4_plan.h"
 
 namespace jup {
@@ -77,9 +78,12 @@ hipError_t w4_pack_weights(const jup_stage& st, const jup_layer_weights_t* layer
 // link != nullptr: scratch buffer and cross-stream events of a chunk that overlaps with its neighbours.
 // tree != nullptr (host table, bt == nullptr): the n tokens are a token tree; only the rotary positions
 // (pos + depth) and the mask inside the chunk differ from an ordinary chunk.
+// paged != nullptr (bt, tree and link null, pos and kv unused): the n rows are a ragged batch over pages of a pool.  The QKV
+// projection leaves their rotated keys and their values in the workspace (where the K-split partial sums go later in the layer), and one
+// more launch per layer takes them to their slots.
 hipError_t bf16_forward(const jup_stage& st, const void* hidden_in, int n, int pos, const KvView& kv,
                         void* hidden_out, hipStream_t s, const BranchTable* bt, const TreeTable* tree,
-                        const ChunkLink* link) {
+                        const ChunkLink* link, const PagedStep* paged) {
     const jup_stage_config_t& c = st.cfg;
     const int d = c.d_model, f = c.d_ffn, H = c.n_heads;
     char* ws = (char*)(link && link->workspace ? link->workspace : st.workspace);
@@ -122,9 +126,18 @@ hipError_t bf16_forward(const jup_stage& st, const void* hidden_in, int n, int p
         } else if (tree) {
             tree_dev = (const TreeTable*)(ws + st.wl.tree);
             launch_begin_tree(a, pos, *tree, (TreeTable*)(ws + st.wl.tree), s);
+        } else if (paged) {
+            launch_begin_paged(a, paged->positions, s);
+            keys = 0;  // (known on the GPU alone)
         } else {
             launch_begin_chunk(a, pos, s);
         }
+    }
+    // a cache of this call's rows: [K|V][head][row][128], behind the sums of squares that lie at the beginning of the partial sums
+    KvView rows_kv{};
+    if (paged) {
+        rows_kv.own = partial + (size_t)4 * ((st.max_chunk_tokens + 31) / 32 * 32) * d;
+        rows_kv.own_cap = n;
     }
 
     // 4-bit stage: the projections read codes, everything else is the bf16 path.  With the expanded copy at hand,
@@ -176,7 +189,7 @@ hipError_t bf16_forward(const jup_stage& st, const void* hidden_in, int n, int p
             TraceScope ts(st, JUP_K_GEMM_QKV, s);
             GemmArgs a{};
             a.A = xn; a.W = (const u16*)(wb + wqkv); a.M = n; a.N = 3 * d; a.K = d; a.n_tok = n_tok;
-            a.q_out = q; a.rope = rope; a.kv = kv; a.layer = l; a.n_heads = H; a.d_model = d; a.pos0 = pos;
+            a.q_out = q; a.rope = rope; a.kv = paged ? rows_kv : kv; a.layer = paged ? 0 : l; a.n_heads = H; a.d_model = d; a.pos0 = paged ? 0 : pos;
             a.branches = bt_dev;
             a.shared_gpu = shared;
             a.ssq = rows && l > 0 ? ssq : nullptr; a.rms_eps = c.rms_eps;
@@ -191,7 +204,18 @@ hipError_t bf16_forward(const jup_stage& st, const void* hidden_in, int n, int p
         {
             TraceScope ts(st, JUP_K_ATTENTION, s);
             if (e != hipSuccess) break;
-            if (bt) e = launch_branch_attention(q, o, bt->n_tok, bt->n_branches, d, H, bt_dev, max_keys, l, s, att, from_memory);
+            if (paged) {
+                const jup_paged_pool_t pool = paged->layer(l);
+                jup_paged_append_t rows_of{};
+                rows_of.n_rows = n; rows_of.slots = paged->slots;
+                rows_of.k = rows_kv.own; rows_of.v = (const u16*)rows_kv.own + (size_t)n * d;
+                rows_of.k_row_stride = rows_of.v_row_stride = 128;
+                rows_of.k_head_stride = rows_of.v_head_stride = (int64_t)n * 128;
+                e = launch_paged_append(pool, rows_of, s);
+                jup_paged_attention_t call = paged->attention;
+                call.q = q; call.out = o; call.q_row_stride = d; call.q_head_stride = 128;
+                if (e == hipSuccess) e = launch_paged_attention(pool, call, s, d >> 5);
+            } else if (bt) e = launch_branch_attention(q, o, bt->n_tok, bt->n_branches, d, H, bt_dev, max_keys, l, s, att, from_memory);
             else e = launch_chunk_attention(q, o, n, d, H, pos, kv, l, s, att, from_memory, tree_dev, shared);
         }
         {

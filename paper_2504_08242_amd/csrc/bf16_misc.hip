@@ -195,6 +195,12 @@ struct BranchRows {
     __device__ void park() const { *dst = t; }
 };
 
+struct PagedRows {
+    const int* positions;
+    __device__ int position(int row) const { return positions[row]; }
+    __device__ void park() const {}
+};
+
 // Everything a call needs before its first projection, in one launch: blocks 0 .. n - 1 norm a row of hidden_in each; the
 // blocks behind them write the rotary table, tab[row][i] = (cos, sin)(position * theta^(-2i/128)) with the angles in fp64 so
 // that large positions stay exact, clear the arrival counters the call's later kernels count in (a fill by a kernel, not a
@@ -269,6 +275,7 @@ void launch_begin_tree(const BeginArgs& a, int pos0, const TreeTable& t, TreeTab
 void launch_begin_branches(const BeginArgs& a, const BranchTable& t, BranchTable* dst, hipStream_t s) {
     launch_begin(a, BranchRows{t, dst}, s);
 }
+void launch_begin_paged(const BeginArgs& a, const int* positions, hipStream_t s) { launch_begin(a, PagedRows{positions}, s); }
 void launch_reduce_norm(float* x32, const u16* hidden_in, const float* partial, int splits, size_t split_stride, const u16* g, u16* xn,
                         float* factor, u16* out, int n, int d, float eps, hipStream_t s) {
     const bool wide = d % 512 == 0 && d / 8 <= 1024;

@@ -168,9 +168,11 @@ struct TraceScope {
 // Records the message jup_last_error() returns on this thread and hands the status code back (jup_api.hip).
 jup_status_t set_error(jup_status_t code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 
+struct PagedStep;  // paged.h: a call over pages of a pool in place of a cache
+
 // ---- check-mode (fp32) path: kernels_f32.hip ------------------------------------------------------
 hipError_t f32_forward(const jup_stage& st, const float* hidden_in, int n, int pos, const KvView& kv,
-                       float* hidden_out, hipStream_t s, const TreeTable* tree = nullptr);
+                       float* hidden_out, hipStream_t s, const TreeTable* tree = nullptr, const PagedStep* paged = nullptr);
 
 // ---- matrix-core (bf16) path: bf16_forward.hip (and bf16_gemm / bf16_attention / bf16_misc) ----------------------------------------------------
 hipError_t bf16_pack_weights(const jup_stage& st, const jup_layer_weights_t* layers, hipStream_t s);
@@ -186,7 +188,7 @@ struct ChunkLink {
 };
 hipError_t bf16_forward(const jup_stage& st, const void* hidden_in, int n, int pos, const KvView& kv,
                         void* hidden_out, hipStream_t s, const BranchTable* branches = nullptr,
-                        const TreeTable* tree = nullptr, const ChunkLink* link = nullptr);
+                        const TreeTable* tree = nullptr, const ChunkLink* link = nullptr, const PagedStep* paged = nullptr);
 
 // ---- cache and table helpers: kv_ops.hip --------------------------------------------------------------
 // The tables of a call travel as kernel arguments and are parked in the workspace, where the kernels of the

@@ -3,7 +3,7 @@
 // strides, mask boundary) against the CPU oracle at tight tolerances; speed is not a goal.
 // Steps follow the decoder layer of Sec. II-A of the Jupiter paper in its Llama-2 form, applied to
 // one sub-sequence with the cached prefix (Sec. IV-A.2).
-#include "jup_internal.h"
+#include "paged.h"
 
 namespace jup {
 namespace {
@@ -177,7 +177,7 @@ void gemm(const float* A, int lda, const float* W, float* C, const float* R, int
 }  // namespace
 
 hipError_t f32_forward(const jup_stage& st, const float* hidden_in, int n, int pos, const KvView& kv,
-                       float* hidden_out, hipStream_t s, const TreeTable* tree) {
+                       float* hidden_out, hipStream_t s, const TreeTable* tree, const PagedStep* paged) {
     const jup_stage_config_t& c = st.cfg;
     const int d = c.d_model, f = c.d_ffn, H = c.n_heads, dh = c.head_dim;
     char* ws = (char*)st.workspace;
@@ -206,12 +206,24 @@ hipError_t f32_forward(const jup_stage& st, const float* hidden_in, int n, int p
 
         hipLaunchKernelGGL(f32_rmsnorm, dim3(n), dim3(256), 0, s, x, g1, xn, d, c.rms_eps);
         gemm(xn, d, wqkv, qkv, nullptr, 3 * d, n, 3 * d, d, s);
-        {
+        if (paged) {
+            const jup_paged_pool_t pool = paged->layer(l);
+            jup_paged_append_t rows{};
+            rows.n_rows = n; rows.n_heads = H; rows.q = rows.q_out = qkv; rows.k = qkv + d; rows.v = qkv + 2 * d;
+            rows.q_row_stride = rows.k_row_stride = rows.v_row_stride = rows.q_out_row_stride = 3 * d;
+            rows.q_head_stride = rows.k_head_stride = rows.v_head_stride = rows.q_out_head_stride = dh;
+            rows.positions = paged->positions; rows.slots = paged->slots; rows.rope_theta = c.rope_theta;
+            e = launch_paged_append(pool, rows, s);
+            jup_paged_attention_t call = paged->attention;
+            call.q = qkv; call.out = o; call.q_row_stride = 3 * d; call.out_row_stride = d; call.q_head_stride = call.out_head_stride = dh;
+            if (e == hipSuccess) e = launch_paged_attention(pool, call, s);
+            if (e != hipSuccess) return e;
+        } else {
             const long long work = (long long)n * H * (dh / 2);
             hipLaunchKernelGGL(f32_rope_append, dim3((unsigned)((work + 255) / 256)), dim3(256), 0, s, qkv, n, d, H, dh,
                                pos, c.rope_theta, kv, l, tree_dev);
+            hipLaunchKernelGGL(f32_attention, dim3(n, H), dim3(kWave), 0, s, qkv, o, d, H, dh, pos, kv, l, tree_dev);
         }
-        hipLaunchKernelGGL(f32_attention, dim3(n, H), dim3(kWave), 0, s, qkv, o, d, H, dh, pos, kv, l, tree_dev);
         gemm(o, d, wo, x, x, d, n, d, d, s);  // x <- x + o Wo^T (each element read and written by one thread)
         hipLaunchKernelGGL(f32_rmsnorm, dim3(n), dim3(256), 0, s, x, g2, xn, d, c.rms_eps);
         gemm(xn, d, wgu, gu, nullptr, 2 * f, n, 2 * f, d, s);

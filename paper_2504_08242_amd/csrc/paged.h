@@ -21,9 +21,27 @@ hipError_t launch_paged_extend(const jup_paged_extend_t& a, hipStream_t s);
 hipError_t launch_paged_append(const jup_paged_pool_t& pool, const jup_paged_append_t& a, hipStream_t s);
 
 // ---- attention (paged_attention.hip) --------------------------------------------------------------------------------
-hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_attention_t& a, hipStream_t s);
+// tiled (JUP_BF16 only): 0, or out is [n_rows, n_heads * 128] in the layout of a projection's operand (tiled_offset), this many stages
+hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_attention_t& a, hipStream_t s, int tiled = 0);
 
 // ---- verification (paged_verify.hip) --------------------------------------------------------------------------------
 hipError_t launch_verify_drafts(const jup_verify_drafts_t& a, hipStream_t s);
+
+// ---- a stage over pages (bf16_forward.hip, kernels_f32.hip) -----------------------------------------------------------
+// What a forward over a ragged batch needs in place of a cache.  attention: the call of one layer, but for q, out and their
+// strides.
+struct PagedStep {
+    jup_paged_pool_t pool;   // the first layer's
+    int64_t layer_stride;    // elements
+    const int32_t *positions, *slots;
+    jup_paged_attention_t attention;
+    jup_paged_pool_t layer(int l) const {
+        jup_paged_pool_t p = pool;
+        const size_t at = (size_t)l * layer_stride * (pool.dtype == JUP_F32 ? 4 : 2);
+        p.k = (char*)pool.k + at;
+        p.v = (char*)pool.v + at;
+        return p;
+    }
+};
 
 }  // namespace jup

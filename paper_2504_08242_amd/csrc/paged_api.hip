@@ -43,6 +43,29 @@ const char* check_workspace(const void* p, size_t bytes) {
     return "";
 }
 
+jup_status_t check_attention(const char* me, const jup_paged_pool_t* pool, const jup_paged_attention_t* a) {
+    const char* why = check_pool(pool);
+    if (*why) return set_error(JUP_EINVAL, "%s: %s", me, why);
+    if (!a) return set_error(JUP_EINVAL, "%s: args is NULL", me);
+    if (a->n_seqs < 0 || a->n_seqs > JUP_PAGED_MAX_SEQS)
+        return set_error(JUP_EINVAL, "%s: n_seqs=%d is outside 0..%d", me, a->n_seqs, JUP_PAGED_MAX_SEQS);
+    if (a->n_rows < 0 || a->max_new < 0) return set_error(JUP_EINVAL, "%s: n_rows and max_new must not be negative", me);
+    if (a->n_heads <= 0 || a->n_heads % pool->n_kv_heads)
+        return set_error(JUP_EINVAL, "%s: n_heads=%d must be a positive multiple of n_kv_heads=%d", me, a->n_heads, pool->n_kv_heads);
+    if ((int64_t)a->n_rows * a->n_heads > INT32_MAX) return set_error(JUP_EINVAL, "%s: n_rows * n_heads exceeds 2^31 - 1", me);
+    if (a->table_width < 0 || (int64_t)a->table_width * pool->page_size > INT32_MAX)
+        return set_error(JUP_EINVAL, "%s: table_width=%d is negative, or table_width * page_size exceeds 2^31 - 1", me, a->table_width);
+    if (a->table_stride < a->table_width) return set_error(JUP_EINVAL, "%s: table_stride is shorter than table_width", me);
+    if (!(a->scale > 0.0f) || a->scale > 3e38f) return set_error(JUP_EINVAL, "%s: scale must be positive and finite", me);
+    if (a->n_rows == 0 || a->n_seqs == 0) return JUP_OK;
+    if (!a->q || !a->out || !a->row_start || !a->lengths || (a->table_width > 0 && !a->table))
+        return set_error(JUP_EINVAL, "%s: the rows, row_start, lengths and table must not be NULL", me);
+    if (bad_rows(pool->dtype, a->q, a->q_row_stride, a->q_head_stride) || bad_rows(pool->dtype, a->out, a->out_row_stride, a->out_head_stride))
+        return set_error(JUP_EINVAL, "%s: strides must not be negative; JUP_BF16: tensors 16-byte aligned, strides multiples of 8", me);
+    if (pool->dtype == JUP_BF16 && *(why = check_workspace(a->workspace, a->workspace_bytes))) return set_error(JUP_EINVAL, "%s: %s", me, why);
+    return JUP_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -88,26 +111,43 @@ jup_status_t jup_paged_append(const jup_paged_pool_t* pool, const jup_paged_appe
 
 jup_status_t jup_paged_attention(const jup_paged_pool_t* pool, const jup_paged_attention_t* a, void* stream) {
     const char* me = "jup_paged_attention";
-    const char* why = check_pool(pool);
-    if (*why) return set_error(JUP_EINVAL, "%s: %s", me, why);
-    if (!a) return set_error(JUP_EINVAL, "%s: args is NULL", me);
-    if (a->n_seqs < 0 || a->n_seqs > JUP_PAGED_MAX_SEQS)
-        return set_error(JUP_EINVAL, "%s: n_seqs=%d is outside 0..%d", me, a->n_seqs, JUP_PAGED_MAX_SEQS);
-    if (a->n_rows < 0 || a->max_new < 0) return set_error(JUP_EINVAL, "%s: n_rows and max_new must not be negative", me);
-    if (a->n_heads <= 0 || a->n_heads % pool->n_kv_heads)
-        return set_error(JUP_EINVAL, "%s: n_heads=%d must be a positive multiple of n_kv_heads=%d", me, a->n_heads, pool->n_kv_heads);
-    if ((int64_t)a->n_rows * a->n_heads > INT32_MAX) return set_error(JUP_EINVAL, "%s: n_rows * n_heads exceeds 2^31 - 1", me);
-    if (a->table_width < 0 || (int64_t)a->table_width * pool->page_size > INT32_MAX)
-        return set_error(JUP_EINVAL, "%s: table_width=%d is negative, or table_width * page_size exceeds 2^31 - 1", me, a->table_width);
-    if (a->table_stride < a->table_width) return set_error(JUP_EINVAL, "%s: table_stride is shorter than table_width", me);
-    if (!(a->scale > 0.0f) || a->scale > 3e38f) return set_error(JUP_EINVAL, "%s: scale must be positive and finite", me);
-    if (a->n_rows == 0 || a->n_seqs == 0) return JUP_OK;
-    if (!a->q || !a->out || !a->row_start || !a->lengths || (a->table_width > 0 && !a->table))
-        return set_error(JUP_EINVAL, "%s: q, out, row_start, lengths and table must not be NULL", me);
-    if (bad_rows(pool->dtype, a->q, a->q_row_stride, a->q_head_stride) || bad_rows(pool->dtype, a->out, a->out_row_stride, a->out_head_stride))
-        return set_error(JUP_EINVAL, "%s: strides must not be negative; JUP_BF16: tensors 16-byte aligned, strides multiples of 8", me);
-    if (pool->dtype == JUP_BF16 && *(why = check_workspace(a->workspace, a->workspace_bytes))) return set_error(JUP_EINVAL, "%s: %s", me, why);
+    const jup_status_t rc = check_attention(me, pool, a);
+    if (rc != JUP_OK || a->n_rows == 0 || a->n_seqs == 0) return rc;
     return launched(me, jup::launch_paged_attention(*pool, *a, (hipStream_t)stream));
+}
+
+jup_status_t jup_stage_prefill_paged(jup_stage_t* stage, const void* hidden_in, int32_t n_rows, const jup_paged_batch_t* b,
+                                     void* hidden_out, void* stream) {
+    const char* me = "jup_stage_prefill_paged";
+    if (!stage) return set_error(JUP_EINVAL, "%s: stage is NULL", me);
+    if (!b) return set_error(JUP_EINVAL, "%s: batch is NULL", me);
+    const jup_stage_config_t& c = stage->cfg;
+    if (n_rows < 0) return set_error(JUP_EINVAL, "%s: n_rows=%d is negative", me, n_rows);
+    if (n_rows > stage->max_chunk_tokens)
+        return set_error(JUP_ECAP, "%s: n_rows=%d exceeds the stage's max_chunk_tokens=%d", me, n_rows, stage->max_chunk_tokens);
+    jup::PagedStep step{};
+    step.pool = b->pool;
+    step.layer_stride = b->layer_stride;
+    step.positions = b->positions;
+    step.slots = b->slots;
+    jup_paged_attention_t& a = step.attention;
+    a.n_seqs = b->n_seqs; a.n_rows = n_rows; a.n_heads = c.n_heads; a.max_new = b->max_new; a.table_width = b->table_width;
+    a.table_stride = b->table_stride; a.row_start = b->row_start; a.lengths = b->lengths; a.table = b->table;
+    a.scale = 1.0f / sqrtf((float)c.head_dim); a.workspace = b->workspace; a.workspace_bytes = b->workspace_bytes;
+    a.q = hidden_in; a.out = hidden_out;  // (stand for the stage's own: given or not, aligned or not)
+    const jup_status_t rc = check_attention(me, &b->pool, &a);
+    if (rc != JUP_OK) return rc;
+    if (b->pool.n_kv_heads != c.n_heads || b->pool.head_dim != c.head_dim || (b->pool.dtype == JUP_F32) != (c.dtype == JUP_F32))
+        return set_error(JUP_EINVAL, "%s: the pool was made for another configuration", me);
+    if (b->layer_stride < 0 || (c.dtype != JUP_F32 && (b->layer_stride & 7)))
+        return set_error(JUP_EINVAL, "%s: layer_stride must not be negative, and a multiple of 8 in a JUP_BF16 pool", me);
+    if (n_rows == 0) return JUP_OK;
+    if (b->n_seqs == 0) return set_error(JUP_EINVAL, "%s: rows without requests", me);
+    if (!b->positions || !b->slots) return set_error(JUP_EINVAL, "%s: positions and slots must not be NULL", me);
+    hipStream_t s = (hipStream_t)stream;
+    return launched(me, c.dtype == JUP_F32
+                            ? jup::f32_forward(*stage, (const float*)hidden_in, n_rows, 0, jup::KvView{}, (float*)hidden_out, s, nullptr, &step)
+                            : jup::bf16_forward(*stage, hidden_in, n_rows, 0, jup::KvView{}, hidden_out, s, nullptr, nullptr, nullptr, &step));
 }
 
 jup_status_t jup_verify_drafts(const jup_verify_drafts_t* a, void* stream) {

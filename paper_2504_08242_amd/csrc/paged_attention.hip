@@ -23,6 +23,7 @@ struct Attention {
     const u16 *q, *k, *v;
     u16* out;
     long long q_row, q_head, out_row, out_head;   // strides
+    int tiled;                                    // not 0: out is [rows, heads x 128] in the layout of a projection's operand, so many stages
     long long block, head, slot;
     const int *row_start, *lengths, *table;
     long long table_row;
@@ -43,6 +44,12 @@ __device__ __forceinline__ Attention args_again() {
     return *(const Attention*)p;
 }
 constexpr int kPartRow = 132;  // 128 un-normalised outputs, maximum, sum, two unused
+
+// Where 16-byte piece `ch` of a row's head goes.
+__device__ __forceinline__ u16* out_piece(const Attention& a, int row, int head, int ch) {
+    if (a.tiled) return a.out + tiled_offset(row, head * 16 + ch, a.tiled);
+    return a.out + row * a.out_row + head * a.out_head + ch * 8;
+}
 
 // ---- who does what -------------------------------------------------------------------------------------------------------
 // A request of m new tokens has ceil(m G / R) tiles of R rows; a tile whose last row sees n keys has ceil(n / 32) key tiles,
@@ -317,7 +324,7 @@ __device__ __forceinline__ void join_rows(const Attention& a, const Work& w, int
         if (wave + x * WAVES >= rows) continue;
         const float inv = l[x] == 0.f ? 0.f : 1.0f / l[x];
         const int row = w.tile * R + wave + x * WAVES, token = a.group.of(row);
-        *(unsigned*)(a.out + (long long)(w.begin + token) * a.out_row + (long long)((kv_head - token) * (int)a.group.d + row) * a.out_head + 2 * lane) =
+        *(unsigned*)(out_piece(a, w.begin + token, (kv_head - token) * (int)a.group.d + row, lane >> 2) + 2 * (lane & 3)) =
             pack_bf16x2(acc[x].x * inv, acc[x].y * inv);
     }
 }
@@ -641,7 +648,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void attention_few(const Attenti
         u32x4 o;
         o[0] = pack_bf16x2(x.x, x.y); o[1] = pack_bf16x2(x.z, x.w);
         o[2] = pack_bf16x2(y.x, y.y); o[3] = pack_bf16x2(y.z, y.w);
-        *(u32x4*)(e.out + (long long)(w.begin + token) * e.out_row + (long long)((kv_head - token) * (int)e.group.d + row) * e.out_head + ch * 8) = o;
+        *(u32x4*)out_piece(e, w.begin + token, (kv_head - token) * (int)e.group.d + row, ch) = o;
     }
 }
 
@@ -976,7 +983,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const Attention a
             const int r = r_wave + r0 + lrow, row = w.tile * kRows + r;
             if (r >= rows) break;
             const int token = e.group.of(row);
-            *(u32x4*)(e.out + (long long)(w.begin + token) * e.out_row + (long long)((kv_head - token) * (int)e.group.d + row) * e.out_head + lp * 8) =
+            *(u32x4*)out_piece(e, w.begin + token, (kv_head - token) * (int)e.group.d + row, lp) =
                 *(const u32x4*)(lds + r * 256 + (lp ^ (r & 15)) * 16);
         }
         return;
@@ -1005,7 +1012,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const Attention a
         u32x4 z;
         z[0] = pack_bf16x2(x.x, x.y); z[1] = pack_bf16x2(x.z, x.w);
         z[2] = pack_bf16x2(y.x, y.y); z[3] = pack_bf16x2(y.z, y.w);
-        *(u32x4*)(e.out + (long long)(w.begin + token) * e.out_row + (long long)((kv_head - token) * (int)e.group.d + row) * e.out_head + ch * 8) = z;
+        *(u32x4*)out_piece(e, w.begin + token, (kv_head - token) * (int)e.group.d + row, ch) = z;
     }
 }
 
@@ -1113,7 +1120,7 @@ hipError_t launch(K* kernel, int threads, int lds, bool* done, Attention a, long
 
 }  // namespace
 
-hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_attention_t& c, hipStream_t s) {
+hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_attention_t& c, hipStream_t s, int tiled) {
     const int shift = log2_of(pool.page_size);
     if (pool.dtype == JUP_F32) {
         hipLaunchKernelGGL(attention_f32, dim3((unsigned)c.n_rows * (unsigned)c.n_heads), dim3(64), 0, s, pool, c, shift);
@@ -1123,6 +1130,7 @@ hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_
     a.q = (const u16*)c.q; a.k = (const u16*)pool.k; a.v = (const u16*)pool.v; a.out = (u16*)c.out;
     a.q_row = c.q_row_stride; a.q_head = c.q_head_stride; a.out_row = c.out_row_stride; a.out_head = c.out_head_stride;
     a.block = pool.block_stride; a.head = pool.head_stride; a.slot = pool.slot_stride;
+    a.tiled = tiled;
     a.row_start = c.row_start; a.lengths = c.lengths; a.table = c.table; a.table_row = c.table_stride;
     a.n_seqs = c.n_seqs; a.n_rows = c.n_rows; a.n_kv_heads = pool.n_kv_heads; a.n_blocks = pool.n_blocks; a.shift = shift;
     a.positions = c.table_width << shift;

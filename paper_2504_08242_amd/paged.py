@@ -8,6 +8,7 @@ whose last is 1, the same for both), a block table an int32 tensor [n_requests, 
     for layer in ...:
         q = append(k, v, step.slots, k_pool, v_pool, positions=step.positions, rope_theta=1e4, q=q)
         out = attention(q, k_pool, v_pool, table, step.row_start, step.lengths, max_new, workspace)
+    # ... or, for a stage of this package: hidden = prefill(stage, hidden, step, k_pools, v_pools, table, max_new, workspace)
     verdict = verify(tokens, target_probs, step.row_start, u_accept, u_sample, workspace, lengths=lengths)
 
 Argument marshalling only: every operator is a HIP kernel of the library.  The calls are asynchronous on ``stream`` (default: the
@@ -57,6 +58,12 @@ class _Verify(ctypes.Structure):
         ("workspace_bytes", _sz)]
 
 
+class _Batch(ctypes.Structure):
+    _fields_ = [("pool", _Pool), ("layer_stride", _i64)] + [(n, _i32) for n in ("n_seqs", "max_new", "table_width")] + [
+        ("table_stride", _i64)] + [(n, _vp) for n in ("row_start", "lengths", "table", "positions", "slots", "workspace")] + [
+        ("workspace_bytes", _sz)]
+
+
 # The structs as one pack() each: a ctypes object of 25 fields takes longer to fill than the GPU to answer a small call.
 _FORMATS = {_i32: "i", _i64: "q", _vp: "P", _f32: "f", _sz: "N"}
 
@@ -82,6 +89,7 @@ def _lib():
             "jup_paged_append": (_i32, [_vp, _vp, _vp]),
             "jup_paged_attention": (_i32, [_vp, _vp, _vp]),
             "jup_paged_workspace_bytes": (_sz, []),
+            "jup_stage_prefill_paged": (_i32, [_vp, _vp, _i32, _vp, _vp, _vp]),
             "jup_verify_drafts": (_i32, [_vp, _vp]),
         }.items():
             fn = getattr(L, name)
@@ -261,6 +269,35 @@ def attention(q, k_pool, v_pool, table, row_start, lengths, max_new, workspace=N
                           1.0 / math.sqrt(dim) if scale is None else scale,
                           *(_scratch(workspace, at) if workspace is not None or dtype is not _F32 else (0, 0))))
     return out
+
+
+def prefill(stage, hidden_in, step, k_pools, v_pools, table, max_new, workspace=None, hidden_out=None, stream=None):
+    """A ``binding.Stage`` over the rows hidden_in [rows, d_model] of a ragged batch (jup_stage_prefill_paged): hidden_out (default: a new
+    tensor).  step: what ``extend`` returned; k_pools, v_pools [n_layers, n_blocks, n_heads, page_size, head_dim]."""
+    if k_pools.dim() != 5 or v_pools.shape != k_pools.shape or k_pools.shape[0] != stage.cfg["n_layers"] or (
+            k_pools.shape[0] > 1 and v_pools.stride(0) != k_pools.stride(0)):
+        raise ValueError(f"k_pools and v_pools must be tensors [{stage.cfg['n_layers']}, n_blocks, n_heads, page_size, head_dim] of the same strides")
+    if k_pools.shape[0] == 0:
+        raise ValueError("a stage without layers has no pools")
+    packed, dtype, at, _, _ = _pool(k_pools[0], v_pools[0])
+    n, rows, width = step.lengths.numel(), hidden_in.shape[0], stage.cfg["d_model"]
+    if hidden_out is None:
+        hidden_out = made = torch.empty_like(hidden_in)
+    else:
+        made = None
+    for name, t in (("hidden_in", hidden_in), ("hidden_out", hidden_out)):
+        if t.dtype is not dtype or t.get_device() != at or t.shape != (rows, width) or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor [{rows}, {width}] on cuda:{at}, not {t.dtype} {list(t.shape)} on {t.device}")
+    if step.positions.numel() < rows or step.slots.numel() < rows:
+        raise ValueError(f"the step has positions of {step.positions.numel()} rows, hidden_in {rows}")
+    tables, table_width, stride = _table(table, at, n)
+    scratch = _scratch(workspace, at) if workspace is not None or dtype is not _F32 else (0, 0)
+    batch = _Batch(_Pool.from_buffer_copy(packed), k_pools.stride(0), n, int(max_new), table_width, stride, _ints("row_start", step.row_start, at, n + 1),
+                   _ints("lengths", step.lengths, at, n), tables, _ints("positions", step.positions, at, step.positions.numel()),
+                   _ints("slots", step.slots, at, step.slots.numel()), *scratch)
+    fn = _lib().jup_stage_prefill_paged
+    _call(lambda handle: fn(stage.handle, hidden_in.data_ptr(), rows, ctypes.byref(batch), hidden_out.data_ptr(), handle), at, stream, made)
+    return hidden_out
 
 
 def _probs(name, t, dtype, at, rows, vocab):

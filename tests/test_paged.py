@@ -827,3 +827,162 @@ def test_a_captured_step_is_replayed():
         for a, b in zip(one.pools, other.pools):
             assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
         assert torch.equal(one.table, other.table) and one.free_count.tolist() == other.free_count.tolist()
+
+
+# ---- a stage over pages -------------------------------------------------------------------------------------------------------------
+
+
+def small_stage(dtype, max_rows, w4_expanded=False):
+    """A stage, one oracle per request on demand, and the config; bars are those of the parity tests."""
+    import oracle
+    from oracle import w4
+    from paper_2504_08242_amd import synth_inputs as si
+    cfg = dict(si.TINY) if dtype == "f32" else dict(si.LLAMA7B_STAGE, n_layers=2, d_model=1024, n_heads=8, d_ffn=2816)
+    if dtype == "w4":
+        layers = si.make_w4_layers(cfg, seed=5)
+        dev, full = jb.upload_w4_layers(layers), w4.dequantize_layers(layers)
+    else:
+        layers = full = si.make_layers(cfg, seed=5, bf16=dtype == "bf16")
+        dev = jb.upload_layers(layers, dtype)
+    stage = jb.Stage(cfg, dtype, dev, max_rows, w4_expanded=w4_expanded)
+    torch.cuda.synchronize()
+    return cfg, stage, lambda n: oracle.OracleStage(cfg, full, n)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,steps", [
+    ("f32", [[37, 5, 0, 16], [1, 3, 20, 1], [1, 1, 1, 1]]),
+    ("bf16", [[37, 5, 0, 16], [1, 3, 20, 1], [1, 1, 1, 1], [5, 5, 1, 5]]),     # 58, 25, 4 and 16 rows
+    ("bf16", [[300, 0, 140, 64], [1, 200, 1, 1]]),
+    ("w4", [[37, 5, 0, 16], [1, 3, 7, 1], [1, 1, 1, 1]]),
+    ("w4+bf16", [[90, 5, 0, 16], [1, 1, 1, 1]])])
+def test_a_stage_over_pages(dtype, steps, workspace):
+    """Ragged steps of four requests through a stage, rows of every request and what it caches against the oracle."""
+    import helpers
+    from paper_2504_08242_amd import synth_inputs as si
+    expanded, dtype = dtype == "w4+bf16", dtype.split("+")[0]
+    page, spare, n = 16, 3, 4
+    most = max(sum(s) for s in steps) + spare
+    cfg, stage, new_oracle = small_stage(dtype, most, expanded)
+    total = [sum(s[i] for s in steps) for i in range(n)]
+    oracles = [new_oracle(max(1, t)) for t in total]
+    td = torch.float32 if dtype == "f32" else torch.bfloat16
+    hidden = [si.make_hidden(cfg, 5, max(1, t), tag=i, bf16=dtype != "f32") for i, t in enumerate(total)]
+    heads, D = cfg["n_heads"], cfg["head_dim"]
+    n_blocks = sum(-(-t // page) for t in total) + 2
+    gen = torch.Generator().manual_seed(1)
+    k_pools, v_pools = (torch.full((cfg["n_layers"], n_blocks, heads, page, D), float("nan"), dtype=td, device=DEV) for _ in "kv")
+    table = torch.full((n, max(-(-t // page) for t in total)), -1, dtype=torch.int32, device=DEV)
+    free, count = ints(torch.randperm(n_blocks, generator=gen).tolist()), ints([n_blocks])
+    lengths, owned = ints([0] * n), ints([0] * n)
+    at = [0] * n
+    for new in steps:
+        rows = sum(new)
+        step = jp.extend(lengths, ints(new), owned, table, free, count, page, rows + spare, in_place=True)
+        x = torch.full((rows + spare, cfg["d_model"]), 0.5, dtype=td, device=DEV)
+        x[:rows] = torch.from_numpy(np.concatenate([h[a:a + m] for h, a, m in zip(hidden, at, new)])).to(DEV, td)
+        y = jp.prefill(stage, x, step, k_pools, v_pools, table, max(new), workspace)
+        assert step.status.item() == 0
+        got, row = y[:rows].float().cpu().numpy(), 0
+        for i, m in enumerate(new):
+            if m:
+                want = oracles[i].prefill_chunk(hidden[i][at[i]:at[i] + m], at[i])
+                if dtype == "f32":
+                    assert helpers.rel_l2(got[row:row + m], want) <= helpers.F32_REL_L2
+                else:
+                    helpers.assert_rows_close(got[row:row + m], want, what=f"request {i}, {m} rows at {at[i]}")
+            row += m
+            at[i] += m
+        again = x.clone()
+        assert jp.prefill(stage, again, step, k_pools, v_pools, table, 1, workspace, hidden_out=again) is again   # in place, wrong hint
+        helpers.assert_rows_close(again[:rows].float().cpu().numpy(), got, bound=1e-6 if dtype == "f32" else helpers.BF16_ROW_REL_L2)
+    assert lengths.tolist() == total
+    t = table.cpu().numpy()
+    for i, m in enumerate(total):
+        for which, pools in enumerate((k_pools, v_pools)):
+            kept = f64(pools[:, t[i, :-(-m // page)]].transpose(1, 2).reshape(cfg["n_layers"], heads, -1, D)[:, :, :m])
+            want = oracles[i].kv[:, which, :, :m]
+            if dtype == "f32":
+                assert helpers.rel_l2(kept, want) <= helpers.F32_REL_L2
+            else:
+                helpers.assert_rows_close(kept, want, what=f"cache of request {i}")
+
+
+@gpu
+def test_a_stage_over_pages_in_a_graph(workspace):
+    """Decoding steps of a stage, captured: tables, all layers; every replay gives what the same calls give outside."""
+    cfg, stage, _ = small_stage("bf16", 16)
+    states = []
+    for _ in range(2):
+        gen = torch.Generator().manual_seed(2)
+        s = dict(lengths=ints([40, 7, 100]), owned=ints([3, 1, 7]), table=torch.full((3, 12), -1, dtype=torch.int32, device=DEV), free=ints(range(11, 40)),
+                 count=ints([29]), pools=[torch.randn((2, 40, 8, 16, 128), generator=gen).to(DEV, torch.bfloat16) for _ in "kv"],
+                 x=torch.randn((16, 1024), generator=gen).to(DEV, torch.bfloat16), n_new=ints([5, 1, 3]))
+        for i, row in enumerate(([0, 1, 2], [3], [4, 5, 6, 7, 8, 9, 10])):
+            s["table"][i, :len(row)] = ints(row)
+        states.append(s)
+
+    def run(s, space):
+        step = jp.extend(s["lengths"], s["n_new"], s["owned"], s["table"], s["free"], s["count"], 16, 16, in_place=True)
+        return step, jp.prefill(stage, s["x"], step, *s["pools"], s["table"], 5, space)
+
+    one, other = states
+    run(one, workspace), run(other, workspace)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph, space = torch.cuda.CUDAGraph(), jp.Workspace(DEV)
+    with torch.cuda.graph(graph, stream=side):
+        step, y = run(one, space)
+    for _ in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        want_step, want = run(other, workspace)
+        torch.cuda.synchronize()
+        assert step.slots.tolist() == want_step.slots.tolist() and one["lengths"].tolist() == other["lengths"].tolist()
+        assert torch.equal(y[:9], want[:9]) and torch.equal(one["pools"][0], other["pools"][0])
+        one["x"].copy_(y), other["x"].copy_(want)
+        one["x"][9:] = other["x"][9:] = 0.25
+
+
+@gpu
+def test_a_stage_over_pages_refuses(workspace):
+    cfg, stage, _ = small_stage("bf16", 8)
+    k = torch.zeros((2, 4, 8, 16, 128), dtype=torch.bfloat16, device=DEV)
+    table = torch.zeros((1, 2), dtype=torch.int32, device=DEV)
+    x = torch.zeros((4, 1024), dtype=torch.bfloat16, device=DEV)
+    step = jp.Step(ints([0, 4]), ints([0, 1, 2, 3]), ints([0, 1, 2, 3]), ints([4]), None, None, None)
+    run = lambda **c: jp.prefill(**dict(dict(stage=stage, hidden_in=x, step=step, k_pools=k, v_pools=k, table=table, max_new=4, workspace=workspace), **c))  # noqa: E731
+    run()
+    torch.cuda.synchronize()
+    for change in (dict(hidden_in=x[:, :512]), dict(hidden_in=x.float()), dict(k_pools=k[:1]), dict(v_pools=k[:, :2]), dict(hidden_out=x[:3]), dict(workspace=None),
+                   dict(step=step._replace(slots=ints([0]))), dict(step=step._replace(row_start=ints([0]))), dict(table=table[:0]),
+                   dict(hidden_in=torch.zeros((5, 1024), dtype=torch.bfloat16, device=DEV))):
+        with pytest.raises(ValueError):
+            run(**change)
+    many = jp.Step(ints([0, 4]), ints(range(9)), ints(range(9)), ints([9]), None, None, None)
+    with pytest.raises(jb.JupiterError) as e:
+        run(hidden_in=torch.zeros((9, 1024), dtype=torch.bfloat16, device=DEV), step=many)
+    assert e.value.status == jb.JUP_ECAP
+    few = torch.zeros((2, 4, 4, 16, 128), dtype=torch.bfloat16, device=DEV)   # pools of four heads
+    with pytest.raises(jb.JupiterError) as e:
+        run(k_pools=few, v_pools=few)
+    assert e.value.status == jb.JUP_EINVAL and "configuration" in str(e.value)
+    none = x[:0]
+    assert run(hidden_in=none).shape == (0, 1024)
+    L, batch = jp._lib(), jp._Batch(pool=pool_args(n_kv_heads=8), n_seqs=1, max_new=1, table_width=2, table_stride=2, row_start=FAKE, lengths=FAKE,
+                                    table=FAKE, positions=FAKE, slots=FAKE, workspace=FAKE, workspace_bytes=workspace.args[1])
+    for change, word in ((dict(layer_stride=-8), "layer_stride"), (dict(layer_stride=4), "layer_stride"), (dict(positions=None), "positions"),
+                         (dict(slots=None), "slots"), (dict(n_seqs=0), "requests"), (dict(max_new=-1), "max_new"), (dict(workspace=None), "workspace"),
+                         (dict(table_stride=1), "table_stride"), (dict(lengths=None), "NULL")):
+        b = jp._Batch.from_buffer_copy(batch)
+        for name, value in change.items():
+            setattr(b, name, value)
+        refused(L.jup_stage_prefill_paged(stage.handle, FAKE, 2, ctypes.byref(b), FAKE, None), word)
+    refused(L.jup_stage_prefill_paged(stage.handle, FAKE, -1, ctypes.byref(batch), FAKE, None), "n_rows")
+    refused(L.jup_stage_prefill_paged(stage.handle, FAKE + 2, 2, ctypes.byref(batch), FAKE, None), "aligned")
+    refused(L.jup_stage_prefill_paged(stage.handle, None, 2, ctypes.byref(batch), FAKE, None), "NULL")
+    refused(L.jup_stage_prefill_paged(stage.handle, FAKE, 2, None, FAKE, None), "batch")
+
+
+def test_a_missing_stage_is_refused():
+    refused(jp._lib().jup_stage_prefill_paged(None, FAKE, 2, ctypes.byref(jp._Batch()), FAKE, None), "stage")
