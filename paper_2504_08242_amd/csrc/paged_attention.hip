@@ -376,17 +376,19 @@ __device__ __forceinline__ void store_pieces(const unsigned char* sums, int row_
 //   QW = 16, 16x16x32 (lane = 16 hh + c): A[m = c][k = 8 hh + e], B[k = 8 hh + e][n = c], D[m = 4 hh + i][n = c].
 // P^T is taken as the scores lie in the accumulators; V^T is read for exactly that order of keys.
 // LDS tiles, rows of 256 bytes in 16 chunks of 16:  K: chunk ch of row r at position ch ^ (r & 15);  V: at (((ch >> 2) ^ (r & 3)) << 2) | (ch & 3).
-constexpr int kFewWaves = 4;
-constexpr int kFewQ = kFewWaves * 2 * kTileBytes;                       // the tile of rows, K layout
-constexpr int few_stat(int QW) { return kFewQ + (QW == 32 ? 8192 : 4096); }  // [2][waves][QW] maxima and sums
-constexpr int few_lds(int QW) { return few_stat(QW) + 2 * kFewWaves * QW * 4; }
-static_assert(kFewWaves * 32 * 132 * 4 <= few_stat(32) && kFewWaves * 16 * 132 * 4 <= few_stat(16), "merge regions overlap the statistics");
-static_assert(2 * few_lds(32) <= 160 * 1024, "two workgroups share a CU");
+template <int QW, int NW>
+struct Few {
+    static constexpr int kQ = NW * 2 * kTileBytes;             // the tile of rows, K layout
+    static constexpr int kStat = kQ + QW * 256;                // [2][waves][QW] maxima and sums
+    static constexpr int kLds = kStat + 2 * NW * QW * 4;
+    static_assert(NW * QW * 132 * 4 <= kStat, "merge regions overlap the statistics");
+    static_assert((8 / NW) * kLds <= 160 * 1024, "two workgroups of four waves share a CU");
+};
 
-template <int QW>
-__global__ __launch_bounds__(64 * kFewWaves, 2) void attention_few(const Attention args, int least) {
+template <int QW, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void attention_few(const Attention args, int least) {
+    typedef Few<QW, NW> L;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-    constexpr int NW = kFewWaves;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & (QW - 1), hh = lane / QW;
@@ -406,7 +408,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void attention_few(const Attenti
         const int r = r0 + lrow;
         const int row = w.tile * QW + min(r, rows - 1), token = a.group.of(row);
         const u16* from = a.q + (long long)(w.begin + token) * a.q_row + (long long)(kv_head * G + row - token * G) * a.q_head;
-        load_to_lds_16(from + (lp ^ (r & 15)) * 8, lds0 + kFewQ + r0 * 256);
+        load_to_lds_16(from + (lp ^ (r & 15)) * 8, lds0 + L::kQ + r0 * 256);
     }
     const int last_key = w.keys - 1;
     const int my_token = a.group.of(w.tile * QW + min(c, rows - 1));
@@ -451,7 +453,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void attention_few(const Attenti
     const unsigned k_lane = c * 256 + ((hh ^ (c & 15)) * 16);
     bf16x8 qf[KS];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const bf16x8*)(lds + kFewQ + (k_lane ^ (kStep * ks)));
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const bf16x8*)(lds + L::kQ + (k_lane ^ (kStep * ks)));
     acc_t oacc[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -591,7 +593,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void attention_few(const Attenti
     constexpr int kRow = 132;
     constexpr int kRegion = QW * kRow;
     float* obuf = (float*)lds;
-    float* stat_m = (float*)(lds + few_stat(QW));
+    float* stat_m = (float*)(lds + L::kStat);
     float* stat_l = stat_m + NW * QW;
     {
         float l_tot = l_run + __shfl_xor(l_run, 32, 64);
@@ -631,7 +633,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void attention_few(const Attenti
     __syncthreads();
     if (w.pieces > 1) {
         store_pieces<NW, NW>(lds, kRow * 4, kRegion * 4, e.partial + part * kPartRow, rows);
-        join_pieces<QW, NW>(w, kv_head, (int*)(lds + few_stat(QW)));
+        join_pieces<QW, NW>(w, kv_head, (int*)(lds + L::kStat));
         return;
     }
     for (int idx = tid; idx < rows * 16; idx += 64 * NW) {
@@ -1087,6 +1089,7 @@ namespace {
 // have on average: four times.
 constexpr int kFewRows = 32;       // a request's rows up to which attention_few has it
 constexpr int kFewPieces = 512;    // two workgroups per CU
+constexpr int kWidePieces = 192;   // of eight waves
 constexpr int kLeast16 = 24, kLeast32 = 16, kLeastMany = 24;  // key tiles that are worth a piece
 constexpr int kManyPieces = 222;   // a workgroup per CU, less what the longest may be longer than the average
 constexpr int kMostSplitHeads = 128;  // (more heads than that fill the chip without dividing keys)
@@ -1140,10 +1143,14 @@ hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_
     a.partial = (float*)((char*)c.workspace + kCountBytes);
     a.least_rows = 0; a.most_rows = INT32_MAX;
     const long long rows = (long long)c.n_rows * a.group.d, most = (long long)c.max_new * a.group.d;
-    static bool done16[64], done32[64], done_many[64];
+    static bool done16[64], done32[64], done16w[64], done32w[64], done_many[64];
     auto few = [&](Attention x, long long tiles16, long long tiles32) {
-        return most <= 16 ? launch(attention_few<16>, 64 * kFewWaves, few_lds(16), done16, x, tiles16, kFewPieces, kFewPlaces, kLeast16, s)
-                          : launch(attention_few<32>, 64 * kFewWaves, few_lds(32), done32, x, tiles32, kFewPieces, kFewPlaces, kLeast32, s);
+        const long long tiles = most <= 16 ? tiles16 : tiles32;
+        if (tiles * pool.n_kv_heads <= 256)  // a workgroup per CU at most: of eight waves, and pieces for three CUs in four
+            return most <= 16 ? launch(attention_few<16, 8>, 512, Few<16, 8>::kLds, done16w, x, tiles, kWidePieces, kFewPlaces, kLeast16, s)
+                              : launch(attention_few<32, 8>, 512, Few<32, 8>::kLds, done32w, x, tiles, kWidePieces, kFewPlaces, kLeast16, s);
+        return most <= 16 ? launch(attention_few<16, 4>, 256, Few<16, 4>::kLds, done16, x, tiles, kFewPieces, kFewPlaces, kLeast16, s)
+                          : launch(attention_few<32, 4>, 256, Few<32, 4>::kLds, done32, x, tiles, kFewPieces, kFewPlaces, kLeast32, s);
     };
     if (most <= kFewRows) return few(a, rows / 16 + c.n_seqs, rows / 32 + c.n_seqs);
     Attention longer = a;
