@@ -23,7 +23,7 @@
  *     slots) is checked by the kernels: whatever these hold, nothing outside the given buffers is read or written.
  *   - dtype JUP_F32 or JUP_BF16 as in jupiter_stage.h: JUP_F32 is the check mode (plain kernels, any even head_dim up to
  *     256); JUP_BF16 needs head_dim 128, 16-byte aligned tensors and strides that are multiples of 8.
- *   - Sizes: page_size is a power of two, 8 .. 65536; n_blocks * page_size and table_width * page_size <= 2^31 - 1;
+ *   - Sizes: page_size is a power of two, 8 .. 65536; n_blocks * page_size <= 2^31 - 1, table_width * page_size <= 2^31 - 256;
  *     n_seqs <= JUP_PAGED_MAX_SEQS.
  */
 #ifndef JUPITER_PAGED_H

@@ -53,8 +53,8 @@ jup_status_t check_attention(const char* me, const jup_paged_pool_t* pool, const
     if (a->n_heads <= 0 || a->n_heads % pool->n_kv_heads)
         return set_error(JUP_EINVAL, "%s: n_heads=%d must be a positive multiple of n_kv_heads=%d", me, a->n_heads, pool->n_kv_heads);
     if ((int64_t)a->n_rows * a->n_heads > INT32_MAX) return set_error(JUP_EINVAL, "%s: n_rows * n_heads exceeds 2^31 - 1", me);
-    if (a->table_width < 0 || (int64_t)a->table_width * pool->page_size > INT32_MAX)
-        return set_error(JUP_EINVAL, "%s: table_width=%d is negative, or table_width * page_size exceeds 2^31 - 1", me, a->table_width);
+    if (a->table_width < 0 || (int64_t)a->table_width * pool->page_size > INT32_MAX - 255)
+        return set_error(JUP_EINVAL, "%s: table_width=%d is negative, or table_width * page_size exceeds 2^31 - 256", me, a->table_width);
     if (a->table_stride < a->table_width) return set_error(JUP_EINVAL, "%s: table_stride is shorter than table_width", me);
     if (!(a->scale > 0.0f) || a->scale > 3e38f) return set_error(JUP_EINVAL, "%s: scale must be positive and finite", me);
     if (a->n_rows == 0 || a->n_seqs == 0) return JUP_OK;
@@ -77,8 +77,8 @@ jup_status_t jup_paged_extend(const jup_paged_extend_t* a, void* stream) {
         return set_error(JUP_EINVAL, "%s: n_seqs=%d is outside 0..%d", me, a->n_seqs, JUP_PAGED_MAX_SEQS);
     if (a->page_size < 8 || a->page_size > jup::kMaxPageSize || (a->page_size & (a->page_size - 1)))
         return set_error(JUP_EINVAL, "%s: page_size=%d must be a power of two, 8 .. 65536", me, a->page_size);
-    if (a->table_width < 0 || (int64_t)a->table_width * a->page_size > INT32_MAX)
-        return set_error(JUP_EINVAL, "%s: table_width=%d is negative, or table_width * page_size exceeds 2^31 - 1", me, a->table_width);
+    if (a->table_width < 0 || (int64_t)a->table_width * a->page_size > INT32_MAX - 255)
+        return set_error(JUP_EINVAL, "%s: table_width=%d is negative, or table_width * page_size exceeds 2^31 - 256", me, a->table_width);
     if (a->table_stride < a->table_width) return set_error(JUP_EINVAL, "%s: table_stride is shorter than table_width", me);
     if (a->n_free < 0 || a->max_rows < 0) return set_error(JUP_EINVAL, "%s: n_free and max_rows must not be negative", me);
     if (!a->free_count || !a->row_start || !a->new_free_count || !a->status)

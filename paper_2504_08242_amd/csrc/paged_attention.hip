@@ -6,7 +6,7 @@
 //
 // Who does what is found on the GPU: lengths are known nowhere else.  Every wave reads the lengths of all requests (64 lanes, a
 // prefix sum), so a launch needs no table of work and no launch before it: the host's grid is an upper bound, and the
-// workgroups past the last piece of work leave.  See find_work().
+// workgroups past the last piece of work leave.  Of more than 64 requests plan_work() makes a table first.  See find_work().
 #include "paged.h"
 
 namespace jup {
@@ -30,6 +30,7 @@ struct Attention {
     int n_seqs, n_rows, n_kv_heads, n_blocks, shift, positions;  // positions: of a table row, table_width pages
     Quotient group;                               // G
     float scale_log2e;
+    const int2* plan;                             // of more than 64 requests: see plan_work()
     int* count;                                   // arrival counters of rows whose keys are divided, zero between launches
     float* partial;                               // [slot][kv head][row of the tile][kPartRow]
     float chunk_factor;                           // 1 / pieces of work per key/value head that fill the chip (find_work); large: keys are not divided
@@ -75,21 +76,19 @@ __device__ __forceinline__ int pieces_of(int key_tiles, int chunk) { return max(
 template <int R>
 struct Request {
     int begin, tokens, before, tiles, key_tiles;  // key_tiles: of the last tile
+    Request() = default;
+    // (no branches: the loads of several requests are in flight together)
     __device__ __forceinline__ Request(const Attention& a, int i, int last) {
-        begin = tokens = before = tiles = key_tiles = 0;
-        if (i >= last) return;
-        begin = a.row_start[i];
-        const int end = a.row_start[i + 1], length = a.lengths[i];
-        if (begin < 0 || end <= begin) return;
-        tokens = min(end, a.n_rows) - begin;
-        const long long rows = (long long)tokens * a.group.d;
-        if (tokens <= 0 || rows < a.least_rows || rows > a.most_rows) {
-            tokens = 0;
-            return;
-        }
-        before = (int)max((long long)length - (end - begin), -(long long)INT32_MAX);
-        tiles = (int)((rows + R - 1) / R);
-        key_tiles = (keys_of(a, tokens - 1) + kKT - 1) / kKT;
+        const int at = min(i, last - 1);
+        const int start = a.row_start[at], end = a.row_start[at + 1], length = a.lengths[at];
+        const int n = (int)((unsigned)min(end, a.n_rows) - (unsigned)start);  // (start >= 0 where it counts)
+        const long long rows = (long long)n * a.group.d;
+        const bool counts = i < last && start >= 0 && end > start && n > 0 && rows >= a.least_rows && rows <= a.most_rows;
+        begin = counts ? start : 0;
+        tokens = counts ? n : 0;
+        before = (int)max((long long)length - ((long long)end - start), -(long long)INT32_MAX);
+        tiles = counts ? (int)((rows + R - 1) / R) : 0;
+        key_tiles = counts ? (keys_of(a, tokens - 1) + kKT - 1) / kKT : 0;
     }
     // keys that token t sees
     __device__ __forceinline__ int keys_of(const Attention& a, int t) const {
@@ -101,88 +100,140 @@ struct Request {
         return (float)tiles * (float)key_tiles;
     }
     __device__ __forceinline__ int pieces(int chunk) const { return tiles == 0 ? 0 : pieces_of(key_tiles, chunk); }
+    __device__ __forceinline__ int items(int chunk) const { return tiles * pieces(chunk); }
+    __device__ __forceinline__ int slots(int chunk) const { return pieces(chunk) > 1 ? items(chunk) : 0; }
 };
 
-// Piece number `item` of a key/value head; false: there are fewer.  All lanes of a wave call it and get the same.  R: rows of a tile;
-// least: the shortest piece worth a workgroup, in key tiles.
+// The longest piece: all requests' costs over the pieces wanted.  (Rounded up by more than the sums are off: at most as many pieces
+// more than tiles as are wanted.)  least: the shortest piece worth a workgroup, in key tiles.
+__device__ __forceinline__ int chunk_of(const Attention& a, float cost, int least) {
+    return __builtin_amdgcn_readfirstlane((int)fminf(fmaxf(cost * a.chunk_factor + 1.0f, (float)least), 1e9f));
+}
+__device__ __forceinline__ void prefix_sums(int& x, int& y, int lane) {  // inclusive, over a wave
+#pragma unroll
+    for (int by = 1; by < 64; by *= 2) {
+        const int x2 = __shfl_up(x, by, 64), y2 = __shfl_up(y, by, 64);
+        if (lane >= by) {
+            x += x2;
+            y += y2;
+        }
+    }
+}
+
+// More than 64 requests, whose prefix sums every wave of every workgroup would otherwise make again: entry i of the plan is the pieces and
+// the places of the scratch before request i, the one behind the last request all pieces and the longest piece.  One workgroup, a few
+// neighbouring requests per thread.
+template <int R>
+__global__ __launch_bounds__(1024) void plan_work(const Attention a, int least, int2* plan) {
+    __shared__ float costs[16];
+    __shared__ int2 sums[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int each = (a.n_seqs + 1023) / 1024, from = tid * each, to = min(a.n_seqs, from + each);
+    float cost = 0.f;
+    for (int i = from; i < to; ++i) cost += Request<R>(a, i, to).cost(a);
+    cost = wave_sum(cost);
+    if (lane == 0) costs[wave] = cost;
+    __syncthreads();
+    cost = 0.f;
+    for (int x = 0; x < 16; ++x) cost += costs[x];
+    const int chunk = chunk_of(a, cost, least);
+    int items = 0, slots = 0;
+    for (int i = from; i < to; ++i) {
+        const Request<R> r(a, i, to);
+        items += r.items(chunk);
+        slots += r.slots(chunk);
+    }
+    int items_to = items, slots_to = slots;
+    prefix_sums(items_to, slots_to, lane);
+    if (lane == 63) sums[wave] = make_int2(items_to, slots_to);
+    __syncthreads();
+    for (int x = 0; x < wave; ++x) {
+        items_to += sums[x].x;
+        slots_to += sums[x].y;
+    }
+    if (tid == 1023) plan[a.n_seqs] = make_int2(items_to, chunk);
+    items_to -= items;
+    slots_to -= slots;
+    for (int i = from; i < to; ++i) {
+        const Request<R> r(a, i, to);
+        plan[i] = make_int2(items_to, slots_to);
+        items_to += r.items(chunk);
+        slots_to += r.slots(chunk);
+    }
+}
+
+// Piece number `item` of a key/value head; false: there are fewer.  All lanes of a wave call it and get the same.  R: rows of a tile.
 constexpr int kOrdered = 16;  // requests that are put in order of their lengths
 
 template <int R>
 __device__ bool find_work(const Attention& a, int item, int least, Work& w) {
     const int lane = threadIdx.x & 63;
-    // the requests from `first` on are dealt to the lanes, `each` neighbours to a lane; the lane whose requests have the piece is gone
-    // into in the same way, until a lane has one request
-    int first = 0, last = a.n_seqs, each = (last + 63) / 64, chunk = 0, slots_before = 0;
-    for (;;) {
-        int items = 0, slots = 0;
-        Request<R> r(a, first + lane * each, last);
-        if (chunk == 0) {  // (first time round)
-            float cost = r.cost(a);
-            for (int j = 1; j < each; ++j) cost += Request<R>(a, first + lane * each + j, last).cost(a);
-            // (rounded up by more than the sums are off: at most as many pieces more than tiles as are wanted, as the grid says)
-            chunk = __builtin_amdgcn_readfirstlane((int)fminf(fmaxf(wave_sum(cost) * a.chunk_factor + 1.0f, (float)least), 1e9f));
-        }
-        for (int j = 0; j < each; ++j) {
-            const Request<R> x = j == 0 ? r : Request<R>(a, first + lane * each + j, min(last, first + (lane + 1) * each));
-            const int p = x.pieces(chunk);
-            items += x.tiles * p;
-            if (p > 1) slots += x.tiles * p;
-        }
+    int seq, chunk, slots_before;
+    Request<R> r;
+    if (!a.plan) {  // a lane per request
+        const int n = a.n_seqs;
+        r = Request<R>(a, lane, n);
+        chunk = chunk_of(a, wave_sum(r.cost(a)), least);
+        const int items = r.items(chunk), slots = r.slots(chunk);
         int items_to = items, slots_to = slots;
-        if (R > 32 && last - first <= kOrdered) {
+        if (R > 32 && n <= kOrdered) {
             // whole prompts: the requests with the most keys first, so that what is left for the end is short
-            for (int j = 0; j < last - first; ++j) {
+            for (int j = 0; j < n; ++j) {
                 const int keys = __builtin_amdgcn_readlane(r.key_tiles, j);
                 const bool before = keys > r.key_tiles || (keys == r.key_tiles && j < lane);
                 items_to += before ? __builtin_amdgcn_readlane(items, j) : 0;
                 slots_to += before ? __builtin_amdgcn_readlane(slots, j) : 0;
             }
         } else {
-#pragma unroll
-            for (int by = 1; by < 64; by *= 2) {
-                const int i = __shfl_up(items_to, by, 64), s = __shfl_up(slots_to, by, 64);
-                if (lane >= by) {
-                    items_to += i;
-                    slots_to += s;
-                }
-            }
+            prefix_sums(items_to, slots_to, lane);
         }
         const unsigned long long there = __ballot(item < items_to && item >= items_to - items);
         if (!there) return false;
-        const int at = __builtin_ctzll(there);
-        item -= __builtin_amdgcn_readlane(items_to - items, at);
-        slots_before += __builtin_amdgcn_readlane(slots_to - slots, at);
-        first += at * each;
-        if (each == 1) {
-            r.begin = __builtin_amdgcn_readlane(r.begin, at);
-            r.tokens = __builtin_amdgcn_readlane(r.tokens, at);
-            r.before = __builtin_amdgcn_readlane(r.before, at);
-            r.tiles = __builtin_amdgcn_readlane(r.tiles, at);
-            r.key_tiles = __builtin_amdgcn_readlane(r.key_tiles, at);
-            const int most = r.pieces(chunk);
-            const int nth = (unsigned)item / (unsigned)max(most, 1);
-            // (sums of requests that overlap in a row_start that makes no sense can wrap)
-            if (item < 0 || nth >= r.tiles || slots_before < 0 || (most > 1 && slots_before + nth * most > a.most_places - most)) return false;
-            w.seq = first;
-            w.begin = r.begin;
-            w.tokens = r.tokens;
-            w.before = r.before;
-            w.tile = r.tiles - 1 - nth;
-            w.piece = item - nth * most;
-            w.slot = slots_before + nth * most;
-            const int last_token = min(a.group.of(min((w.tile + 1) * R, r.tokens * (int)a.group.d) - 1), r.tokens - 1);
-            w.keys = r.keys_of(a, last_token);
-            const int key_tiles = (w.keys + kKT - 1) / kKT;
-            w.pieces = pieces_of(key_tiles, chunk);
-            if (w.piece >= w.pieces) return false;  // (an earlier tile of a prompt: fewer keys than the last one)
-            const int even = (unsigned)key_tiles / (unsigned)w.pieces, over = key_tiles - even * w.pieces;
-            w.tile_lo = w.piece * even + min(w.piece, over);
-            w.tile_hi = w.tile_lo + even + (w.piece < over);
-            return true;
+        seq = __builtin_ctzll(there);
+        item -= __builtin_amdgcn_readlane(items_to - items, seq);
+        slots_before = __builtin_amdgcn_readlane(slots_to - slots, seq);
+        for (int* x : {&r.begin, &r.tokens, &r.before, &r.tiles, &r.key_tiles}) *x = __builtin_amdgcn_readlane(*x, seq);
+    } else {  // the last request with no more than `item` pieces before it: of 64 runs of neighbours, then of 64 of the run's, ...
+        const int2 all = a.plan[a.n_seqs];
+        if (item >= all.x) return false;
+        chunk = all.y;
+        seq = 0;
+        for (int last = a.n_seqs, each = (last + 63) / 64;; each = (each + 63) / 64) {
+            const int i = seq + lane * each;
+            const int2 before = a.plan[min(i, last - 1)];
+            const unsigned long long there = __ballot(i < last && before.x <= item);
+            if (!there) return false;
+            const int at = 63 - __builtin_clzll(there);
+            seq += at * each;
+            if (each == 1) {
+                item -= __builtin_amdgcn_readlane(before.x, at);
+                slots_before = __builtin_amdgcn_readlane(before.y, at);
+                break;
+            }
+            last = min(last, seq + each);
         }
-        last = min(last, first + each);
-        each = (each + 63) / 64;
+        r = Request<R>(a, seq, a.n_seqs);
     }
+    const int most = r.pieces(chunk);
+    const int nth = (unsigned)item / (unsigned)max(most, 1);
+    // (sums of requests that overlap in a row_start that makes no sense can wrap)
+    if (item < 0 || nth >= r.tiles || slots_before < 0 || (most > 1 && slots_before + nth * most > a.most_places - most)) return false;
+    w.seq = seq;
+    w.begin = r.begin;
+    w.tokens = r.tokens;
+    w.before = r.before;
+    w.tile = r.tiles - 1 - nth;
+    w.piece = item - nth * most;
+    w.slot = slots_before + nth * most;
+    const int last_token = min(a.group.of(min((w.tile + 1) * R, r.tokens * (int)a.group.d) - 1), r.tokens - 1);
+    w.keys = r.keys_of(a, last_token);
+    const int key_tiles = (w.keys + kKT - 1) / kKT;
+    w.pieces = pieces_of(key_tiles, chunk);
+    if (w.piece >= w.pieces) return false;  // (an earlier tile of a prompt: fewer keys than the last one)
+    const int even = (unsigned)key_tiles / (unsigned)w.pieces, over = key_tiles - even * w.pieces;
+    w.tile_lo = w.piece * even + min(w.piece, over);
+    w.tile_hi = w.tile_lo + even + (w.piece < over);
+    return true;
 }
 
 // ---- pages -----------------------------------------------------------------------------------------------------------------
@@ -577,7 +628,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_few(const Attention args
             if (tile < first_masked && there == ~0u) continue;
             for (int k = 0; k < kKT; ++k) {
                 if (!((there >> k) & 1)) continue;
-                const char* row = group_base(a, v_pool, b.id[k >> 3], tile * kKT + (k & ~7)) + (k & 7) * row_bytes;
+                const char* row = group_base(a, v_pool, table_row[(tile * kKT + k) >> a.shift], tile * kKT + (k & ~7)) + (k & 7) * row_bytes;
                 if (!row_not_finite(row)) continue;
 #pragma unroll
                 for (int x = 0; x < (QW == 16 ? 8 : 16); ++x) {
@@ -677,7 +728,7 @@ struct Many {
     static constexpr int kFlag = kThere + 64;
     static constexpr int kStat = kFlag + 64;                 // [2][waves][32] maxima and sums
     static constexpr int kLds = kStat + (KP > 1 ? 2 * 32 * NW * 4 : 0);
-    static_assert(kLds <= 160 * 1024 && kRing * kStepTiles * 4 <= 64);
+    static_assert(kLds <= 160 * 1024 && kRing * kStepTiles * 4 <= 64 && kRing >= 2);
     // queries go through the last places of the ring, the first kFirst steps are fetched beside them
     static constexpr int kFirst = (kThere - kQ) / (2 * kHalf) < kRing - 1 ? (kThere - kQ) / (2 * kHalf) : kRing - 1;
     static constexpr int kQAt = kThere - kQ;
@@ -942,7 +993,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const Attention a
             const unsigned there = rows_there(a, ids, tile, last_key);
             for (int k = 0; k < kKT; ++k) {
                 if (!((there >> k) & 1)) continue;
-                const char* row = group_base(a, v_pool, ids.id[k >> 3], tile * kKT + (k & ~7)) + (k & 7) * (unsigned)(a.slot * 2);
+                const char* row = group_base(a, v_pool, table_row[(tile * kKT + k) >> a.shift], tile * kKT + (k & ~7)) + (k & 7) * (unsigned)(a.slot * 2);
                 if (!row_not_finite(row)) continue;
 #pragma unroll
                 for (int x = 0; x < 16; ++x) add_not_finite(o[x >> 2], 4 * (x & 3), row, 8 * x + 4 * hh, tile * kKT + k <= sees_to);
@@ -1095,6 +1146,7 @@ constexpr int kManyPieces = 222;   // a workgroup per CU, less what the longest 
 constexpr int kMostSplitHeads = 128;  // (more heads than that fill the chip without dividing keys)
 constexpr int kFewPlaces = 2 * (kFewPieces + kMostSplitHeads), kManyPlaces = 4 * (kManyPieces + kMostSplitHeads);
 constexpr size_t kPartialBytes = (size_t)(kFewPlaces * 32 > kManyPlaces * 64 ? kFewPlaces * 32 : kManyPlaces * 64) * kPartRow * 4;
+constexpr size_t kPlanBytes = ((size_t)JUP_PAGED_MAX_SEQS + 2) * 8;
 static_assert(kFewPlaces * 4 <= kCountBytes && kManyPlaces * 4 <= kCountBytes);
 
 template <class K>
@@ -1108,7 +1160,7 @@ hipError_t with_lds(K* kernel, int bytes, bool* done) {  // once per device: a k
 }
 
 // tiles: at most so many tiles of rows per key/value head
-template <class K>
+template <int R, class K>
 hipError_t launch(K* kernel, int threads, int lds, bool* done, Attention a, long long tiles, int pieces, int places, int least, hipStream_t s) {
     hipError_t e = with_lds(kernel, lds, done);
     if (e != hipSuccess) return e;
@@ -1117,6 +1169,7 @@ hipError_t launch(K* kernel, int threads, int lds, bool* done, Attention a, long
     a.most_places = places / a.n_kv_heads;
     const long long grid = (tiles + 2 * pieces) * a.n_kv_heads;
     if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (a.plan) hipLaunchKernelGGL(plan_work<R>, dim3(1), dim3(1024), 0, s, a, least, (int2*)a.plan);
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), lds, s, a, least);
     return hipGetLastError();
 }
@@ -1140,28 +1193,28 @@ hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_
     a.group.set(c.n_heads / pool.n_kv_heads);
     a.scale_log2e = c.scale * 1.4426950408889634f;
     a.count = (int*)c.workspace;
-    a.partial = (float*)((char*)c.workspace + kCountBytes);
+    a.plan = c.n_seqs > 64 ? (const int2*)((char*)c.workspace + kCountBytes) : nullptr;
+    a.partial = (float*)((char*)c.workspace + kCountBytes + kPlanBytes);
     a.least_rows = 0; a.most_rows = INT32_MAX;
     const long long rows = (long long)c.n_rows * a.group.d, most = (long long)c.max_new * a.group.d;
     static bool done16[64], done32[64], done16w[64], done32w[64], done_many[64];
     auto few = [&](Attention x, long long tiles16, long long tiles32) {
         const long long tiles = most <= 16 ? tiles16 : tiles32;
         if (tiles * pool.n_kv_heads <= 256)  // a workgroup per CU at most: of eight waves, and pieces for three CUs in four
-            return most <= 16 ? launch(attention_few<16, 8>, 512, Few<16, 8>::kLds, done16w, x, tiles, kWidePieces, kFewPlaces, kLeast16, s)
-                              : launch(attention_few<32, 8>, 512, Few<32, 8>::kLds, done32w, x, tiles, kWidePieces, kFewPlaces, kLeast16, s);
-        return most <= 16 ? launch(attention_few<16, 4>, 256, Few<16, 4>::kLds, done16, x, tiles, kFewPieces, kFewPlaces, kLeast16, s)
-                          : launch(attention_few<32, 4>, 256, Few<32, 4>::kLds, done32, x, tiles, kFewPieces, kFewPlaces, kLeast32, s);
+            return most <= 16 ? launch<16>(attention_few<16, 8>, 512, Few<16, 8>::kLds, done16w, x, tiles, kWidePieces, kFewPlaces, kLeast16, s)
+                              : launch<32>(attention_few<32, 8>, 512, Few<32, 8>::kLds, done32w, x, tiles, kWidePieces, kFewPlaces, kLeast16, s);
+        return most <= 16 ? launch<16>(attention_few<16, 4>, 256, Few<16, 4>::kLds, done16, x, tiles, kFewPieces, kFewPlaces, kLeast16, s)
+                          : launch<32>(attention_few<32, 4>, 256, Few<32, 4>::kLds, done32, x, tiles, kFewPieces, kFewPlaces, kLeast32, s);
     };
     if (most <= kFewRows) return few(a, rows / 16 + c.n_seqs, rows / 32 + c.n_seqs);
     Attention longer = a;
-    // A few requests go to attention_many whatever their rows: a launch of attention_few for none of them costs as much as it saves.
-    const bool all = c.n_seqs <= 4;
+    const bool all = c.n_seqs == 1;
     longer.least_rows = all ? 0 : kFewRows + 1;
     static bool done2[64], done4[64];
         const long long groups = (rows / 256 + c.n_seqs) * pool.n_kv_heads;
-    hipError_t e = groups >= 384   ? launch(attention_many<8, 1, 2, 2, 2, 2>, 512, Many<8, 1, 2, 2, 2>::kLds, done_many, longer, rows / 256 + c.n_seqs, 0, 0, 8, s)
-                   : groups >= 112 ? launch(attention_many<8, 2, 2, 1, 2, 2>, 512, Many<8, 2, 2, 1, 2>::kLds, done2, longer, rows / 128 + c.n_seqs, 0, 0, 8, s)
-                                   : launch(attention_many<8, 4, 1, 1, 2, 2>, 512, Many<8, 4, 1, 1, 2>::kLds, done4, longer, rows / 64 + c.n_seqs, kManyPieces, kManyPlaces, kLeastMany, s);
+    hipError_t e = groups >= 384   ? launch<256>(attention_many<8, 1, 2, 2, 2, 2>, 512, Many<8, 1, 2, 2, 2>::kLds, done_many, longer, rows / 256 + c.n_seqs, 0, 0, 8, s)
+                   : groups >= 112 ? launch<128>(attention_many<8, 2, 2, 1, 2, 2>, 512, Many<8, 2, 2, 1, 2>::kLds, done2, longer, rows / 128 + c.n_seqs, 0, 0, 8, s)
+                                   : launch<64>(attention_many<8, 4, 1, 1, 2, 2>, 512, Many<8, 4, 1, 1, 2>::kLds, done4, longer, rows / 64 + c.n_seqs, kManyPieces, kManyPlaces, kLeastMany, s);
     if (e != hipSuccess || all) return e;
     a.most_rows = kFewRows;
     const long long tiles = (long long)c.n_seqs * (kFewRows / 32);
@@ -1171,5 +1224,5 @@ hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_
 }  // namespace jup
 
 extern "C" size_t jup_paged_workspace_bytes(void) {
-    return jup::kCountBytes + (jup::kPartialBytes > jup::kVerifyBytes ? jup::kPartialBytes : jup::kVerifyBytes);
+    return jup::kCountBytes + (jup::kPlanBytes + jup::kPartialBytes > jup::kVerifyBytes ? jup::kPlanBytes + jup::kPartialBytes : jup::kVerifyBytes);
 }
