@@ -105,10 +105,13 @@ JUP_API jup_status_t jup_paged_append(const jup_paged_pool_t *pool, const jup_pa
  * A position whose table entry is outside [0, n_blocks), or that lies behind table_width pages, is not there; a row that
  * sees no position gets zeros.  Values of positions a row does not see do not reach it, whatever they are.  Rows of q and
  * out outside [row_start[0], row_start[n_seqs]) are neither read nor written.
+ *   out             may be q, with its strides
  *   n_rows          rows of q and out; max_new: the longest m expected.  It chooses between kernels and decides nothing
  *                   else: results are right whatever it says.
  *   workspace       >= jup_paged_workspace_bytes(...) bytes, 256-byte aligned, ZERO when first used; every call leaves it
- *                   ready for the next.  Calls that share one must not overlap in time (captured graphs included).  Not needed in check mode.
+ *                   ready for the next.  Calls that share one must not overlap in time (captured
+ *                   graphs included).  Not needed in check mode
+ *   scale           positive, at most 1e38
  * Results do not depend on what the pages' order in the pool is, nor on the run; they do depend, in the last bits of fp32
  * sums, on how the keys are divided among workgroups, which follows from all requests of the call.
  * Errors: JUP_EINVAL, JUP_EDEVICE.

@@ -56,7 +56,7 @@ jup_status_t check_attention(const char* me, const jup_paged_pool_t* pool, const
     if (a->table_width < 0 || (int64_t)a->table_width * pool->page_size > INT32_MAX - 255)
         return set_error(JUP_EINVAL, "%s: table_width=%d is negative, or table_width * page_size exceeds 2^31 - 256", me, a->table_width);
     if (a->table_stride < a->table_width) return set_error(JUP_EINVAL, "%s: table_stride is shorter than table_width", me);
-    if (!(a->scale > 0.0f) || a->scale > 3e38f) return set_error(JUP_EINVAL, "%s: scale must be positive and finite", me);
+    if (!(a->scale > 0.0f) || a->scale > 1e38f) return set_error(JUP_EINVAL, "%s: scale must be positive and at most 1e38", me);
     if (a->n_rows == 0 || a->n_seqs == 0) return JUP_OK;
     if (!a->q || !a->out || !a->row_start || !a->lengths || (a->table_width > 0 && !a->table))
         return set_error(JUP_EINVAL, "%s: the rows, row_start, lengths and table must not be NULL", me);

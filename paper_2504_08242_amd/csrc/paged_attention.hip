@@ -34,7 +34,7 @@ struct Attention {
     int* count;                                   // arrival counters of rows whose keys are divided, zero between launches
     float* partial;                               // [slot][kv head][row of the tile][kPartRow]
     float chunk_factor;                           // 1 / pieces of work per key/value head that fill the chip (find_work); large: keys are not divided
-    int most_places;                              // of the scratch, per key/value head
+    int most_items, most_places;                  // pieces of the grid and places of the scratch, per key/value head
     int least_rows, most_rows;                    // requests with so many rows (tokens x G) are this launch's
 };
 // The arguments, read from memory where they are used: behind a main loop that needs the scalar registers itself.
@@ -168,6 +168,7 @@ constexpr int kOrdered = 16;  // requests that are put in order of their lengths
 template <int R>
 __device__ bool find_work(const Attention& a, int item, int least, Work& w) {
     const int lane = threadIdx.x & 63;
+    const int at_item = item;
     int seq, chunk, slots_before;
     Request<R> r;
     if (!a.plan) {  // a lane per request
@@ -216,7 +217,8 @@ __device__ bool find_work(const Attention& a, int item, int least, Work& w) {
     }
     const int most = r.pieces(chunk);
     const int nth = (unsigned)item / (unsigned)max(most, 1);
-    // (sums of requests that overlap in a row_start that makes no sense can wrap)
+    // (requests that overlap in a row_start that makes no sense: sums can wrap, and a tile whose pieces are not all in the grid is left
+    // out, so that its counter stays 0)
     if (item < 0 || nth >= r.tiles || slots_before < 0 || (most > 1 && slots_before + nth * most > a.most_places - most)) return false;
     w.seq = seq;
     w.begin = r.begin;
@@ -229,7 +231,7 @@ __device__ bool find_work(const Attention& a, int item, int least, Work& w) {
     w.keys = r.keys_of(a, last_token);
     const int key_tiles = (w.keys + kKT - 1) / kKT;
     w.pieces = pieces_of(key_tiles, chunk);
-    if (w.piece >= w.pieces) return false;  // (an earlier tile of a prompt: fewer keys than the last one)
+    if (w.piece >= w.pieces || at_item - w.piece + w.pieces > a.most_items) return false;  // (an earlier tile of a prompt: fewer keys than the last one)
     const int even = (unsigned)key_tiles / (unsigned)w.pieces, over = key_tiles - even * w.pieces;
     w.tile_lo = w.piece * even + min(w.piece, over);
     w.tile_hi = w.tile_lo + even + (w.piece < over);
@@ -1167,8 +1169,9 @@ hipError_t launch(K* kernel, int threads, int lds, bool* done, Attention a, long
     pieces = a.n_kv_heads > kMostSplitHeads || pieces == 0 ? 0 : (pieces + a.n_kv_heads - 1) / a.n_kv_heads;
     a.chunk_factor = pieces > 0 ? 1.0001f / pieces : 1e30f;
     a.most_places = places / a.n_kv_heads;
-    const long long grid = (tiles + 2 * pieces) * a.n_kv_heads;
+    const long long items = tiles + 2 * pieces, grid = items * a.n_kv_heads;
     if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
+    a.most_items = (int)items;
     if (a.plan) hipLaunchKernelGGL(plan_work<R>, dim3(1), dim3(1024), 0, s, a, least, (int2*)a.plan);
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), lds, s, a, least);
     return hipGetLastError();

@@ -217,7 +217,8 @@ __global__ __launch_bounds__(kThreads) void verify(const jup_verify_drafts_t a, 
         }
         run += s.sum[k];
     }
-    if (at >= 0) next = search(w, min(at * length, a.vocab), min((at + 1) * length, a.vocab), before, border, s);
+    // (beyond the slice, should its sum in this order fall short of the border by a rounding)
+    if (at >= 0) next = search(w, min(at * length, a.vocab), a.vocab, before, border, s);
     if (next < 0) {  // hardly ever, and this workgroup alone: u leaves no token (or rounding does), or there is none
         next = last_weight(w, a.vocab, s);
         if (next < 0 && row < end - 1) {  // a rejected row whose weights are all 0: the target itself

@@ -18,6 +18,7 @@ current one of the tensors' device) and read nothing back.  ``ValueError`` for t
 import collections
 import ctypes
 import math
+import struct
 
 import torch
 
@@ -69,10 +70,15 @@ _FORMATS = {_i32: "i", _i64: "q", _vp: "P", _f32: "f", _sz: "N"}
 
 
 def _packer(struct_type):
-    import struct
     packer = struct.Struct("@" + "".join(_FORMATS[t] for _, t in struct_type._fields_) + "0q")
     assert packer.size == ctypes.sizeof(struct_type), struct_type
-    return packer.pack
+
+    def pack(*values):
+        try:
+            return packer.pack(*values)
+        except (struct.error, OverflowError) as e:
+            raise ValueError(f"a number is too large for the field it goes into: {e}") from None
+    return pack
 
 
 _pack_pool, _pack_extend, _pack_append, _pack_attention, _pack_verify = map(_packer, (_Pool, _Extend, _Append, _Attention, _Verify))
@@ -183,13 +189,17 @@ class Workspace:
 
     def __init__(self, device="cuda:0"):
         self.buf = torch.zeros(_lib().jup_paged_workspace_bytes(), dtype=torch.uint8, device=device)
+        if not torch.cuda.is_current_stream_capturing():   # (the first call may be on another stream)
+            torch.cuda.current_stream(self.buf.device).synchronize()
         self.args = self.buf.data_ptr(), self.buf.numel()
         self.at = self.buf.get_device()
 
 
-def _scratch(workspace, at):
+def _scratch(workspace, at, stream):
     if not isinstance(workspace, Workspace) or workspace.at != at:
         raise ValueError(f"workspace must be a Workspace on cuda:{at}")
+    if stream is not None:
+        workspace.buf.record_stream(stream)
     return workspace.args
 
 
@@ -267,7 +277,7 @@ def attention(q, k_pool, v_pool, table, row_start, lengths, max_new, workspace=N
           _pack_attention(n, rows, heads, int(max_new), width, stride, q_at, out_at, *q_strides, *out_strides,
                           _ints("row_start", row_start, at, n + 1), _ints("lengths", lengths, at, n), tables,
                           1.0 / math.sqrt(dim) if scale is None else scale,
-                          *(_scratch(workspace, at) if workspace is not None or dtype is not _F32 else (0, 0))))
+                          *(_scratch(workspace, at, stream) if workspace is not None or dtype is not _F32 else (0, 0))))
     return out
 
 
@@ -291,7 +301,7 @@ def prefill(stage, hidden_in, step, k_pools, v_pools, table, max_new, workspace=
     if step.positions.numel() < rows or step.slots.numel() < rows:
         raise ValueError(f"the step has positions of {step.positions.numel()} rows, hidden_in {rows}")
     tables, table_width, stride = _table(table, at, n)
-    scratch = _scratch(workspace, at) if workspace is not None or dtype is not _F32 else (0, 0)
+    scratch = _scratch(workspace, at, stream) if workspace is not None or dtype is not _F32 else (0, 0)
     batch = _Batch(_Pool.from_buffer_copy(packed), k_pools.stride(0), n, int(max_new), table_width, stride, _ints("row_start", step.row_start, at, n + 1),
                    _ints("lengths", step.lengths, at, n), tables, _ints("positions", step.positions, at, step.positions.numel()),
                    _ints("slots", step.slots, at, step.slots.numel()), *scratch)
@@ -341,5 +351,5 @@ def verify(tokens, target_probs, row_start, u_accept, u_sample, workspace, draft
     _call(_lib().jup_verify_drafts, at, stream, made,
           _pack_verify(n, rows, vocab, _DTYPES[dtype], _ints("tokens", tokens, at, rows), _ints("row_start", row_start, at, n + 1), target,
                        draft, target_stride, draft_stride, _uniforms("u_accept", u_accept, at, rows), _uniforms("u_sample", u_sample, at, n),
-                       base, base + 4 * n, base + 8 * n, lengths_at, after_at, *_scratch(workspace, at)))
+                       base, base + 4 * n, base + 8 * n, lengths_at, after_at, *_scratch(workspace, at, stream)))
     return Verdict(n_accepted, next_token, emitted, new_lengths)

@@ -183,6 +183,18 @@ def test_the_front_end_refuses_tensors_that_do_not_fit_on_the_gpu(workspace):
         assert e.value.status == jb.JUP_EINVAL
 
 
+@gpu
+def test_numbers_too_large_for_their_fields_are_refused(workspace):
+    k = torch.zeros((5, 2, 16, 128), dtype=torch.bfloat16, device=DEV)
+    q, i = torch.zeros((3, 2, 128), dtype=torch.bfloat16, device=DEV), ints([0, 1, 2])
+    table, at = torch.zeros((3, 2), dtype=torch.int32, device=DEV), ints([0, 1, 2, 3])
+    for bad in (lambda: jp.attention(q, k, k, table, at, i, 2 ** 31, workspace), lambda: jp.attention(q, k, k, table, at, i, 1, workspace, scale=1e300),
+                lambda: jp.attention(q, k, k, table, at, i, 1, workspace, scale=3e38), lambda: jp.append(q, q, i, k, k, positions=i, rope_theta=1e300),
+                lambda: jp.extend(i, i, i, table, i, i[:1], 2 ** 40, 4)):
+        with pytest.raises((ValueError, jb.JupiterError)):
+            bad()
+
+
 # ---- tables -----------------------------------------------------------------------------------------------------------------
 
 
@@ -416,6 +428,151 @@ def test_attention_over_pages(workspace, dtype, heads, kv_heads, page, requests)
     assert torch.equal(got, b.run(workspace))
 
 
+MANY_HEADS = [
+    # enough key/value heads that tiles of 128 (60 heads) or 256 rows (150) fill the GPU; more than 128: keys are not divided
+    (60, 60, 16, [(100, 70), (0, 150), (33, 40), (700, 1)]),
+    (120, 60, 32, [(10, 129), (333, 17), (64, 0)]),
+    (150, 150, 16, [(30, 70), (0, 41), (257, 2)]),
+    (300, 150, 64, [(5, 140), (0, 33), (63, 1)]),
+    (200, 200, 16, [(900, 1), (31, 4)]),
+    (160, 160, 8, [(70, 30)]),
+]
+
+
+@gpu
+@pytest.mark.parametrize("heads,kv_heads,page,requests", MANY_HEADS)
+def test_attention_of_many_heads(workspace, heads, kv_heads, page, requests):
+    b = Batch(torch.bfloat16, heads, kv_heads, page, requests)
+    b.check(b.run(workspace))
+    b.check(b.run(workspace, max_new=1))
+
+
+@gpu
+@pytest.mark.parametrize("heads", [60, 150])
+def test_holes_and_unseen_values_with_many_heads(workspace, heads):
+    requests = [(100, 90), (0, 50)]
+    b = Batch(torch.bfloat16, heads, heads, 16, requests)
+    t = b.table.copy()
+    t[0, [0, 5, 6]] = [-1, b.k.shape[0], 2 ** 31 - 1]
+    t[1, 0] = -5
+    got = b.run(workspace, table=t)
+    b.check(got, table=t)
+    assert (got[90:106] == 0).all()
+    want = b.run(workspace)
+    for bad in (float("nan"), float("inf")):
+        c = Batch(torch.bfloat16, heads, heads, 16, requests)
+        pos = 100 + 60
+        c.k[int(c.table[0, pos // 16]), :, pos % 16, 5] = bad
+        c.v[int(c.table[0, pos // 16]), :, pos % 16, 7] = bad
+        got = c.run(workspace)
+        assert torch.equal(got[:60], want[:60]) and torch.equal(got[90:], want[90:])
+        assert not torch.isfinite(got[60:90, :, 7]).any()
+
+
+def many_requests(n, most_cached, most_new, seed):
+    rng = np.random.default_rng(seed)
+    requests = [(int(rng.integers(0, most_cached + 1)), int(rng.integers(0, most_new + 1))) for _ in range(n)]
+    requests[n // 3] = (3000, 2)       # one long cache among them
+    requests[-1] = (5, 1)
+    return requests
+
+
+@gpu
+@pytest.mark.parametrize("n,most_cached,most_new,heads,kv_heads", [
+    (64, 100, 3, 4, 2), (65, 100, 3, 4, 2), (200, 300, 1, 2, 2), (1000, 40, 2, 2, 1), (1025, 20, 1, 16, 1), (4097, 12, 1, 1, 1), (16384, 3, 1, 1, 1),
+    (70, 60, 40, 4, 1), (130, 200, 17, 8, 2),
+])
+def test_attention_of_many_requests(workspace, n, most_cached, most_new, heads, kv_heads):
+    b = Batch(torch.bfloat16, heads, kv_heads, 16, many_requests(n, most_cached, most_new, n))
+    got = b.run(workspace)
+    b.check(got)
+    b.check(b.run(workspace, max_new=100))
+    assert torch.equal(got, b.run(workspace))
+
+
+@gpu
+@pytest.mark.parametrize("n", [70, 3000])
+def test_many_requests_without_tokens(workspace, n):
+    b = Batch(torch.bfloat16, 2, 2, 16, [(20, 0)] * (n - 1) + [(30, 2)])
+    b.check(b.run(workspace))
+    b = Batch(torch.bfloat16, 2, 2, 16, [(20, 0)] * n, pad_rows=1)
+    out = torch.full_like(b.q, 3.0)
+    b.run(workspace, out=out)
+    assert (out == 3.0).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("heads,kv_heads,requests", [(4, 2, [(500, 3), (2000, 1)]), (4, 4, [(0, 300), (1700, 70)]), (60, 60, [(0, 150)]), (150, 150, [(9, 70)])])
+def test_results_in_place_of_the_queries(workspace, dtype, heads, kv_heads, requests):
+    b = Batch(dtype, heads, kv_heads, 16, requests)
+    want, q = b.run(workspace), b.q.clone()
+    assert b.run(workspace, out=b.q) is b.q
+    assert torch.equal(b.q, want) and not torch.equal(b.q, q)
+
+
+@gpu
+@pytest.mark.parametrize("new", [2, 60])
+def test_pages_of_several_requests(workspace, new):
+    """Branches that share a prefix name the same pages; a page may even be named twice in a row."""
+    b = Batch(torch.bfloat16, 4, 2, 16, [(160 + 5, new), (160 + 9, new), (160, new)])
+    b.table[1:, :10] = b.table[0, :10]
+    b.table[2, 3] = b.table[2, 4]
+    b.check(b.run(workspace))
+
+
+@gpu
+def test_rows_of_requests_that_overlap_spoil_no_later_call():
+    """A row_start that makes no sense: more pieces of work than a launch has room for.  Later calls on the workspace are right."""
+    workspace = jp.Workspace(DEV)
+    b = Batch(torch.bfloat16, 4, 2, 16, [(4000, 1), (50, 2), (3000, 1)])
+    want = b.run(workspace)
+    n = 60
+    table = torch.from_numpy(np.repeat(b.table[:1], n, 0)).to(DEV, torch.int32)
+    for ends in ([0, 4], [4, 0], [0, 1]):
+        row_start = ints((ends * n)[:n + 1])
+        for expected in (1, 100):
+            jp.attention(b.q, b.k, b.v, table, row_start, ints([4001] * n), expected, workspace)
+    assert torch.equal(b.run(workspace), want)
+
+
+@gpu
+def test_a_workspace_made_behind_work_and_used_on_another_stream():
+    b = Batch(torch.bfloat16, 4, 2, 16, [(4000, 1), (300, 3)])
+    want = b.run(jp.Workspace(DEV))
+    dirt = torch.full_like(jp.Workspace(DEV).buf, 1)
+    torch.cuda.synchronize()
+    del dirt                                 # (the next workspace may get this memory)
+    x = torch.randn((4096, 4096), device=DEV)
+    for _ in range(20):
+        x = x @ x * 1e-2
+    side = torch.cuda.Stream()
+    got = b.run(jp.Workspace(DEV), stream=side)
+    side.synchronize()
+    assert torch.equal(got, want)
+
+
+@gpu
+def test_two_graphs_share_a_workspace(workspace):
+    """Replayed one after the other, with eager calls on the same workspace between them."""
+    batches = [Batch(torch.bfloat16, 4, 2, 16, r) for r in ([(3000, 1), (700, 4)], [(2500, 40), (100, 90)], many_requests(100, 60, 2, 1))]
+    want = [b.run(workspace) for b in batches]
+    graphs, outs = [], []
+    for b in batches:
+        args = b.q, b.k, b.v, torch.from_numpy(b.table).to(DEV, torch.int32), ints(b.row_start), ints(b.lengths), max(b.new), workspace
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = jp.attention(*args)
+        graphs.append((graph, args))
+        outs.append(out)
+    for _ in range(4):
+        for (graph, _), out, w, b in zip(graphs, outs, want, batches):
+            out.zero_()
+            graph.replay()
+            assert torch.equal(out, w)
+            assert torch.equal(b.run(workspace), w)
+
+
 @gpu
 @pytest.mark.parametrize("order", ORDERS)
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
@@ -624,6 +781,14 @@ def test_verification(workspace, n, most, vocab, dtype, from_draft):
         most = 2
     want = check_verify(workspace, *make_verify(n, most, vocab, dtype, from_draft, n * vocab + most))
     assert len(want[0]) == n
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [524288, 700001])
+def test_verification_of_a_very_large_vocabulary(workspace, dtype, vocab):
+    """Slices of more than one round each."""
+    check_verify(workspace, *make_verify(2, 1, vocab, dtype, True, vocab))
 
 
 @gpu
