@@ -107,7 +107,7 @@ def _lib():
 Step = collections.namedtuple("Step", "row_start positions slots lengths owned free_count status")
 Verdict = collections.namedtuple("Verdict", "n_accepted next_token emitted lengths")
 
-_F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
+_F32, _BF16, _I32, _CONTIGUOUS = torch.float32, torch.bfloat16, torch.int32, torch.contiguous_format
 _DTYPES = {_F32: jb.JUP_F32, _BF16: jb.JUP_BF16}
 
 
@@ -162,7 +162,7 @@ def _pool(k_pool, v_pool):
             dtype, at, heads, dim)
 
 
-_current_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
+_current_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice  # (the tensors are on the GPU: it is initialised)
 
 
 def _call(fn, at, stream, made, *structs):
@@ -217,8 +217,8 @@ def extend(lengths, n_new, owned, table, free_blocks, free_count, page_size, max
     tables, width, stride = _table(table, at, n)
     free = (_ints("free_blocks", free_blocks, at, n_free), _ints("free_count", free_count, at, 1))
     sizes = [n + 1, max_rows, max_rows, 1] if in_place else [n + 1, max_rows, max_rows, 1, n, n, 1]
-    made = torch.empty(sum(sizes), dtype=_I32, device=lengths.device)
-    row_start, positions, slots, status, *new = made.split(sizes)
+    made = lengths.new_empty(sum(sizes))
+    row_start, positions, slots, status, *new = made.split_with_sizes(sizes)
     new_lengths, new_owned, new_count = (lengths, owned, free_count) if in_place else new
     base = made.data_ptr()
     ends = base + 4 * (n + 1), base + 4 * (n + 1 + max_rows), base + 4 * (n + 1 + 2 * max_rows)
@@ -249,8 +249,10 @@ def append(k, v, slots, k_pool, v_pool, positions=None, rope_theta=None, q=None,
         heads = q.shape[1] if q.dim() == 3 else -1
         q_at, *q_strides = _heads("q", q, dtype, at, rows, heads, dim)
         if q_out is None:
-            q_out = made = torch.empty(q.shape, dtype=dtype, device=q.device)
-        out_at, *out_strides = _heads("q_out", q_out, dtype, at, rows, heads, dim, written=True)
+            q_out = made = torch.empty_like(q, memory_format=_CONTIGUOUS)
+            out_at, out_strides = made.data_ptr(), (heads * dim, dim)
+        else:
+            out_at, *out_strides = _heads("q_out", q_out, dtype, at, rows, heads, dim, written=True)
     elif q_out is not None:
         raise ValueError("q_out goes with q")
     _call(_lib().jup_paged_append, at, stream, made, pool,
@@ -270,8 +272,10 @@ def attention(q, k_pool, v_pool, table, row_start, lengths, max_new, workspace=N
     q_at, *q_strides = _heads("q", q, dtype, at, rows, heads, dim)
     made = None
     if out is None:
-        out = made = torch.empty(q.shape, dtype=dtype, device=q.device)
-    out_at, *out_strides = _heads("out", out, dtype, at, rows, heads, dim, written=True)
+        out = made = torch.empty_like(q, memory_format=_CONTIGUOUS)
+        out_at, out_strides = made.data_ptr(), (heads * dim, dim)
+    else:
+        out_at, *out_strides = _heads("out", out, dtype, at, rows, heads, dim, written=True)
     tables, width, stride = _table(table, at, n)
     _call(_lib().jup_paged_attention, at, stream, made, pool,
           _pack_attention(n, rows, heads, int(max_new), width, stride, q_at, out_at, *q_strides, *out_strides,
@@ -338,8 +342,8 @@ def verify(tokens, target_probs, row_start, u_accept, u_sample, workspace, draft
     target, target_stride = _probs("target_probs", target_probs, dtype, at, rows, vocab)
     draft, draft_stride = (0, 0) if draft_probs is None else _probs("draft_probs", draft_probs, dtype, at, rows, vocab)
     sizes = [n, n, rows] if lengths is None or in_place else [n, n, rows, n]
-    made = torch.empty(sum(sizes), dtype=_I32, device=row_start.device)
-    n_accepted, next_token, emitted, *new = made.split(sizes)
+    made = tokens.new_empty(sum(sizes))
+    n_accepted, next_token, emitted, *new = made.split_with_sizes(sizes)
     base = made.data_ptr()
     lengths_at = after_at = 0
     new_lengths = None
