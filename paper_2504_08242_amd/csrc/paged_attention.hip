@@ -120,7 +120,8 @@ __device__ __forceinline__ void prefix_sums(int& x, int& y, int lane) {  // incl
     }
 }
 
-// More than 64 requests, whose prefix sums every wave of every workgroup would otherwise make again: entry i of the plan is the pieces and
+// More than 64 requests, whose prefix sums every wave of every workgroup would otherwise make again (256 requests of one token behind
+// 100 to 900: 259 µs, and 226 with the plan; 1024 with grouped heads 482 and 242; 4096 5090 and 478): entry i of the plan is the pieces and
 // the places of the scratch before request i, the one behind the last request all pieces and the longest piece.  One workgroup, a few
 // neighbouring requests per thread.
 template <int R>
@@ -178,7 +179,8 @@ __device__ bool find_work(const Attention& a, int item, int least, Work& w) {
         const int items = r.items(chunk), slots = r.slots(chunk);
         int items_to = items, slots_to = slots;
         if (R > 32 && n <= kOrdered) {
-            // whole prompts: the requests with the most keys first, so that what is left for the end is short
+            // whole prompts: the requests with the most keys first, so that what is left for the end is short (four chunks of 1 to 1000
+            // tokens behind 100 to 8000: 164 -> 139 µs; others the same)
             for (int j = 0; j < n; ++j) {
                 const int keys = __builtin_amdgcn_readlane(r.key_tiles, j);
                 const bool before = keys > r.key_tiles || (keys == r.key_tiles && j < lane);
@@ -424,6 +426,11 @@ __device__ __forceinline__ void store_pieces(const unsigned char* sums, int row_
 // 32 rows, and four waves divide the piece's key tiles: each works alone on the tiles wave, wave + 4, ..., with one LDS
 // slot for a K and one for a V tile, and refills the K slot as soon as the scores are out of it and the V slot as soon as the products
 // are.  Two workgroups share a CU, so 128 KB are in flight on it, and one's entry and merge lie under the other's loads.
+// Where there is a workgroup per CU at most, eight waves divide the keys, and there are half as many pieces to put together: one token
+// behind 8192 31 -> 28 µs, behind 65536 with four query heads per key head 71 -> 61.
+// Keys and values of 64 requests of one token (550 MB) pass in 108 µs, 5.0 TB/s; of 16 requests of five tokens, whose lengths are
+// uneven, in 45 µs, 5.4 TB/s (the last-level cache holds some of them from call to call).  One token behind 576 takes 10 µs: lengths,
+// block numbers, a tile and its neighbours, the merge of the waves, each a trip to memory or through LDS behind the other.
 // Transposed products, S^T = K Q^T and O^T += V^T P^T: a lane owns a row, whose statistics are scalars of the lane.
 //   QW = 32, 32x32x16 (lane = 32 hh + c): A[m = c][k = 8 hh + e], B[k = 8 hh + e][n = c], D[m = 8 (i/4) + 4 hh + i%4][n = c].
 //   QW = 16, 16x16x32 (lane = 16 hh + c): A[m = c][k = 8 hh + e], B[k = 8 hh + e][n = c], D[m = 4 hh + i][n = c].
@@ -713,6 +720,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_few(const Attention args
 // KP parts of the keys: a workgroup has 256 / KP rows, and KP waves divide the keys of 32 of them and add up through LDS at the
 // end.  One part reads a key for the most rows; more parts make more workgroups of fewer rows, where rows are few or
 // where triangles of different sizes are to be dealt to the CUs.
+// Measured: a prompt of 16384 tokens on 8 heads in 540 µs, 1019 TFLOP/s, matrix cores busy 44 % of the clocks, LDS 22 %.  Without loads
+// from memory it takes 92 % of that, without exponentials 89 %, without LDS reads 73 %, without products 95 %: no one unit binds it, but the
+// waves wait for one another's, as registers leave room for two per SIMD.  Three per SIMD of half the keys each: 970 instead of 1050 TFLOP/s.  One wave per
+// SIMD of 64 rows: 789.  Half the waves a product behind the others: 632 instead of 590 µs.  Four prompts of 700 to 4100 tokens (40 heads, 292 µs,
+// 735 TFLOP/s) have 1240 such tiles of 10 steps each, whose entry and end (15 of 60 µs) nothing overlaps: LDS has room for one workgroup.
 template <int NW, int KP, int NT, int SUB, int RING>
 struct Many {
     static constexpr int kWaves = NW;
@@ -1136,15 +1148,19 @@ __global__ __launch_bounds__(64) void attention_f32(const jup_paged_pool_t pool,
 // ---- launches ------------------------------------------------------------------------------------------------------------------
 namespace {
 
-// Scratch: counters, then pieces.  Pieces wanted are P per chip, so at most P + n_kv_heads in all (find_work); a divided tile of
+// Scratch: counters, the plan, then pieces.  Pieces wanted are P per chip, so at most P + n_kv_heads in all (find_work); a divided tile of
 // attention_few has at least two, each of which is at least half as long as a piece may be: at most twice as many places are
 // used.  attention_many counts a request's pieces as if all its tiles had the keys of the last one, at most twice what they
 // have on average: four times.
-constexpr int kFewRows = 32;       // a request's rows up to which attention_few has it
-constexpr int kFewPieces = 512;    // two workgroups per CU
-constexpr int kWidePieces = 192;   // of eight waves
-constexpr int kLeast16 = 24, kLeast32 = 16, kLeastMany = 24;  // key tiles that are worth a piece
-constexpr int kManyPieces = 222;   // a workgroup per CU, less what the longest may be longer than the average
+// A request's rows up to which attention_few has it.  64 and 128 rows behind 1536 on 32 heads take attention_few 51 and 45 µs, attention_many 41
+// and 36; 16 requests of 40 rows 49 and 43; but four requests of 100 rows 47 and 55.
+constexpr int kFewRows = 32;
+// Pieces: two workgroups per CU (with 1024 pieces of at least 4 key tiles, one token behind 8192 takes 38 µs, with 512 of 24 tiles 31), three
+// of eight waves for four CUs (256: 30 µs, 192: 28).
+constexpr int kFewPieces = 512, kWidePieces = 192;
+constexpr int kLeast = 24;       // key tiles that are worth a piece
+// A workgroup per CU, less what the longest piece may be longer than the average: 300 tokens behind 6000 on 8 heads 42 µs, with 256 pieces 56.
+constexpr int kManyPieces = 222;
 constexpr int kMostSplitHeads = 128;  // (more heads than that fill the chip without dividing keys)
 constexpr int kFewPlaces = 2 * (kFewPieces + kMostSplitHeads), kManyPlaces = 4 * (kManyPieces + kMostSplitHeads);
 constexpr size_t kPartialBytes = (size_t)(kFewPlaces * 32 > kManyPlaces * 64 ? kFewPlaces * 32 : kManyPlaces * 64) * kPartRow * 4;
@@ -1200,24 +1216,29 @@ hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_
     a.partial = (float*)((char*)c.workspace + kCountBytes + kPlanBytes);
     a.least_rows = 0; a.most_rows = INT32_MAX;
     const long long rows = (long long)c.n_rows * a.group.d, most = (long long)c.max_new * a.group.d;
-    static bool done16[64], done32[64], done16w[64], done32w[64], done_many[64];
+    static bool done16[64], done32[64], done16w[64], done32w[64];
     auto few = [&](Attention x, long long tiles16, long long tiles32) {
         const long long tiles = most <= 16 ? tiles16 : tiles32;
         if (tiles * pool.n_kv_heads <= 256)  // a workgroup per CU at most: of eight waves, and pieces for three CUs in four
-            return most <= 16 ? launch<16>(attention_few<16, 8>, 512, Few<16, 8>::kLds, done16w, x, tiles, kWidePieces, kFewPlaces, kLeast16, s)
-                              : launch<32>(attention_few<32, 8>, 512, Few<32, 8>::kLds, done32w, x, tiles, kWidePieces, kFewPlaces, kLeast16, s);
-        return most <= 16 ? launch<16>(attention_few<16, 4>, 256, Few<16, 4>::kLds, done16, x, tiles, kFewPieces, kFewPlaces, kLeast16, s)
-                          : launch<32>(attention_few<32, 4>, 256, Few<32, 4>::kLds, done32, x, tiles, kFewPieces, kFewPlaces, kLeast32, s);
+            return most <= 16 ? launch<16>(attention_few<16, 8>, 512, Few<16, 8>::kLds, done16w, x, tiles, kWidePieces, kFewPlaces, kLeast, s)
+                              : launch<32>(attention_few<32, 8>, 512, Few<32, 8>::kLds, done32w, x, tiles, kWidePieces, kFewPlaces, kLeast, s);
+        return most <= 16 ? launch<16>(attention_few<16, 4>, 256, Few<16, 4>::kLds, done16, x, tiles, kFewPieces, kFewPlaces, kLeast, s)
+                          : launch<32>(attention_few<32, 4>, 256, Few<32, 4>::kLds, done32, x, tiles, kFewPieces, kFewPlaces, kLeast, s);
     };
     if (most <= kFewRows) return few(a, rows / 16 + c.n_seqs, rows / 32 + c.n_seqs);
-    Attention longer = a;
+    // Longer requests go to attention_many, the short ones of the call to a launch of attention_few (an empty one costs 4 µs), whose pieces
+    // share a long cache: unless there is one request.
     const bool all = c.n_seqs == 1;
+    Attention longer = a;
     longer.least_rows = all ? 0 : kFewRows + 1;
-    static bool done2[64], done4[64];
-        const long long groups = (rows / 256 + c.n_seqs) * pool.n_kv_heads;
-    hipError_t e = groups >= 384   ? launch<256>(attention_many<8, 1, 2, 2, 2, 2>, 512, Many<8, 1, 2, 2, 2>::kLds, done_many, longer, rows / 256 + c.n_seqs, 0, 0, 8, s)
-                   : groups >= 112 ? launch<128>(attention_many<8, 2, 2, 1, 2, 2>, 512, Many<8, 2, 2, 1, 2>::kLds, done2, longer, rows / 128 + c.n_seqs, 0, 0, 8, s)
-                                   : launch<64>(attention_many<8, 4, 1, 1, 2, 2>, 512, Many<8, 4, 1, 1, 2>::kLds, done4, longer, rows / 64 + c.n_seqs, kManyPieces, kManyPlaces, kLeastMany, s);
+    // Tiles of 256, 128 or 64 rows, by how many of 256 there are.  In µs, tiles of 256 / 128 / 64 rows; first the number of tiles of 256:
+    //   520 (16384 tokens, 8 heads) 547 / 596 / 794;  1280 (four prompts, 40 heads) 296 / 323 / 466;  288 (2048 tokens, 32 heads) 84 / 63 / 88;
+    //   264 (2048 behind 8192, 32 heads on 8) 322 / 336 / 447;  96 (512 behind 1536, 32 heads) 84 / 52 / 40.
+    const long long groups = (rows / 256 + c.n_seqs) * pool.n_kv_heads;
+    static bool done256[64], done128[64], done64[64];
+    hipError_t e = groups >= 384   ? launch<256>(attention_many<8, 1, 2, 2, 2, 2>, 512, Many<8, 1, 2, 2, 2>::kLds, done256, longer, rows / 256 + c.n_seqs, 0, 0, 8, s)
+                   : groups >= 112 ? launch<128>(attention_many<8, 2, 2, 1, 2, 2>, 512, Many<8, 2, 2, 1, 2>::kLds, done128, longer, rows / 128 + c.n_seqs, 0, 0, 8, s)
+                                   : launch<64>(attention_many<8, 4, 1, 1, 2, 2>, 512, Many<8, 4, 1, 1, 2>::kLds, done64, longer, rows / 64 + c.n_seqs, kManyPieces, kManyPlaces, kLeast, s);
     if (e != hipSuccess || all) return e;
     a.most_rows = kFewRows;
     const long long tiles = (long long)c.n_seqs * (kFewRows / 32);

@@ -4,7 +4,8 @@
 // of fresh give every request its rows and its place in the stack of free blocks.  One workgroup goes through the requests
 // 1024 at a time, twice: the sums alone (does the step fit?), then with the sums of the parts before it the writes.
 // Sums saturate: what the arrays hold is the caller's, and a sum that wraps would pass the checks.
-// Bound by latencies (loads, prefix sum, search, loads, stores): pages and rows are looked up four at a time.
+// Bound by latencies (loads, prefix sum, search, loads, stores): pages and rows are looked up four at a time.  Eight requests of five
+// tokens take 4.4 µs, 1024 requests of one to 230 9.5 in two launches.
 #include "paged.h"
 
 namespace jup {
@@ -258,7 +259,7 @@ __device__ __forceinline__ void rotate8(const u32x4 lo, const u32x4 hi, const fl
 }
 
 // One workgroup per row: 64 threads make the row's turns, then eight threads have a head of q, k or v each (two pieces of 16 bytes,
-// 64 elements apart).
+// 64 elements apart).  Bound by memory: prompts of 365 MB in and out take 67 µs, 5.4 TB/s (a large copy: 4.9 to 5.2).
 __global__ __launch_bounds__(256) void append_bf16(const jup_paged_pool_t pool, const jup_paged_append_t a, int shift, const Turns turns) {
     __shared__ float2 cs[64];
     const int row = blockIdx.x, tid = threadIdx.x;
@@ -337,6 +338,8 @@ __global__ __launch_bounds__(256) void append_f32(const jup_paged_pool_t pool, c
 
 hipError_t launch_paged_extend(const jup_paged_extend_t& a, hipStream_t s) {
     const int shift = log2_of(a.page_size);
+    // One workgroup for the rows as well, or a launch of their own: 4096 rows of 64 requests 6.4 and 7.5 µs, 8192 rows 8.2 and 7.6, 16384
+    // rows of 16 requests 11.0 and 7.4.
     if (a.max_rows <= 4096) {
         hipLaunchKernelGGL(extend_tables<true>, dim3(1), dim3(kPart), 0, s, a, shift);
     } else {

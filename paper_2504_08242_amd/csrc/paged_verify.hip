@@ -149,7 +149,9 @@ __device__ int search(const Weights<T>& w, int lo, int hi, double before, double
 }
 
 // `slices` workgroups per request, each with `length` tokens of the vocabulary.  All of them find the row (a few loads); the one that
-// is done last knows where the border is and goes through its slice again.
+// is done last knows where the border is and goes through its slice again.  Bound by trips to memory behind one another (rows, tokens,
+// their probabilities, the slice, the other slices' sums, the slice with the border): 12 µs for one request and 32000 tokens, 16 for 16
+// requests (one workgroup of 1024 threads per request instead: 22); 64 requests and 131072 tokens, 67 MB, take 26.
 template <class T>
 __global__ __launch_bounds__(kThreads) void verify(const jup_verify_drafts_t a, int slices, int length, int* count, double* scratch) {
     __shared__ Shared s;
