@@ -11,8 +11,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kEach = 32;                        // probabilities of a thread at a time
-constexpr int kBlock = kThreads * kEach;         // and of a workgroup: the shortest slice
+// E: probabilities of a thread at a time; kThreads * E are a workgroup's, the shortest slice
 constexpr int kMostSlices = kVerifySlices;
 
 // What the next token is drawn from: a row of the target's probabilities, less the draft's, or without one token.
@@ -64,7 +63,7 @@ struct Shared {
 // Sum of w over [lo, hi), the same in all threads.  64-bit operations are what this costs (half the rate of 32-bit ones, five per
 // token): the maximum with 0 takes care of negative differences and of NaN; an infinity shows in the sum, which is then made again
 // with every weight looked at.
-template <class T>
+template <int E, class T>
 __device__ double add_up(const Weights<T>& w, int lo, int hi, Shared& s) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     constexpr int V = 16 / sizeof(T);
@@ -72,9 +71,9 @@ __device__ double add_up(const Weights<T>& w, int lo, int hi, Shared& s) {
     double sum = 0.0;
     for (int careful = 0; careful < 2; ++careful) {
         double mine = 0.0;
-        for (int j0 = lo; j0 < hi; j0 += kBlock) {
+        for (int j0 = lo; j0 < hi; j0 += kThreads * E) {
 #pragma unroll
-            for (int k = 0; k < kEach / V; ++k)  // neighbouring threads have neighbouring pieces of 16 bytes
+            for (int k = 0; k < E / V; ++k)  // neighbouring threads have neighbouring pieces of 16 bytes
                 w.template run<V>(j0 + (k * kThreads + tid) * V, hi, vector, [&](T p, T q, int j) {
                     mine += careful ? w.weight(p, q, j) : fmax((double)(j == w.without ? 0.0f : w.value(p)) - (double)w.value(q), 0.0);
                 });
@@ -106,14 +105,14 @@ __device__ int last_weight(const Weights<T>& w, int vocab, Shared& s) {
     return s.found;
 }
 
-// The lowest j of [lo, hi) with before + w_lo + .. + w_j > border, or -1.  A thread has 32 neighbours.
-template <class T>
+// The lowest j of [lo, hi) with before + w_lo + .. + w_j > border, or -1.  A thread has E neighbours.
+template <int E, class T>
 __device__ int search(const Weights<T>& w, int lo, int hi, double before, double border, Shared& s) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const bool vector = w.aligned();
-    for (int j0 = lo; j0 < hi; j0 += kBlock) {
+    for (int j0 = lo; j0 < hi; j0 += kThreads * E) {
         double mine = 0.0;
-        w.template run<kEach>(j0 + tid * kEach, hi, vector, [&](T p, T q, int j) { mine += w.weight(p, q, j); });
+        w.template run<E>(j0 + tid * E, hi, vector, [&](T p, T q, int j) { mine += w.weight(p, q, j); });
         double upto = mine;
 #pragma unroll
         for (int by = 1; by < 64; by *= 2) {
@@ -134,7 +133,7 @@ __device__ int search(const Weights<T>& w, int lo, int hi, double before, double
         if (mine > 0.0 && run + mine > border) {
             // (threads behind the one that has the border get here too, and find something later)
             int at = INT32_MAX;
-            w.template run<kEach>(j0 + tid * kEach, hi, vector, [&](T p, T q, int j) {
+            w.template run<E>(j0 + tid * E, hi, vector, [&](T p, T q, int j) {
                 const double x = w.weight(p, q, j);
                 run += x;
                 if (x > 0.0 && run > border) at = min(at, j);
@@ -150,9 +149,9 @@ __device__ int search(const Weights<T>& w, int lo, int hi, double before, double
 
 // `slices` workgroups per request, each with `length` tokens of the vocabulary.  All of them find the row (a few loads); the one that
 // is done last knows where the border is and goes through its slice again.  Bound by trips to memory behind one another (rows, tokens,
-// their probabilities, the slice, the other slices' sums, the slice with the border): 12 µs for one request and 32000 tokens, 16 for 16
-// requests (one workgroup of 1024 threads per request instead: 22); 64 requests and 131072 tokens, 67 MB, take 26.
-template <class T>
+// their probabilities, the slice, the other slices' sums, the slice with the border): 9.5 µs for one request and 32000 tokens, 11.5 for
+// 16 requests (one workgroup of 1024 threads per request instead: 22); 64 requests and 131072 tokens, 67 MB, take 27.
+template <class T, int E>
 __global__ __launch_bounds__(kThreads) void verify(const jup_verify_drafts_t a, int slices, int length, int* count, double* scratch) {
     __shared__ Shared s;
     const int i = blockIdx.x / slices, slice = blockIdx.x - i * slices, tid = threadIdx.x;
@@ -184,7 +183,7 @@ __global__ __launch_bounds__(kThreads) void verify(const jup_verify_drafts_t a, 
         if (a.draft_probs) w.q = (const T*)a.draft_probs + row * a.draft_row_stride;
         else w.without = a.tokens[row + 1];
     }
-    const double sum = add_up(w, min(slice * length, a.vocab), min((slice + 1) * length, a.vocab), s);
+    const double sum = add_up<E>(w, min(slice * length, a.vocab), min((slice + 1) * length, a.vocab), s);
     if (slices > 1) {
         float* mine = (float*)(scratch + (long long)i * slices + slice);
         if (tid == 0) {
@@ -220,14 +219,14 @@ __global__ __launch_bounds__(kThreads) void verify(const jup_verify_drafts_t a, 
         run += s.sum[k];
     }
     // (beyond the slice, should its sum in this order fall short of the border by a rounding)
-    if (at >= 0) next = search(w, min(at * length, a.vocab), a.vocab, before, border, s);
+    if (at >= 0) next = search<E>(w, min(at * length, a.vocab), a.vocab, before, border, s);
     if (next < 0) {  // hardly ever, and this workgroup alone: u leaves no token (or rounding does), or there is none
         next = last_weight(w, a.vocab, s);
         if (next < 0 && row < end - 1) {  // a rejected row whose weights are all 0: the target itself
             w.q = nullptr;
             w.without = -1;
-            const double whole = add_up(w, 0, a.vocab, s);
-            next = search(w, 0, a.vocab, 0.0, u < 0.0f ? 0.0 : (double)u * whole, s);
+            const double whole = add_up<E>(w, 0, a.vocab, s);
+            next = search<E>(w, 0, a.vocab, 0.0, u < 0.0f ? 0.0 : (double)u * whole, s);
             if (next < 0) next = last_weight(w, a.vocab, s);
         }
     }
@@ -243,14 +242,18 @@ __global__ __launch_bounds__(kThreads) void verify(const jup_verify_drafts_t a, 
 }  // namespace
 
 hipError_t launch_verify_drafts(const jup_verify_drafts_t& a, hipStream_t s) {
-    int length = kBlock;
-    if ((long long)length * kMostSlices < a.vocab) length = (int)(((long long)a.vocab + kMostSlices * kBlock - 1) / (kMostSlices * kBlock)) * kBlock;
-    const int slices = (a.vocab + length - 1) / length;
-    int* count = (int*)a.workspace;
-    double* scratch = (double*)((char*)a.workspace + kCountBytes);
-    const dim3 grid((unsigned)a.n_seqs * (unsigned)slices);
-    if (a.probs_dtype == JUP_BF16) hipLaunchKernelGGL(verify<u16>, grid, dim3(kThreads), 0, s, a, slices, length, count, scratch);
-    else hipLaunchKernelGGL(verify<float>, grid, dim3(kThreads), 0, s, a, slices, length, count, scratch);
+    auto go = [&](auto kernel, int each) {
+        const int block = kThreads * each;
+        const int length = (int)(((long long)a.vocab + (long long)kMostSlices * block - 1) / ((long long)kMostSlices * block)) * block;
+        const int slices = (a.vocab + length - 1) / length;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)a.n_seqs * (unsigned)slices), dim3(kThreads), 0, s, a, slices, length, (int*)a.workspace,
+                           (double*)((char*)a.workspace + kCountBytes));
+    };
+    // Slices of 4096 tokens, or of 8192 where the short ones would be more workgroups than four per CU.  16 requests and 32000 tokens 11.5 and
+    // 15.6 µs, 32 and 131072 (1024 short slices) 19.8 and 20.4; 64 and 131072 27.8 and 27.0, 256 and 32000 21.5 and 19.5.
+    const bool shorter = (long long)a.n_seqs * ((a.vocab + 4095) / 4096) <= 1024;
+    if (a.probs_dtype == JUP_BF16) shorter ? go(verify<u16, 16>, 16) : go(verify<u16, 32>, 32);
+    else shorter ? go(verify<float, 16>, 16) : go(verify<float, 32>, 32);
     return hipGetLastError();
 }
 

@@ -793,6 +793,14 @@ def test_verification_of_a_very_large_vocabulary(workspace, dtype, vocab):
 
 @gpu
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,most,vocab", [(64, 1, 65536), (61, 1, 65537), (66, 2, 65537), (260, 0, 16385), (1100, 1, 60)])
+def test_verification_of_many_requests(workspace, dtype, n, most, vocab):
+    """So many that slices are longer (more than 1024 short ones), and just not so many."""
+    check_verify(workspace, *make_verify(n, most, vocab, dtype, most != 2, vocab))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_verification_of_unusual_numbers(workspace, dtype):
     nan, inf = float("nan"), float("inf")
     V = 300
