@@ -326,61 +326,74 @@ __device__ __forceinline__ bool row_not_finite(const char* row) {
 // ---- pieces of one tile put together ------------------------------------------------------------------------------------------
 // The workgroups of a tile's pieces leave un-normalised sums and their softmax statistics in the scratch; the one that
 // arrives last adds them in the order of the pieces (the result does not depend on who that is) and writes the rows.  Nobody
-// waits.  A wave has a row, a lane two neighbouring features: whole lines go to memory and back (8 bytes at 32-byte steps, as the
-// sums lie in the registers, are a partial write each).
+// waits.  Half a wave has a row, a lane 16 bytes of it: whole lines go to memory and back (a few bytes at 32-byte steps, as the sums lie
+// in the registers, are a partial write each).  One CU takes 20 GB/s out of memory in loads of 8 bytes per lane: with 16 bytes, and no
+// branches between the loads, 88 rows behind 8200 take 42 µs instead of 65, 300 tokens behind 6000 29 instead of 41.
 
-// N rows per wave, PC pieces of each in flight at once: they come from memory, microseconds away.
+// Accesses of 16 bytes that are performed chip-wide, as load_coherent2() and store_coherent2() of 8 are.
+constexpr int kCoherent = 16;  // of the buffer builtins: past L2
+__device__ __forceinline__ auto scratch_of(const float* p) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)uniform_ptr((const char*)p), 0, 0x7FFFFFFF, 0x00027000);
+}
+
+// Two rows per wave at a time (a half has one, a lane four features of it: 16 bytes), N such pairs and PC pieces of each in flight at once:
+// they come from memory, microseconds away.  No branches around the loads: what is not there is read twice and counts as a piece without keys.
 template <int WAVES, int N, int PC>
 __device__ __forceinline__ void join_rows(const Attention& a, const Work& w, int R, int kv_head, int rows, const float* base, long long step) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r0 = 2 * wave + ((threadIdx.x >> 5) & 1);
+    const auto scratch = scratch_of(base);
     float m[N], l[N];
-    float2 acc[N];
+    f32x4 acc[N];
 #pragma unroll
     for (int x = 0; x < N; ++x) {
         m[x] = -INFINITY;
-        l[x] = acc[x].x = acc[x].y = 0.f;
+        l[x] = 0.f;
+        acc[x] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
     for (int p0 = 0; p0 < w.pieces; p0 += PC) {
-        float2 stat[N][PC], val[N][PC];
+        u32x2 stat[N][PC];
+        u32x4 val[N][PC];
 #pragma unroll
         for (int x = 0; x < N; ++x)
 #pragma unroll
             for (int p = 0; p < PC; ++p) {
-                if (wave + x * WAVES >= rows || p0 + p >= w.pieces) continue;
-                const float* from = base + (p0 + p) * step + (long long)(wave + x * WAVES) * kPartRow;
-                stat[x][p] = load_coherent2(from + 128);
-                val[x][p] = load_coherent2(from + 2 * lane);
+                const unsigned at = (unsigned)(min(p0 + p, w.pieces - 1) * (int)step * 4) + min(r0 + x * 2 * WAVES, rows - 1) * (kPartRow * 4);
+                stat[x][p] = __builtin_amdgcn_raw_buffer_load_b64(scratch, at + 512, 0, kCoherent);
+                val[x][p] = __builtin_amdgcn_raw_buffer_load_b128(scratch, at + 16 * lane, 0, kCoherent);
             }
 #pragma unroll
         for (int x = 0; x < N; ++x) {
-            if (wave + x * WAVES >= rows) continue;
             float top = m[x];
 #pragma unroll
-            for (int p = 0; p < PC; ++p)
-                if (p0 + p < w.pieces) top = fmaxf(top, stat[x][p].x);
+            for (int p = 0; p < PC; ++p) top = fmaxf(top, __uint_as_float(stat[x][p][0]));
             if (top == -INFINITY) top = 0.f;
             const float back = __builtin_amdgcn_exp2f(m[x] - top);
             l[x] *= back;
-            acc[x].x *= back;
-            acc[x].y *= back;
+            acc[x] *= back;
 #pragma unroll
-            for (int p = 0; p < PC; ++p)
-                if (p0 + p < w.pieces && stat[x][p].y != 0.f) {  // (0: a piece this row sees nothing of)
-                    const float f = __builtin_amdgcn_exp2f(stat[x][p].x - top);
-                    l[x] += stat[x][p].y * f;
-                    acc[x].x += val[x][p].x * f;
-                    acc[x].y += val[x][p].y * f;
+            for (int p = 0; p < PC; ++p) {
+                const float sum = __uint_as_float(stat[x][p][1]);
+                if (p0 + p < w.pieces && sum != 0.f) {  // (0: a piece this row sees nothing of)
+                    const float f = __builtin_amdgcn_exp2f(__uint_as_float(stat[x][p][0]) - top);
+                    l[x] += sum * f;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[x][e] += __uint_as_float(val[x][p][e]) * f;
                 }
+            }
             m[x] = top;
         }
     }
 #pragma unroll
     for (int x = 0; x < N; ++x) {
-        if (wave + x * WAVES >= rows) continue;
+        const int r = r0 + x * 2 * WAVES;
+        if (r >= rows) continue;
         const float inv = l[x] == 0.f ? 0.f : 1.0f / l[x];
-        const int row = w.tile * R + wave + x * WAVES, token = a.group.of(row);
-        *(unsigned*)(out_piece(a, w.begin + token, (kv_head - token) * (int)a.group.d + row, lane >> 2) + 2 * (lane & 3)) =
-            pack_bf16x2(acc[x].x * inv, acc[x].y * inv);
+        const int row = w.tile * R + r, token = a.group.of(row);
+        u32x2 o;
+        o[0] = pack_bf16x2(acc[x][0] * inv, acc[x][1] * inv);
+        o[1] = pack_bf16x2(acc[x][2] * inv, acc[x][3] * inv);
+        *(u32x2*)(out_piece(a, w.begin + token, (kv_head - token) * (int)a.group.d + row, lane >> 1) + 4 * (lane & 1)) = o;
     }
 }
 
@@ -401,23 +414,20 @@ __device__ __forceinline__ void join_pieces(const Work& w, int kv_head, int* fla
     const long long step = (long long)a.n_kv_heads * R * kPartRow;
     const float* base = a.partial + ((long long)w.slot * a.n_kv_heads + kv_head) * R * kPartRow;
     const int rows = min(R, w.tokens * (int)a.group.d - w.tile * R);
-    constexpr int N = R / WAVES;
-    if (rows <= WAVES) join_rows<WAVES, 1, 24>(a, w, R, kv_head, rows, base, step);
-    else join_rows<WAVES, N, (N >= 32 ? 1 : 32 / N)>(a, w, R, kv_head, rows, base, step);
+    constexpr int N = R / (2 * WAVES);
+    if (rows <= 2 * WAVES) join_rows<WAVES, 1, 16>(a, w, R, kv_head, rows, base, step);
+    else join_rows<WAVES, N, 16 / N>(a, w, R, kv_head, rows, base, step);
 }
 // A workgroup's sums of row r, in LDS as `PARTS` partial ones `region` bytes apart, into their place in the scratch.
 template <int PARTS, int WAVES>
 __device__ __forceinline__ void store_pieces(const unsigned char* sums, int row_bytes, int region, float* place, int rows) {
-    const int lane = threadIdx.x & 63;
-    for (int r = threadIdx.x >> 6; r < rows; r += WAVES) {
-        float2 x = *(const float2*)(sums + r * row_bytes + lane * 8);
+    const int lane = threadIdx.x & 31;
+    const auto scratch = scratch_of(place);
+    for (int r = threadIdx.x >> 5; r < rows; r += 2 * WAVES) {
+        f32x4 x = *(const f32x4*)(sums + r * row_bytes + lane * 16);
 #pragma unroll
-        for (int k = 1; k < PARTS; ++k) {
-            const float2 y = *(const float2*)(sums + k * region + r * row_bytes + lane * 8);
-            x.x += y.x;
-            x.y += y.y;
-        }
-        store_coherent2(place + (long long)r * kPartRow + 2 * lane, x.x, x.y);
+        for (int k = 1; k < PARTS; ++k) x += *(const f32x4*)(sums + k * region + r * row_bytes + lane * 16);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), scratch, r * kPartRow * 4 + lane * 16, 0, kCoherent);
     }
 }
 
@@ -1155,11 +1165,15 @@ namespace {
 // A request's rows up to which attention_few has it.  64 and 128 rows behind 1536 on 32 heads take attention_few 51 and 45 µs, attention_many 41
 // and 36; 16 requests of 40 rows 49 and 43; but four requests of 100 rows 47 and 55.
 constexpr int kFewRows = 32;
-// Pieces: two workgroups per CU (with 1024 pieces of at least 4 key tiles, one token behind 8192 takes 38 µs, with 512 of 24 tiles 31), three
-// of eight waves for four CUs (256: 30 µs, 192: 28).
+// Pieces: two workgroups per CU (one token behind 8192 27.4 µs with 768, 27.0 with 512 as with 192 of eight waves), three of
+// eight waves for four CUs (16 requests behind 10 to 8000 on 8 heads 28 µs, with 256 pieces 36).
 constexpr int kFewPieces = 512, kWidePieces = 192;
-constexpr int kLeast = 24;       // key tiles that are worth a piece
-// A workgroup per CU, less what the longest piece may be longer than the average: 300 tokens behind 6000 on 8 heads 42 µs, with 256 pieces 56.
+// Key tiles that are worth a piece.  One token behind 576 (19 tiles) takes 10.4 µs whole and 12.3 in two pieces, behind 2048 14.3 in pieces of 24
+// tiles and 12.9 in pieces of 16; 48 rows behind 1300 take 24.2, 21.3 and 20.2 in pieces of 24, 16 and 12; 88 rows behind 8200 42 in all of these,
+// 47 in pieces of 8.
+constexpr int kLeast = 20, kLeastMany = 16;
+// A workgroup per CU, less what the longest piece may be longer than the average: 300 tokens behind 6000 on 8 heads 29 µs (with 256 pieces half as much
+// again).
 constexpr int kManyPieces = 222;
 constexpr int kMostSplitHeads = 128;  // (more heads than that fill the chip without dividing keys)
 constexpr int kFewPlaces = 2 * (kFewPieces + kMostSplitHeads), kManyPlaces = 4 * (kManyPieces + kMostSplitHeads);
@@ -1238,7 +1252,7 @@ hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_
     static bool done256[64], done128[64], done64[64];
     hipError_t e = groups >= 384   ? launch<256>(attention_many<8, 1, 2, 2, 2, 2>, 512, Many<8, 1, 2, 2, 2>::kLds, done256, longer, rows / 256 + c.n_seqs, 0, 0, 8, s)
                    : groups >= 112 ? launch<128>(attention_many<8, 2, 2, 1, 2, 2>, 512, Many<8, 2, 2, 1, 2>::kLds, done128, longer, rows / 128 + c.n_seqs, 0, 0, 8, s)
-                                   : launch<64>(attention_many<8, 4, 1, 1, 2, 2>, 512, Many<8, 4, 1, 1, 2>::kLds, done64, longer, rows / 64 + c.n_seqs, kManyPieces, kManyPlaces, kLeast, s);
+                                   : launch<64>(attention_many<8, 4, 1, 1, 2, 2>, 512, Many<8, 4, 1, 1, 2>::kLds, done64, longer, rows / 64 + c.n_seqs, kManyPieces, kManyPlaces, kLeastMany, s);
     if (e != hipSuccess || all) return e;
     a.most_rows = kFewRows;
     const long long tiles = (long long)c.n_seqs * (kFewRows / 32);
