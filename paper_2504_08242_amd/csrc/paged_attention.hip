@@ -339,9 +339,9 @@ __device__ __forceinline__ auto scratch_of(const float* p) {
 // Two rows per wave at a time (a half has one, a lane four features of it: 16 bytes), N such pairs and PC pieces of each in flight at once:
 // they come from memory, microseconds away.  No branches around the loads: what is not there is read twice and counts as a piece without keys.
 template <int WAVES, int N, int PC>
-__device__ __forceinline__ void join_rows(const Attention& a, const Work& w, int R, int kv_head, int rows, const float* base, long long step) {
+__device__ __forceinline__ void join_rows(const Attention& a, const Work& w, int R, int kv_head, int first, int rows, const float* base, long long step) {
     const int lane = threadIdx.x & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r0 = 2 * wave + ((threadIdx.x >> 5) & 1);
+    const int r0 = first + 2 * wave + ((threadIdx.x >> 5) & 1);
     const auto scratch = scratch_of(base);
     float m[N], l[N];
     f32x4 acc[N];
@@ -414,9 +414,10 @@ __device__ __forceinline__ void join_pieces(const Work& w, int kv_head, int* fla
     const long long step = (long long)a.n_kv_heads * R * kPartRow;
     const float* base = a.partial + ((long long)w.slot * a.n_kv_heads + kv_head) * R * kPartRow;
     const int rows = min(R, w.tokens * (int)a.group.d - w.tile * R);
-    constexpr int N = R / (2 * WAVES);
-    if (rows <= 2 * WAVES) join_rows<WAVES, 1, 16>(a, w, R, kv_head, rows, base, step);
-    else join_rows<WAVES, N, 16 / N>(a, w, R, kv_head, rows, base, step);
+    constexpr int N = R / (2 * WAVES) < 4 ? R / (2 * WAVES) : 4;
+    if (rows <= 2 * WAVES) join_rows<WAVES, 1, 16>(a, w, R, kv_head, 0, rows, base, step);
+    else
+        for (int first = 0; first < rows; first += 2 * WAVES * N) join_rows<WAVES, N, 16 / N>(a, w, R, kv_head, first, rows, base, step);
 }
 // A workgroup's sums of row r, in LDS as `PARTS` partial ones `region` bytes apart, into their place in the scratch.
 template <int PARTS, int WAVES>
@@ -729,7 +730,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_few(const Attention args
 // waves, and the waves meet once per step.  Two waves share a SIMD: one's exponentials lie under the other's products.
 // KP parts of the keys: a workgroup has 256 / KP rows, and KP waves divide the keys of 32 of them and add up through LDS at the
 // end.  One part reads a key for the most rows; more parts make more workgroups of fewer rows, where rows are few or
-// where triangles of different sizes are to be dealt to the CUs.
+// where triangles of different sizes are to be dealt to the CUs.  Where one request's keys are far more than the others', they are divided
+// among workgroups: five requests of 100 to 300 tokens behind 10 to 20000 take 122 µs instead of 342, three of 40 to 500 behind 2000 to 9000
+// 84 instead of 138 (but six of 1 to 600 behind 10 to 32000 660 instead of 603: 320 equal pieces for 256 CUs).
 // Measured: a prompt of 16384 tokens on 8 heads in 540 µs, 1019 TFLOP/s, matrix cores busy 44 % of the clocks, LDS 22 %.  Without loads
 // from memory it takes 92 % of that, without exponentials 89 %, without LDS reads 73 %, without products 95 %: no one unit binds it, but the
 // waves wait for one another's, as registers leave room for two per SIMD.  Three per SIMD of half the keys each: 970 instead of 1050 TFLOP/s.  One wave per
@@ -747,7 +750,7 @@ struct Many {
     static constexpr int kGroups = kStepTiles * 4 / kWaves;  // groups of eight rows that a wave fetches per step: wave, wave + NW
     static_assert(kGroups * kWaves == kStepTiles * 4);
     static constexpr int kRowBytes = 132 * 4;                // a row of a part's sums
-    static constexpr int kSteps = kRing * 2 * kHalf, kSums = KP > 1 ? 32 * NW * kRowBytes : 0, kQ = 32 * NW * 256;
+    static constexpr int kSteps = kRing * 2 * kHalf, kSums = 32 * NW * kRowBytes, kQ = 32 * NW * 256;
     static constexpr int kThere = (kSteps > kSums ? kSteps > kQ ? kSteps : kQ : kSums);  // [kRing][kStepTiles * 4] bytes: which rows of a step's groups are keys
     static constexpr int kFlag = kThere + 64;
     static constexpr int kStat = kFlag + 64;                 // [2][waves][32] maxima and sums
@@ -756,8 +759,6 @@ struct Many {
     // queries go through the last places of the ring, the first kFirst steps are fetched beside them
     static constexpr int kFirst = (kThere - kQ) / (2 * kHalf) < kRing - 1 ? (kThere - kQ) / (2 * kHalf) : kRing - 1;
     static constexpr int kQAt = kThere - kQ;
-    // Only the shape with the fewest rows divides keys among workgroups: the sums of 64 rows are 34 KB per piece, and one CU reads them all.
-    static constexpr bool kSplits = KP == 4;
 };
 
 // Waits until at most `steps` steps' loads of this wave (four or eight each) are in flight.
@@ -1043,11 +1044,11 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const Attention a
         for (int x = 0; x < KP; ++x) l += stat[32 * NW + (first + x) * 32 + c] * __builtin_amdgcn_exp2f(stat[(first + x) * 32 + c] - ref);
         f = __builtin_amdgcn_exp2f(m_run - ref);
     }
-    const bool pieces = L::kSplits && w.pieces > 1;
+    const bool pieces = w.pieces > 1;
     if (!pieces) f *= l == 0.f ? 0.f : 1.0f / l;
     const long long place = ((long long)(w.slot + w.piece) * e.n_kv_heads + kv_head) * kRows;
     if (pieces && part == 0 && hh == 0 && r_wave + c < rows) store_coherent2(e.partial + (place + r_wave + c) * kPartRow + 128, m, l);
-    if (KP == 1) {  // rows as they are, through LDS to whole lines (a wave reads its own rows only)
+    if (KP == 1 && !pieces) {  // rows as they are, through LDS to whole lines (a wave reads its own rows only)
         unsigned char* to = lds + (r_wave + c) * 256;  // 16-byte pieces as in a K tile
 #pragma unroll
         for (int x = 0; x < 16; ++x) {
@@ -1175,9 +1176,9 @@ constexpr int kLeast = 20, kLeastMany = 16;
 // A workgroup per CU, less what the longest piece may be longer than the average: 300 tokens behind 6000 on 8 heads 29 µs (with 256 pieces half as much
 // again).
 constexpr int kManyPieces = 222;
-constexpr int kMostSplitHeads = 128;  // (more heads than that fill the chip without dividing keys)
+constexpr int kMostSplitHeads = 64;  // (more heads than that fill the chip without dividing keys)
 constexpr int kFewPlaces = 2 * (kFewPieces + kMostSplitHeads), kManyPlaces = 4 * (kManyPieces + kMostSplitHeads);
-constexpr size_t kPartialBytes = (size_t)(kFewPlaces * 32 > kManyPlaces * 64 ? kFewPlaces * 32 : kManyPlaces * 64) * kPartRow * 4;
+constexpr size_t kPartialBytes = (size_t)(kFewPlaces * 32 > kManyPlaces * 256 ? kFewPlaces * 32 : kManyPlaces * 256) * kPartRow * 4;
 constexpr size_t kPlanBytes = ((size_t)JUP_PAGED_MAX_SEQS + 2) * 8;
 static_assert(kFewPlaces * 4 <= kCountBytes && kManyPlaces * 4 <= kCountBytes);
 
@@ -1250,8 +1251,8 @@ hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_
     //   264 (2048 behind 8192, 32 heads on 8) 322 / 336 / 447;  96 (512 behind 1536, 32 heads) 84 / 52 / 40.
     const long long groups = (rows / 256 + c.n_seqs) * pool.n_kv_heads;
     static bool done256[64], done128[64], done64[64];
-    hipError_t e = groups >= 384   ? launch<256>(attention_many<8, 1, 2, 2, 2, 2>, 512, Many<8, 1, 2, 2, 2>::kLds, done256, longer, rows / 256 + c.n_seqs, 0, 0, 8, s)
-                   : groups >= 112 ? launch<128>(attention_many<8, 2, 2, 1, 2, 2>, 512, Many<8, 2, 2, 1, 2>::kLds, done128, longer, rows / 128 + c.n_seqs, 0, 0, 8, s)
+    hipError_t e = groups >= 384   ? launch<256>(attention_many<8, 1, 2, 2, 2, 2>, 512, Many<8, 1, 2, 2, 2>::kLds, done256, longer, rows / 256 + c.n_seqs, kManyPieces, kManyPlaces, kLeastMany, s)
+                   : groups >= 112 ? launch<128>(attention_many<8, 2, 2, 1, 2, 2>, 512, Many<8, 2, 2, 1, 2>::kLds, done128, longer, rows / 128 + c.n_seqs, kManyPieces, kManyPlaces, kLeastMany, s)
                                    : launch<64>(attention_many<8, 4, 1, 1, 2, 2>, 512, Many<8, 4, 1, 1, 2>::kLds, done64, longer, rows / 64 + c.n_seqs, kManyPieces, kManyPlaces, kLeastMany, s);
     if (e != hipSuccess || all) return e;
     a.most_rows = kFewRows;

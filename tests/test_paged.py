@@ -469,6 +469,29 @@ def test_holes_and_unseen_values_with_many_heads(workspace, heads):
         assert not torch.isfinite(got[60:90, :, 7]).any()
 
 
+@gpu
+@pytest.mark.parametrize("requests", [[(3000, 40), (0, 33)], [(0, 33)] * 6 + [(3000, 40)]])
+def test_a_long_cache_among_many_heads(workspace, requests):
+    """Tiles of 128 and of 256 rows whose keys are divided; with pages that are not there, values that are no numbers, and in place."""
+    b = Batch(torch.bfloat16, 60, 60, 16, requests)
+    want = b.run(workspace)
+    b.check(want)
+    long = int(np.argmax(b.lengths))
+    t = b.table.copy()
+    t[long, [0, 7, 100, 150, 151]] = [-1, b.k.shape[0], 2 ** 31 - 1, -2, -3]
+    b.check(b.run(workspace, table=t), table=t)
+    c = Batch(torch.bfloat16, 60, 60, 16, requests)
+    new = requests[long][1]
+    pos, at = 3000 + new // 2, c.row_start[long] + new // 2
+    c.v[int(c.table[long, pos // 16]), :, pos % 16, 7] = float("inf")
+    got = c.run(workspace)
+    assert torch.equal(got[:at], want[:at]) and torch.equal(got[c.row_start[long + 1]:], want[c.row_start[long + 1]:])
+    assert (got[at:c.row_start[long + 1], :, 7] == float("inf")).all()
+    got[at:c.row_start[long + 1], :, 7] = want[at:c.row_start[long + 1], :, 7]
+    assert torch.equal(got, want)
+    assert b.run(workspace, out=b.q) is b.q and torch.equal(b.q, want)
+
+
 def many_requests(n, most_cached, most_new, seed):
     rng = np.random.default_rng(seed)
     requests = [(int(rng.integers(0, most_cached + 1)), int(rng.integers(0, most_new + 1))) for _ in range(n)]
