@@ -1241,9 +1241,10 @@ hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_
                           : launch<32>(attention_few<32, 4>, 256, Few<32, 4>::kLds, done32, x, tiles, kFewPieces, kFewPlaces, kLeast, s);
     };
     if (most <= kFewRows) return few(a, rows / 16 + c.n_seqs, rows / 32 + c.n_seqs);
-    // Longer requests go to attention_many, the short ones of the call to a launch of attention_few (an empty one costs 4 µs), whose pieces
-    // share a long cache: unless there is one request.
-    const bool all = c.n_seqs == 1;
+    // Up to 32 requests all go to attention_many, of more the short ones to a launch of attention_few (an empty one costs 4 µs).  One launch
+    // and two: four of 24 to 39 tokens 11 and 18 µs, 13 of 1 to 7 (eight query heads per key head) 18 and 30, 15 of one token behind 4000 and one
+    // of 512 62 and 65, 32 of 1 to 300 behind 100 to 3000 171 and 180; 63 of one token behind 4000 and one of 256 807 and 760.
+    const bool all = c.n_seqs <= 32;
     Attention longer = a;
     longer.least_rows = all ? 0 : kFewRows + 1;
     // Tiles of 256, 128 or 64 rows, by how many of 256 there are.  In µs, tiles of 256 / 128 / 64 rows; first the number of tiles of 256:
