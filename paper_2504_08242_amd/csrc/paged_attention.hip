@@ -439,7 +439,7 @@ __device__ __forceinline__ void store_pieces(const unsigned char* sums, int row_
 // are.  Two workgroups share a CU, so 128 KB are in flight on it, and one's entry and merge lie under the other's loads.
 // Where there is a workgroup per CU at most, eight waves divide the keys, and there are half as many pieces to put together: one token
 // behind 8192 31 -> 28 µs, behind 65536 with four query heads per key head 71 -> 61.
-// Keys and values of 64 requests of one token (550 MB) pass in 108 µs, 5.0 TB/s; of 16 requests of five tokens, whose lengths are
+// Keys and values of 64 requests of one token (550 MB) pass in 110 µs, 5.0 TB/s; of 16 requests of five tokens, whose lengths are
 // uneven, in 45 µs, 5.4 TB/s (the last-level cache holds some of them from call to call).  One token behind 576 takes 10 µs: lengths,
 // block numbers, a tile and its neighbours, the merge of the waves, each a trip to memory or through LDS behind the other.
 // Transposed products, S^T = K Q^T and O^T += V^T P^T: a lane owns a row, whose statistics are scalars of the lane.
@@ -1247,9 +1247,10 @@ hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_
     const bool all = c.n_seqs <= 32;
     Attention longer = a;
     longer.least_rows = all ? 0 : kFewRows + 1;
-    // Tiles of 256, 128 or 64 rows, by how many of 256 there are.  In µs, tiles of 256 / 128 / 64 rows; first the number of tiles of 256:
-    //   520 (16384 tokens, 8 heads) 547 / 596 / 794;  1280 (four prompts, 40 heads) 296 / 323 / 466;  288 (2048 tokens, 32 heads) 84 / 63 / 88;
-    //   264 (2048 behind 8192, 32 heads on 8) 322 / 336 / 447;  96 (512 behind 1536, 32 heads) 84 / 52 / 40.
+    // Tiles of 256, 128 or 64 rows, by how many of 256 there are at most.  In µs, tiles of 256 / 128 / 64 rows; first the number of tiles of 256:
+    //   1280 (four prompts, 40 heads) 292 / 320 / 458;  520 (16384 tokens, 8 heads) 542 / 594 / 782;  384 (2900 tokens, 32 heads) 100 / 104 / 141;
+    //   360 (2048 tokens, 40 heads) 78 / 76 / 101;  320 (three chunks, 40 heads) 64 / 55 / 74;  288 (2048 tokens, 32 heads) 66 / 57 / 81;  264 (2048 behind
+    //   8192, 32 heads on 8) 317 / 333 / 438;  160 (1024 tokens) 42 / 31 / 32;  128 (768 behind 1536) 54 / 61 / 57;  96 (512 behind 1536) 43 / 36 / 33.
     const long long groups = (rows / 256 + c.n_seqs) * pool.n_kv_heads;
     static bool done256[64], done128[64], done64[64];
     hipError_t e = groups >= 384   ? launch<256>(attention_many<8, 1, 2, 2, 2, 2>, 512, Many<8, 1, 2, 2, 2>::kLds, done256, longer, rows / 256 + c.n_seqs, kManyPieces, kManyPlaces, kLeastMany, s)

@@ -259,7 +259,7 @@ __device__ __forceinline__ void rotate8(const u32x4 lo, const u32x4 hi, const fl
 }
 
 // One workgroup per row: 64 threads make the row's turns, then eight threads have a head of q, k or v each (two pieces of 16 bytes,
-// 64 elements apart).  Bound by memory: prompts of 365 MB in and out take 67 µs, 5.4 TB/s (a large copy: 4.9 to 5.2).
+// 64 elements apart).  Bound by memory: prompts of 365 MB in and out take 69 µs, 5.3 TB/s (a large copy: 4.9 to 5.2).
 __global__ __launch_bounds__(256) void append_bf16(const jup_paged_pool_t pool, const jup_paged_append_t a, int shift, const Turns turns) {
     __shared__ float2 cs[64];
     const int row = blockIdx.x, tid = threadIdx.x;
