@@ -27,8 +27,7 @@ struct Weights {
         return j != without && w > 0.0 && w < INFINITY ? w : 0.0;
     }
     // f(p_j, q_j, j) for N consecutive j from `first` on, those below `end`.  (Rows of an odd vocabulary begin anywhere: 16-byte loads need
-    // no more than a probability's own alignment; one by one, 64 requests and 131073 tokens take 73 µs
-    // instead of 33.)
+    // no more than a probability's own alignment; one by one, 64 requests and 131073 tokens take 73 µs instead of 33.)
     template <int N, class F>
     __device__ __forceinline__ void run(int first, int end, F f) const {
         if (first + N <= end) {

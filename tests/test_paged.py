@@ -492,6 +492,17 @@ def test_a_long_cache_among_many_heads(workspace, requests):
     assert b.run(workspace, out=b.q) is b.q and torch.equal(b.q, want)
 
 
+@gpu
+@pytest.mark.parametrize("heads,requests", [(20, [(0, 1)] * 5 + [(2000, 200)]), (20, [(0, 1)] * 19 + [(2000, 200)]), (4, [(3000, 200), (10, 3)]),
+                                            (64, [(0, 2)] * 6 + [(1500, 36)]), (65, [(0, 2)] * 6 + [(1500, 36)])])
+def test_tall_tiles_put_together(workspace, heads, requests):
+    """All rows of tiles of 128, 256 and 64 whose keys are divided; and as many heads as keys are divided for, and one more."""
+    b = Batch(torch.bfloat16, heads, heads, 32, requests)
+    got = b.run(workspace)
+    b.check(got)
+    assert torch.equal(got, b.run(workspace))
+
+
 def many_requests(n, most_cached, most_new, seed):
     rng = np.random.default_rng(seed)
     requests = [(int(rng.integers(0, most_cached + 1)), int(rng.integers(0, most_new + 1))) for _ in range(n)]
@@ -1050,6 +1061,7 @@ def small_stage(dtype, max_rows, w4_expanded=False):
     ("f32", [[37, 5, 0, 16], [1, 3, 20, 1], [1, 1, 1, 1]]),
     ("bf16", [[37, 5, 0, 16], [1, 3, 20, 1], [1, 1, 1, 1], [5, 5, 1, 5]]),     # 58, 25, 4 and 16 rows
     ("bf16", [[300, 0, 140, 64], [1, 200, 1, 1]]),
+    ("bf16", [[900, 20, 0, 40], [1, 130, 700, 1], [1, 1, 1, 5]]),             # keys divided among workgroups, in both kernels
     ("w4", [[37, 5, 0, 16], [1, 3, 7, 1], [1, 1, 1, 1]]),
     ("w4+bf16", [[90, 5, 0, 16], [1, 1, 1, 1]])])
 def test_a_stage_over_pages(dtype, steps, workspace):
