@@ -133,6 +133,12 @@ def test_verify_refuses(change, word):
     refused(jp._lib().jup_verify_drafts(ctypes.byref(verify_args(**change)), None), word)
 
 
+@pytest.mark.parametrize("change,word", [(dict(scale=1.1e38), "scale"), (dict(table_width=(1 << 27) - 1, table_stride=1 << 27), "2^31 - 256")])
+def test_attention_refuses_what_would_overflow(change, word):
+    a = attention_args(**change)
+    refused(jp._lib().jup_paged_attention(ctypes.byref(pool_args()), ctypes.byref(a), None), word)
+
+
 def test_null_arguments_and_empty_calls():
     L = jp._lib()
     refused(L.jup_paged_extend(None, None), "NULL")
@@ -771,6 +777,22 @@ def test_another_stream(workspace):
     got = b.run(jp.Workspace(DEV), stream=side)
     side.synchronize()
     assert torch.equal(got, want)
+
+
+@gpu
+def test_two_streams_at_once():
+    """Calls that overlap, each stream with a workspace of its own."""
+    batches = [Batch(torch.bfloat16, 4, 2, 16, r, seed=s) for s, r in enumerate(([(3000, 2), (900, 1)], [(2500, 70), (40, 3)]))]
+    spaces, streams = [jp.Workspace(DEV) for _ in batches], [torch.cuda.Stream() for _ in batches]
+    want = [b.run(w) for b, w in zip(batches, spaces)]
+    args = [(b.q, b.k, b.v, torch.from_numpy(b.table).to(DEV, torch.int32), ints(b.row_start), ints(b.lengths), max(b.new), w)
+            for b, w in zip(batches, spaces)]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(20):
+        got.append([jp.attention(*a, stream=s) for a, s in zip(args, streams)])
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for run in got for x, y in zip(run, want))
 
 
 # ---- verification ----------------------------------------------------------------------------------------------------------------
