@@ -433,7 +433,8 @@ __device__ __forceinline__ void store_pieces(const unsigned char* sums, int row_
 }
 
 // ---- few rows ----------------------------------------------------------------------------------------------------------------
-// Decoding and verification: a handful of rows against a long cache, bound by reading keys and values.  A tile has QW = 16 or
+// Decoding and verification: a handful of rows against a long cache, bound by reading keys and values (and calls of so few rows that
+// taller tiles would leave CUs without any).  A tile has QW = 16 or
 // 32 rows, and four waves divide the piece's key tiles: each works alone on the tiles wave, wave + 4, ..., with one LDS
 // slot for a K and one for a V tile, and refills the K slot as soon as the scores are out of it and the V slot as soon as the products
 // are.  Two workgroups share a CU, so 128 KB are in flight on it, and one's entry and merge lie under the other's loads.
@@ -1163,9 +1164,12 @@ namespace {
 // attention_few has at least two, each of which is at least half as long as a piece may be: at most twice as many places are
 // used.  attention_many counts a request's pieces as if all its tiles had the keys of the last one, at most twice what they
 // have on average: four times.
-// A request's rows up to which attention_few has it.  64 and 128 rows behind 1536 on 32 heads take attention_few 51 and 45 µs, attention_many 41
-// and 36; 16 requests of 40 rows 49 and 43; but four requests of 100 rows 47 and 55.
-constexpr int kFewRows = 32;
+// Calls whose requests have up to 96 rows, or that have no more tiles of 32 rows than fit the chip at once (two per CU), are attention_few's.
+// In µs, attention_few and attention_many: 64 rows behind 1536 on 32 heads 16 / 20, 96 rows 17 / 20, 128 rows (of 128 tiles) 17 / 21, 192 rows 20 / 34;
+// 16 requests of 96 rows behind 500 to 2100 29 / 38; 900 tokens behind 3000 on 16 heads over 2 (452 tiles) 78 / 87; four requests of 100 (416
+// tiles) 34 / 32; 512 tokens behind 1536 (544 tiles) 33 / 33; 20 requests of 128 rows behind 300 to 1000 (2560 tiles) 81 / 74.
+constexpr int kFewRows = 96;
+constexpr int kFewTiles = 512;
 // Pieces: two workgroups per CU (one token behind 8192 27.4 µs with 768, 27.0 with 512 as with 192 of eight waves), three of
 // eight waves for four CUs (16 requests behind 10 to 8000 on 8 heads 28 µs, with 256 pieces 36).
 constexpr int kFewPieces = 512, kWidePieces = 192;
@@ -1240,7 +1244,7 @@ hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_
         return most <= 16 ? launch<16>(attention_few<16, 4>, 256, Few<16, 4>::kLds, done16, x, tiles, kFewPieces, kFewPlaces, kLeast, s)
                           : launch<32>(attention_few<32, 4>, 256, Few<32, 4>::kLds, done32, x, tiles, kFewPieces, kFewPlaces, kLeast, s);
     };
-    if (most <= kFewRows) return few(a, rows / 16 + c.n_seqs, rows / 32 + c.n_seqs);
+    if (most <= kFewRows || (rows / 32 + c.n_seqs) * pool.n_kv_heads <= kFewTiles) return few(a, rows / 16 + c.n_seqs, rows / 32 + c.n_seqs);
     // Up to 32 requests all go to attention_many, of more the short ones to a launch of attention_few (an empty one costs 4 µs).  One launch
     // and two: four of 24 to 39 tokens 11 and 18 µs, 13 of 1 to 7 (eight query heads per key head) 18 and 30, 15 of one token behind 4000 and one
     // of 512 62 and 65, 32 of 1 to 300 behind 100 to 3000 171 and 180; 63 of one token behind 4000 and one of 256 807 and 760.
@@ -1258,7 +1262,7 @@ hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_
                                    : launch<64>(attention_many<8, 4, 1, 1, 2, 2>, 512, Many<8, 4, 1, 1, 2>::kLds, done64, longer, rows / 64 + c.n_seqs, kManyPieces, kManyPlaces, kLeastMany, s);
     if (e != hipSuccess || all) return e;
     a.most_rows = kFewRows;
-    const long long tiles = (long long)c.n_seqs * (kFewRows / 32);
+    const long long tiles = (long long)c.n_seqs * (kFewRows / 32);  // (32 rows each)
     return few(a, 0, tiles < rows / 32 + c.n_seqs ? tiles : rows / 32 + c.n_seqs);
 }
 

@@ -509,6 +509,31 @@ def test_tall_tiles_put_together(workspace, heads, requests):
     assert torch.equal(got, b.run(workspace))
 
 
+@gpu
+@pytest.mark.parametrize("heads,kv_heads,requests", [(80, 80, [(100, 120), (0, 50)]), (200, 200, [(100, 120), (0, 50)]), (32, 4, [(100, 400), (0, 150)]),
+                                                     (60, 60, [(1000, 120)] + [(0, 1)] * 5), (60, 60, [(1000, 120)] + [(0, 1)] * 7), (32, 4, [(2500, 33), (0, 500)])])
+def test_tall_tiles(workspace, heads, kv_heads, requests):
+    """Tiles of 128, 256 and 64 rows, the keys of one request divided in the last three: pages that are not there, infinities that some rows see, in
+    place of the queries."""
+    b = Batch(torch.bfloat16, heads, kv_heads, 16, requests)
+    want = b.run(workspace)
+    b.check(want)
+    t = b.table.copy()
+    t[0, [0, 5, 6]] = [-1, b.k.shape[0], 2 ** 31 - 1]
+    t[1, 0] = -5
+    b.check(b.run(workspace, table=t), table=t)
+    c = Batch(torch.bfloat16, heads, kv_heads, 16, requests)
+    cached, new = requests[0]
+    pos = cached + new // 2
+    c.v[int(c.table[0, pos // 16]), :, pos % 16, 7] = float("inf")
+    got = c.run(workspace)
+    sees = slice(new // 2, new)
+    assert (got[sees, :, 7] == float("inf")).all()
+    got[sees, :, 7] = want[sees, :, 7]
+    assert torch.equal(got, want)
+    assert b.run(workspace, out=b.q) is b.q and torch.equal(b.q, want)
+
+
 def many_requests(n, most_cached, most_new, seed):
     rng = np.random.default_rng(seed)
     requests = [(int(rng.integers(0, most_cached + 1)), int(rng.integers(0, most_new + 1))) for _ in range(n)]
@@ -1083,7 +1108,9 @@ def small_stage(dtype, max_rows, w4_expanded=False):
     ("f32", [[37, 5, 0, 16], [1, 3, 20, 1], [1, 1, 1, 1]]),
     ("bf16", [[37, 5, 0, 16], [1, 3, 20, 1], [1, 1, 1, 1], [5, 5, 1, 5]]),     # 58, 25, 4 and 16 rows
     ("bf16", [[300, 0, 140, 64], [1, 200, 1, 1]]),
-    ("bf16", [[900, 20, 0, 40], [1, 130, 700, 1], [1, 1, 1, 5]]),             # keys divided among workgroups, in both kernels
+    ("bf16", [[900, 20, 0, 40], [1, 130, 700, 1], [1, 1, 1, 5]]),             # keys divided among workgroups
+    ("bf16", [[2000, 20, 0, 40], [1, 5, 1, 1]]),                              # tiles of 64 rows
+    ("bf16", [[2700, 20, 0, 40], [1, 5, 1, 1]]),                              # and of 128
     ("w4", [[37, 5, 0, 16], [1, 3, 7, 1], [1, 1, 1, 1]]),
     ("w4+bf16", [[90, 5, 0, 16], [1, 1, 1, 1]])])
 def test_a_stage_over_pages(dtype, steps, workspace):
