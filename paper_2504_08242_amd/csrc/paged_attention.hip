@@ -1170,6 +1170,7 @@ namespace {
 // tiles) 34 / 32; 512 tokens behind 1536 (544 tiles) 33 / 33; 20 requests of 128 rows behind 300 to 1000 (2560 tiles) 81 / 74.
 constexpr int kFewRows = 96;
 constexpr int kFewTiles = 512;
+constexpr int kShortRows = 32;
 // Pieces: two workgroups per CU (one token behind 8192 27.4 µs with 768, 27.0 with 512 as with 192 of eight waves), three of
 // eight waves for four CUs (16 requests behind 10 to 8000 on 8 heads 28 µs, with 256 pieces 36).
 constexpr int kFewPieces = 512, kWidePieces = 192;
@@ -1245,12 +1246,12 @@ hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_
                           : launch<32>(attention_few<32, 4>, 256, Few<32, 4>::kLds, done32, x, tiles, kFewPieces, kFewPlaces, kLeast, s);
     };
     if (most <= kFewRows || (rows / 32 + c.n_seqs) * pool.n_kv_heads <= kFewTiles) return few(a, rows / 16 + c.n_seqs, rows / 32 + c.n_seqs);
-    // Up to 32 requests all go to attention_many, of more the short ones to a launch of attention_few (an empty one costs 4 µs).  One launch
-    // and two: four of 24 to 39 tokens 11 and 18 µs, 13 of 1 to 7 (eight query heads per key head) 18 and 30, 15 of one token behind 4000 and one
-    // of 512 62 and 65, 32 of 1 to 300 behind 100 to 3000 171 and 180; 63 of one token behind 4000 and one of 256 807 and 760.
+    // Up to 32 requests all go to attention_many, of more those of up to 32 rows to a launch of attention_few (an empty one costs 4 µs).  One
+    // launch and two: 15 requests of one token behind 4000 and one of 512 61 and 65 µs, 32 of 1 to 300 behind 100 to 3000 171 and 180, 60 of one
+    // behind 2000 and four of 300 142 and 160; 63 of one behind 1000 and one of 512 76 and 66, 63 behind 4000 and one of 256 804 and 760.
     const bool all = c.n_seqs <= 32;
     Attention longer = a;
-    longer.least_rows = all ? 0 : kFewRows + 1;
+    longer.least_rows = all ? 0 : kShortRows + 1;
     // Tiles of 256, 128 or 64 rows, by how many of 256 there are at most.  In µs, tiles of 256 / 128 / 64 rows; first the number of tiles of 256:
     //   1280 (four prompts, 40 heads) 292 / 320 / 458;  520 (16384 tokens, 8 heads) 542 / 594 / 782;  384 (2900 tokens, 32 heads) 100 / 104 / 141;
     //   360 (2048 tokens, 40 heads) 78 / 76 / 101;  320 (three chunks, 40 heads) 64 / 55 / 74;  288 (2048 tokens, 32 heads) 66 / 57 / 81;  264 (2048 behind
@@ -1261,9 +1262,8 @@ hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_
                    : groups >= 112 ? launch<128>(attention_many<8, 2, 2, 1, 2, 2>, 512, Many<8, 2, 2, 1, 2>::kLds, done128, longer, rows / 128 + c.n_seqs, kManyPieces, kManyPlaces, kLeastMany, s)
                                    : launch<64>(attention_many<8, 4, 1, 1, 2, 2>, 512, Many<8, 4, 1, 1, 2>::kLds, done64, longer, rows / 64 + c.n_seqs, kManyPieces, kManyPlaces, kLeastMany, s);
     if (e != hipSuccess || all) return e;
-    a.most_rows = kFewRows;
-    const long long tiles = (long long)c.n_seqs * (kFewRows / 32);  // (32 rows each)
-    return few(a, 0, tiles < rows / 32 + c.n_seqs ? tiles : rows / 32 + c.n_seqs);
+    a.most_rows = kShortRows;  // (one tile each)
+    return few(a, 0, c.n_seqs);
 }
 
 }  // namespace jup
