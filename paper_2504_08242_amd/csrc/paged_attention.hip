@@ -328,7 +328,7 @@ __device__ __forceinline__ bool row_not_finite(const char* row) {
 // arrives last adds them in the order of the pieces (the result does not depend on who that is) and writes the rows.  Nobody
 // waits.  Half a wave has a row, a lane 16 bytes of it: whole lines go to memory and back (a few bytes at 32-byte steps, as the sums lie
 // in the registers, are a partial write each).  One CU takes 20 GB/s out of memory in loads of 8 bytes per lane: with 16 bytes, and no
-// branches between the loads, 88 rows behind 8200 take 42 µs instead of 65, 300 tokens behind 6000 29 instead of 41.
+// branches between the loads, 300 tokens behind 6000 on 8 heads, in tiles of 64 rows, took 29 µs instead of 41.
 
 // Accesses of 16 bytes that are performed chip-wide, as load_coherent2() and store_coherent2() of 8 are.
 constexpr int kCoherent = 16;  // of the buffer builtins: past L2
@@ -1174,12 +1174,11 @@ constexpr int kShortRows = 32;
 // Pieces: two workgroups per CU (one token behind 8192 27.4 µs with 768, 27.0 with 512 as with 192 of eight waves), three of
 // eight waves for four CUs (16 requests behind 10 to 8000 on 8 heads 28 µs, with 256 pieces 36).
 constexpr int kFewPieces = 512, kWidePieces = 192;
-// Key tiles that are worth a piece.  One token behind 576 (19 tiles) takes 10.4 µs whole and 12.3 in two pieces, behind 2048 14.3 in pieces of 24
-// tiles and 12.9 in pieces of 16; 48 rows behind 1300 take 24.2, 21.3 and 20.2 in pieces of 24, 16 and 12; 88 rows behind 8200 42 in all of these,
-// 47 in pieces of 8.
-constexpr int kLeast = 20, kLeastMany = 16;
-// A workgroup per CU, less what the longest piece may be longer than the average: 300 tokens behind 6000 on 8 heads 29 µs (with 256 pieces half as much
-// again).
+// Key tiles that are worth a piece.  One token behind 576 (19 tiles) takes 10.3 µs whole and 12.3 in two pieces; behind 2048 14.3 in pieces of
+// 24 tiles, 12.8 in pieces of 20 or 16; 48 rows behind 1300 15.9, 14.1 and 14.1; 60 rows behind 400 11.1 whole, 13.3 in pieces of 12.
+constexpr int kLeast = 20;
+// A workgroup per CU, less what the longest piece may be longer than the average.  With 128, 222 and 333: three requests of 40 to 500 tokens
+// behind 2000 to 9000 86, 84 and 102 µs, five of 100 to 300 behind 10 to 20000 150, 122 and 130.
 constexpr int kManyPieces = 222;
 constexpr int kMostSplitHeads = 64;  // (more heads than that fill the chip without dividing keys)
 constexpr int kFewPlaces = 2 * (kFewPieces + kMostSplitHeads), kManyPlaces = 4 * (kManyPieces + kMostSplitHeads);
@@ -1258,9 +1257,9 @@ hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_
     //   8192, 32 heads on 8) 317 / 333 / 438;  160 (1024 tokens) 42 / 31 / 32;  128 (768 behind 1536) 54 / 61 / 57;  96 (512 behind 1536) 43 / 36 / 33.
     const long long groups = (rows / 256 + c.n_seqs) * pool.n_kv_heads;
     static bool done256[64], done128[64], done64[64];
-    hipError_t e = groups >= 384   ? launch<256>(attention_many<8, 1, 2, 2, 2, 2>, 512, Many<8, 1, 2, 2, 2>::kLds, done256, longer, rows / 256 + c.n_seqs, kManyPieces, kManyPlaces, kLeastMany, s)
-                   : groups >= 112 ? launch<128>(attention_many<8, 2, 2, 1, 2, 2>, 512, Many<8, 2, 2, 1, 2>::kLds, done128, longer, rows / 128 + c.n_seqs, kManyPieces, kManyPlaces, kLeastMany, s)
-                                   : launch<64>(attention_many<8, 4, 1, 1, 2, 2>, 512, Many<8, 4, 1, 1, 2>::kLds, done64, longer, rows / 64 + c.n_seqs, kManyPieces, kManyPlaces, kLeastMany, s);
+    hipError_t e = groups >= 384   ? launch<256>(attention_many<8, 1, 2, 2, 2, 2>, 512, Many<8, 1, 2, 2, 2>::kLds, done256, longer, rows / 256 + c.n_seqs, kManyPieces, kManyPlaces, kLeast, s)
+                   : groups >= 112 ? launch<128>(attention_many<8, 2, 2, 1, 2, 2>, 512, Many<8, 2, 2, 1, 2>::kLds, done128, longer, rows / 128 + c.n_seqs, kManyPieces, kManyPlaces, kLeast, s)
+                                   : launch<64>(attention_many<8, 4, 1, 1, 2, 2>, 512, Many<8, 4, 1, 1, 2>::kLds, done64, longer, rows / 64 + c.n_seqs, kManyPieces, kManyPlaces, kLeast, s);
     if (e != hipSuccess || all) return e;
     a.most_rows = kShortRows;  // (one tile each)
     return few(a, 0, c.n_seqs);
