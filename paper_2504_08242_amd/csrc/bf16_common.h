@@ -102,8 +102,10 @@ __device__ inline float2 load_coherent2(const float* p) {
 __device__ inline int arrive_coherent(int* counter) {
     return __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-// Waits until this wave's stores have been performed (a coherent store is performed when it is visible chip-wide).
-__device__ inline void wait_stores_performed() { __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup"); }
+// Waits until this wave's stores have been performed (a coherent store is performed when it is visible chip-wide).  Every wave that
+// stored calls it, in front of the barrier behind which its workgroup arrives.  The instruction itself: a workgroup-scope fence waits for
+// LDS alone, and without the wait the arrival can overtake the stores it announces, on their way to other channels than the counter's.
+__device__ inline void wait_stores_performed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // Sum over the wave, in every lane: pairs 32, 16, 8, 4, 2 and 1 lanes apart, in registers.
 template <int DPP>
