@@ -367,15 +367,15 @@ __device__ __forceinline__ void join_rows(const Attention& a, const Work& w, int
             float top = m[x];
 #pragma unroll
             for (int p = 0; p < PC; ++p) top = fmaxf(top, __uint_as_float(stat[x][p][0]));
-            if (top == -INFINITY) top = 0.f;
-            const float back = __builtin_amdgcn_exp2f(m[x] - top);
+            const float ref = top == -INFINITY ? 0.f : top;  // (nothing seen so far: the maximum stays open)
+            const float back = __builtin_amdgcn_exp2f(m[x] - ref);
             l[x] *= back;
             acc[x] *= back;
 #pragma unroll
             for (int p = 0; p < PC; ++p) {
                 const float sum = __uint_as_float(stat[x][p][1]);
                 if (p0 + p < w.pieces && sum != 0.f) {  // (0: a piece this row sees nothing of)
-                    const float f = __builtin_amdgcn_exp2f(__uint_as_float(stat[x][p][0]) - top);
+                    const float f = __builtin_amdgcn_exp2f(__uint_as_float(stat[x][p][0]) - ref);
                     l[x] += sum * f;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[x][e] += __uint_as_float(val[x][p][e]) * f;

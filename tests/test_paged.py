@@ -534,6 +534,19 @@ def test_tall_tiles(workspace, heads, kv_heads, requests):
     assert b.run(workspace, out=b.q) is b.q and torch.equal(b.q, want)
 
 
+@gpu
+@pytest.mark.parametrize("heads,kv_heads,requests,gone", [(1, 1, [(13000, 1)], 11500), (1, 1, [(9000, 30)], 6400), (32, 4, [(6400, 33), (0, 500)], 6000)])
+def test_old_pages_that_were_dropped(workspace, heads, kv_heads, requests, gone):
+    """Divided keys whose first pieces hold nothing (more of them than are put together at a time), and scores far below 0 behind them."""
+    b = Batch(torch.bfloat16, heads, kv_heads, 16, requests)
+    b.q += 4.0
+    b.k -= 4.0
+    b.table[0, :gone // 16] = -1
+    got = b.run(workspace)
+    b.check(got)
+    assert got[:requests[0][1]].any()
+
+
 def many_requests(n, most_cached, most_new, seed):
     rng = np.random.default_rng(seed)
     requests = [(int(rng.integers(0, most_cached + 1)), int(rng.integers(0, most_new + 1))) for _ in range(n)]
