@@ -133,6 +133,16 @@ def _table(t, at, n):
     return t.data_ptr(), width, stride
 
 
+def _overlap(rows, heads, dim, row, head):
+    """Whether two heads of a tensor with these strides (0 where there is one entry) share an element."""
+    if (row < dim and rows > 1) or (head < dim and heads > 1):
+        return True
+    if rows == 1 or heads == 1 or row >= (heads - 1) * head + dim or head >= (rows - 1) * row + dim:
+        return False
+    # neither lies whole between two of the other: the rows next to h heads further on
+    return any(abs(h * head - r * row) < dim for h in range(1, heads) for r in (h * head // row, h * head // row + 1) if r < rows)
+
+
 def _heads(name, t, dtype, at, rows, heads, dim, written=False):
     """(address, row stride, head stride) of a tensor [rows, heads, dim] whose heads are contiguous."""
     if t.dtype is not dtype or t.get_device() != at or t.shape != (rows, heads, dim):
@@ -142,7 +152,7 @@ def _heads(name, t, dtype, at, rows, heads, dim, written=False):
         raise ValueError(f"elements of a head of {name} must be neighbours")
     # (the stride of an axis of one entry is not used, and says nothing)
     row, head = row if rows > 1 else 0, head if heads > 1 else 0
-    if written and ((row < dim and rows > 1) or (head < dim and heads > 1)) and t.numel():
+    if written and t.numel() and _overlap(rows, heads, dim, row, head):
         raise ValueError(f"heads of {name} overlap")
     return t.data_ptr(), row, head
 

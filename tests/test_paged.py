@@ -164,6 +164,22 @@ def test_the_front_end_refuses_tensors_that_do_not_fit():
         jp.verify(i, p[0, 0], i, i, i, None)
 
 
+@pytest.mark.parametrize("shape,strides,fits", [
+    ((5, 3, 8), (24, 8, 1), True), ((5, 3, 8), (8, 40, 1), True), ((5, 3, 8), (100, 9, 1), True), ((5, 1, 8), (8, 0, 1), True), ((1, 3, 8), (0, 8, 1), True),
+    ((2, 3, 8), (8, 16, 1), True),                                                # heads between the rows of another
+    ((5, 3, 8), (8, 8, 1), False), ((5, 3, 8), (23, 8, 1), False), ((5, 3, 8), (8, 39, 1), False), ((5, 3, 8), (0, 8, 1), False), ((5, 3, 8), (24, 7, 1), False),
+    ((3, 3, 8), (8, 16, 1), False), ((4, 40, 8), (50, 10, 1), False), ((2, 7, 8), (60, 10, 1), False), ((2, 6, 8), (58, 10, 1), True)])
+def test_results_whose_heads_overlap_are_refused(shape, strides, fits):
+    t = torch.empty(10000).as_strided(shape, strides)
+    offsets = [r * strides[0] + h * strides[1] + i for r in range(shape[0]) for h in range(shape[1]) for i in range(shape[2])]
+    assert fits == (len(set(offsets)) == len(offsets))
+    if fits:
+        jp._heads("out", t, torch.float32, -1, *shape, written=True)
+    else:
+        with pytest.raises(ValueError, match="overlap"):
+            jp._heads("out", t, torch.float32, -1, *shape, written=True)
+
+
 @gpu
 def test_the_front_end_refuses_tensors_that_do_not_fit_on_the_gpu(workspace):
     k = torch.zeros((5, 2, 16, 128), dtype=torch.bfloat16, device=DEV)
