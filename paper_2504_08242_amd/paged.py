@@ -12,8 +12,9 @@ whose last is 1, the same for both), a block table an int32 tensor [n_requests, 
     verdict = verify(tokens, target_probs, step.row_start, u_accept, u_sample, workspace, lengths=lengths)
 
 Argument marshalling only: every operator is a HIP kernel of the library.  The calls are asynchronous on ``stream`` (default: the
-current one of the tensors' device) and read nothing back.  ``ValueError`` for tensors that do not fit together,
-``binding.JupiterError`` for what the library refuses.
+current one of the tensors' device) and read nothing back.  On another stream than the current one, that stream waits for what made
+the tensors that are handed in, and the caller keeps them until the call is done; results that the call makes itself are that stream's.
+``ValueError`` for tensors that do not fit together, ``binding.JupiterError`` for what the library refuses.
 """
 import collections
 import ctypes
@@ -175,16 +176,25 @@ def _pool(k_pool, v_pool):
 _current_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice  # (the tensors are on the GPU: it is initialised)
 
 
-def _call(fn, at, stream, made, *structs):
-    """The call on `stream`, with the tensors' device current; made: the tensor that was allocated for it, or None."""
+def _new(stream, at, allocate):
+    """A result that the call makes itself.  It is written on `stream`, so its memory is that stream's: what another stream has freed may
+    still be written there by work that `stream` does not wait for.  The current stream, whose caller reads it, holds it too."""
+    if stream is None:
+        return allocate()
+    with torch.cuda.stream(stream):
+        t = allocate()
+    t.record_stream(torch.cuda.current_stream(at))
+    return t
+
+
+def _call(fn, at, stream, *structs):
+    """The call on `stream`, with the tensors' device current."""
     if stream is None:
         handle = _current_stream(at)
     else:
         if stream.device.index != at:
             raise ValueError(f"the stream is on {stream.device}, the tensors on cuda:{at}")
         handle = stream.cuda_stream
-        if made is not None:
-            made.record_stream(stream)
     if at == _current_device():
         status = fn(*structs, handle)
     else:
@@ -227,13 +237,13 @@ def extend(lengths, n_new, owned, table, free_blocks, free_count, page_size, max
     tables, width, stride = _table(table, at, n)
     free = (_ints("free_blocks", free_blocks, at, n_free), _ints("free_count", free_count, at, 1))
     sizes = [n + 1, max_rows, max_rows, 1] if in_place else [n + 1, max_rows, max_rows, 1, n, n, 1]
-    made = lengths.new_empty(sum(sizes))
+    made = _new(stream, at, lambda: lengths.new_empty(sum(sizes)))
     row_start, positions, slots, status, *new = made.split_with_sizes(sizes)
     new_lengths, new_owned, new_count = (lengths, owned, free_count) if in_place else new
     base = made.data_ptr()
     ends = base + 4 * (n + 1), base + 4 * (n + 1 + max_rows), base + 4 * (n + 1 + 2 * max_rows)
     after = (inputs[0], inputs[2], free[1]) if in_place else (ends[2] + 4, ends[2] + 4 * (n + 1), ends[2] + 4 * (2 * n + 1))
-    _call(_lib().jup_paged_extend, at, stream, made,
+    _call(_lib().jup_paged_extend, at, stream,
           _pack_extend(n, int(page_size), width, n_free, max_rows, stride, *inputs, tables, *free, base, ends[0], ends[1], *after, ends[2]))
     return Step(row_start, positions, slots, new_lengths, new_owned, new_count, status)
 
@@ -254,18 +264,18 @@ def append(k, v, slots, k_pool, v_pool, positions=None, rope_theta=None, q=None,
         if positions is None or not rope_theta > 0:
             raise ValueError("rope_theta must be positive, and goes with positions")
         theta, positions_at = rope_theta, _ints("positions", positions, at, rows)
-    made, heads, q_at, q_strides, out_at, out_strides = None, 0, 0, (0, 0), 0, (0, 0)
+    heads, q_at, q_strides, out_at, out_strides = 0, 0, (0, 0), 0, (0, 0)
     if q is not None:
         heads = q.shape[1] if q.dim() == 3 else -1
         q_at, *q_strides = _heads("q", q, dtype, at, rows, heads, dim)
         if q_out is None:
-            q_out = made = torch.empty_like(q, memory_format=_CONTIGUOUS)
-            out_at, out_strides = made.data_ptr(), (heads * dim, dim)
+            q_out = _new(stream, at, lambda: torch.empty_like(q, memory_format=_CONTIGUOUS))
+            out_at, out_strides = q_out.data_ptr(), (heads * dim, dim)
         else:
             out_at, *out_strides = _heads("q_out", q_out, dtype, at, rows, heads, dim, written=True)
     elif q_out is not None:
         raise ValueError("q_out goes with q")
-    _call(_lib().jup_paged_append, at, stream, made, pool,
+    _call(_lib().jup_paged_append, at, stream, pool,
           _pack_append(rows, heads, q_at, k_at, v_at, out_at, *q_strides, *k_strides, *v_strides, *out_strides, positions_at, slots_at, theta))
     return q_out
 
@@ -280,14 +290,13 @@ def attention(q, k_pool, v_pool, table, row_start, lengths, max_new, workspace=N
         raise ValueError("q must be a tensor [rows, n_heads, head_dim]")
     rows, heads = q.shape[0], q.shape[1]
     q_at, *q_strides = _heads("q", q, dtype, at, rows, heads, dim)
-    made = None
     if out is None:
-        out = made = torch.empty_like(q, memory_format=_CONTIGUOUS)
-        out_at, out_strides = made.data_ptr(), (heads * dim, dim)
+        out = _new(stream, at, lambda: torch.empty_like(q, memory_format=_CONTIGUOUS))
+        out_at, out_strides = out.data_ptr(), (heads * dim, dim)
     else:
         out_at, *out_strides = _heads("out", out, dtype, at, rows, heads, dim, written=True)
     tables, width, stride = _table(table, at, n)
-    _call(_lib().jup_paged_attention, at, stream, made, pool,
+    _call(_lib().jup_paged_attention, at, stream, pool,
           _pack_attention(n, rows, heads, int(max_new), width, stride, q_at, out_at, *q_strides, *out_strides,
                           _ints("row_start", row_start, at, n + 1), _ints("lengths", lengths, at, n), tables,
                           1.0 / math.sqrt(dim) if scale is None else scale,
@@ -305,11 +314,7 @@ def prefill(stage, hidden_in, step, k_pools, v_pools, table, max_new, workspace=
         raise ValueError("a stage without layers has no pools")
     packed, dtype, at, _, _ = _pool(k_pools[0], v_pools[0])
     n, rows, width = step.lengths.numel(), hidden_in.shape[0], stage.cfg["d_model"]
-    if hidden_out is None:
-        hidden_out = made = torch.empty_like(hidden_in)
-    else:
-        made = None
-    for name, t in (("hidden_in", hidden_in), ("hidden_out", hidden_out)):
+    for name, t in (("hidden_in", hidden_in), ("hidden_out", hidden_in if hidden_out is None else hidden_out)):
         if t.dtype is not dtype or t.get_device() != at or t.shape != (rows, width) or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous {dtype} tensor [{rows}, {width}] on cuda:{at}, not {t.dtype} {list(t.shape)} on {t.device}")
     if step.positions.numel() < rows or step.slots.numel() < rows:
@@ -319,8 +324,10 @@ def prefill(stage, hidden_in, step, k_pools, v_pools, table, max_new, workspace=
     batch = _Batch(_Pool.from_buffer_copy(packed), k_pools.stride(0), n, int(max_new), table_width, stride, _ints("row_start", step.row_start, at, n + 1),
                    _ints("lengths", step.lengths, at, n), tables, _ints("positions", step.positions, at, step.positions.numel()),
                    _ints("slots", step.slots, at, step.slots.numel()), *scratch)
+    if hidden_out is None:
+        hidden_out = _new(stream, at, lambda: torch.empty_like(hidden_in))
     fn = _lib().jup_stage_prefill_paged
-    _call(lambda handle: fn(stage.handle, hidden_in.data_ptr(), rows, ctypes.byref(batch), hidden_out.data_ptr(), handle), at, stream, made)
+    _call(lambda handle: fn(stage.handle, hidden_in.data_ptr(), rows, ctypes.byref(batch), hidden_out.data_ptr(), handle), at, stream)
     return hidden_out
 
 
@@ -351,8 +358,9 @@ def verify(tokens, target_probs, row_start, u_accept, u_sample, workspace, draft
     vocab = target_probs.shape[1]
     target, target_stride = _probs("target_probs", target_probs, dtype, at, rows, vocab)
     draft, draft_stride = (0, 0) if draft_probs is None else _probs("draft_probs", draft_probs, dtype, at, rows, vocab)
+    tokens_at = _ints("tokens", tokens, at, rows)
     sizes = [n, n, rows] if lengths is None or in_place else [n, n, rows, n]
-    made = tokens.new_empty(sum(sizes))
+    made = _new(stream, at, lambda: tokens.new_empty(sum(sizes)))
     n_accepted, next_token, emitted, *new = made.split_with_sizes(sizes)
     base = made.data_ptr()
     lengths_at = after_at = 0
@@ -362,8 +370,8 @@ def verify(tokens, target_probs, row_start, u_accept, u_sample, workspace, draft
         new_lengths = lengths
         if not in_place:
             new_lengths, after_at = new[0], base + 4 * (2 * n + rows)
-    _call(_lib().jup_verify_drafts, at, stream, made,
-          _pack_verify(n, rows, vocab, _DTYPES[dtype], _ints("tokens", tokens, at, rows), _ints("row_start", row_start, at, n + 1), target,
+    _call(_lib().jup_verify_drafts, at, stream,
+          _pack_verify(n, rows, vocab, _DTYPES[dtype], tokens_at, _ints("row_start", row_start, at, n + 1), target,
                        draft, target_stride, draft_stride, _uniforms("u_accept", u_accept, at, rows), _uniforms("u_sample", u_sample, at, n),
                        base, base + 4 * n, base + 8 * n, lengths_at, after_at, *_scratch(workspace, at, stream)))
     return Verdict(n_accepted, next_token, emitted, new_lengths)

@@ -834,6 +834,39 @@ def test_another_stream(workspace):
 
 
 @gpu
+def test_results_made_for_another_stream_are_not_written_by_this_one(workspace):
+    """Memory that the current stream has freed, with its work on it still ahead, is not what a call on another stream gets."""
+    b = Batch(torch.bfloat16, 4, 2, 16, [(300, 3), (50, 1)])
+    lengths, table, at = ints(b.lengths), torch.from_numpy(b.table).to(DEV, torch.int32), ints(b.row_start)
+    n_new, owned, free, count = ints(b.new), ints([b.table.shape[1]] * 2), ints([]), ints([0])
+    slots, positions = torch.full((4,), -1, dtype=torch.int32, device=DEV), ints([5, 6, 7, 8])
+    probs, u = torch.softmax(torch.randn((4, 100), device=DEV), -1), torch.rand(4, device=DEV)
+    tokens, new_k = ints([3, 1, 4, 1]), b.q[:, :2].contiguous()
+    cfg, stage, _ = small_stage("bf16", 8)
+    pools = [torch.zeros((2, 4, 8, 16, 128), dtype=torch.bfloat16, device=DEV) for _ in "kv"]
+    hidden, step = torch.randn((4, 1024), device=DEV).bfloat16(), jp.Step(ints([0, 4]), ints([0, 1, 2, 3]), ints([0, 1, 2, 3]), ints([4]), None, None, None)
+    stage_table, space = ints([1])[None], jp.Workspace(DEV)
+    calls = [lambda s: [jp.attention(b.q, b.k, b.v, table, at, lengths, 3, space, stream=s)],
+             lambda s: [jp.append(new_k, new_k, slots, b.k, b.v, positions=positions, rope_theta=1e4, q=b.q, stream=s)],
+             lambda s: list(jp.extend(lengths, n_new, owned, table, free, count, 16, 4, stream=s)),
+             lambda s: list(jp.verify(tokens, probs, at, u, u[:2].clone(), space, lengths=lengths, stream=s)),
+             lambda s: [jp.prefill(stage, hidden, step, *pools, stage_table, 4, space, stream=s)]]
+    side, x = torch.cuda.Stream(), torch.randn((4096, 4096), device=DEV)
+    for call in calls:
+        want = [t.clone() for t in call(None)]
+        freed = [torch.empty(t.untyped_storage().nbytes(), dtype=torch.uint8, device=DEV) for t in call(None)[:1] for _ in range(20)]
+        torch.cuda.synchronize()
+        for _ in range(30):
+            x = x @ x * 1e-2
+        for f in freed:
+            f.fill_(77)
+        del f, freed
+        got = call(side)
+        torch.cuda.synchronize()
+        assert all(torch.equal(g, w) for g, w in zip(got, want))
+
+
+@gpu
 def test_two_streams_at_once():
     """Calls that overlap, each stream with a workspace of its own."""
     batches = [Batch(torch.bfloat16, 4, 2, 16, r, seed=s) for s, r in enumerate(([(3000, 2), (900, 1)], [(2500, 70), (40, 3)]))]
