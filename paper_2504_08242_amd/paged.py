@@ -317,6 +317,8 @@ def prefill(stage, hidden_in, step, k_pools, v_pools, table, max_new, workspace=
     for name, t in (("hidden_in", hidden_in), ("hidden_out", hidden_in if hidden_out is None else hidden_out)):
         if t.dtype is not dtype or t.get_device() != at or t.shape != (rows, width) or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous {dtype} tensor [{rows}, {width}] on cuda:{at}, not {t.dtype} {list(t.shape)} on {t.device}")
+    if stage.workspace.get_device() != at:
+        raise ValueError(f"the stage is on {stage.workspace.device}, the tensors on cuda:{at}")
     if step.positions.numel() < rows or step.slots.numel() < rows:
         raise ValueError(f"the step has positions of {step.positions.numel()} rows, hidden_in {rows}")
     tables, table_width, stride = _table(table, at, n)

@@ -6,6 +6,7 @@ the exponentials a few 2^-23.  Rotated rows: one rounding, of a result whose fp3
 """
 import ctypes
 import random
+import types
 
 import numpy as np
 import pytest
@@ -1301,6 +1302,16 @@ def test_a_stage_over_pages_refuses(workspace):
     refused(L.jup_stage_prefill_paged(stage.handle, FAKE + 2, 2, ctypes.byref(batch), FAKE, None), "aligned")
     refused(L.jup_stage_prefill_paged(stage.handle, None, 2, ctypes.byref(batch), FAKE, None), "NULL")
     refused(L.jup_stage_prefill_paged(stage.handle, FAKE, 2, None, FAKE, None), "batch")
+
+
+@gpu
+def test_a_stage_on_another_device_is_refused(workspace):
+    k = torch.zeros((2, 4, 8, 16, 128), dtype=torch.bfloat16, device=DEV)
+    x, table = torch.zeros((4, 1024), dtype=torch.bfloat16, device=DEV), torch.zeros((1, 2), dtype=torch.int32, device=DEV)
+    step = jp.Step(ints([0, 4]), ints([0, 1, 2, 3]), ints([0, 1, 2, 3]), ints([4]), None, None, None)
+    elsewhere = types.SimpleNamespace(cfg=dict(n_layers=2, d_model=1024), handle=None, workspace=torch.empty(1, dtype=torch.uint8))
+    with pytest.raises(ValueError, match="stage"):
+        jp.prefill(elsewhere, x, step, k, k, table, 4, workspace)
 
 
 def test_a_missing_stage_is_refused():
