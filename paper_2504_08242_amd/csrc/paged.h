@@ -16,6 +16,15 @@ constexpr size_t kVerifyBytes = (size_t)JUP_PAGED_MAX_SEQS * kVerifySlices * 8;
 // page_size is a power of two
 inline int log2_of(int page_size) { return __builtin_ctz((unsigned)page_size); }
 
+// A launch of 2^32 threads or more along one axis runs some of its workgroups only, and reports no error: many workgroups lie in lines of 2^20.
+// There may be more of them than asked for.
+constexpr int kLineBits = 20;
+inline dim3 grid_of(long long blocks) {
+    const long long line = 1ll << kLineBits;
+    return blocks <= line ? dim3((unsigned)blocks) : dim3((unsigned)line, (unsigned)((blocks + line - 1) / line));
+}
+__device__ __forceinline__ unsigned block_number() { return blockIdx.y << kLineBits | blockIdx.x; }
+
 // ---- tables and append (paged_tables.hip) -------------------------------------------------------------------------
 hipError_t launch_paged_extend(const jup_paged_extend_t& a, hipStream_t s);
 hipError_t launch_paged_append(const jup_paged_pool_t& pool, const jup_paged_append_t& a, hipStream_t s);

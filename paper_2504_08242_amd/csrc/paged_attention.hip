@@ -229,7 +229,7 @@ __device__ bool find_work(const Attention& a, int item, int least, Work& w) {
     w.tile = r.tiles - 1 - nth;
     w.piece = item - nth * most;
     w.slot = slots_before + nth * most;
-    const int last_token = min(a.group.of(min((w.tile + 1) * R, r.tokens * (int)a.group.d) - 1), r.tokens - 1);
+    const int last_token = min(a.group.of(w.tile * R + min(R, r.tokens * (int)a.group.d - w.tile * R) - 1), r.tokens - 1);
     w.keys = r.keys_of(a, last_token);
     const int key_tiles = (w.keys + kKT - 1) / kKT;
     w.pieces = pieces_of(key_tiles, chunk);
@@ -465,7 +465,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_few(const Attention args
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & (QW - 1), hh = lane / QW;
     // consecutive workgroups are the heads of a piece: a head's pieces meet on one XCD where the heads are a multiple of 8
-    const int kv_head = (int)(blockIdx.x % (unsigned)args.n_kv_heads), item = (int)(blockIdx.x / (unsigned)args.n_kv_heads);
+    const int kv_head = (int)(block_number() % (unsigned)args.n_kv_heads), item = (int)(block_number() / (unsigned)args.n_kv_heads);
     Work w;
     if (!find_work<QW>(args, item, least, w)) return;
     w.make_uniform();
@@ -780,7 +780,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const Attention a
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 31, hh = lane >> 5;
     const int part = wave % KP, r_wave = wave / KP * 32;  // this wave's keys of a step, and its rows
-    const int kv_head = (int)(blockIdx.x % (unsigned)args.n_kv_heads), item = (int)(blockIdx.x / (unsigned)args.n_kv_heads);
+    const int kv_head = (int)(block_number() % (unsigned)args.n_kv_heads), item = (int)(block_number() / (unsigned)args.n_kv_heads);
     Work w;
     if (!find_work<kRows>(args, item, least, w)) return;
     w.make_uniform();
@@ -1098,7 +1098,8 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const Attention a
 // Check mode.  One wave per (row, query head): 64 keys at a time, a lane has a key's score, then D / 64 columns of the output (rounded up).
 __global__ __launch_bounds__(64) void attention_f32(const jup_paged_pool_t pool, const jup_paged_attention_t a, int shift) {
     __shared__ float q[256];
-    const int lane = threadIdx.x, row = blockIdx.x / a.n_heads, head = blockIdx.x - row * a.n_heads;
+    const int lane = threadIdx.x, row = (int)(block_number() / (unsigned)a.n_heads), head = (int)block_number() - row * a.n_heads;
+    if (row >= a.n_rows) return;
     const int D = pool.head_dim, kv_head = head / (a.n_heads / pool.n_kv_heads);
     int lo = 0, hi = a.n_seqs;  // the request: the last one that begins at or before the row
     if (row < a.row_start[0]) return;
@@ -1208,7 +1209,7 @@ hipError_t launch(K* kernel, int threads, int lds, bool* done, Attention a, long
     if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
     a.most_items = (int)items;
     if (a.plan) hipLaunchKernelGGL(plan_work<R>, dim3(1), dim3(1024), 0, s, a, least, (int2*)a.plan);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), lds, s, a, least);
+    hipLaunchKernelGGL(kernel, grid_of(grid), dim3(threads), lds, s, a, least);
     return hipGetLastError();
 }
 
@@ -1217,7 +1218,7 @@ hipError_t launch(K* kernel, int threads, int lds, bool* done, Attention a, long
 hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_attention_t& c, hipStream_t s, int tiled) {
     const int shift = log2_of(pool.page_size);
     if (pool.dtype == JUP_F32) {
-        hipLaunchKernelGGL(attention_f32, dim3((unsigned)c.n_rows * (unsigned)c.n_heads), dim3(64), 0, s, pool, c, shift);
+        hipLaunchKernelGGL(attention_f32, grid_of((long long)c.n_rows * c.n_heads), dim3(64), 0, s, pool, c, shift);
         return hipGetLastError();
     }
     Attention a{};

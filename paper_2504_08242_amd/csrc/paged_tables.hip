@@ -262,7 +262,8 @@ __device__ __forceinline__ void rotate8(const u32x4 lo, const u32x4 hi, const fl
 // 64 elements apart).  Bound by memory: prompts of 365 MB in and out take 69 µs, 5.3 TB/s (a large copy: 4.9 to 5.2).
 __global__ __launch_bounds__(256) void append_bf16(const jup_paged_pool_t pool, const jup_paged_append_t a, int shift, const Turns turns) {
     __shared__ float2 cs[64];
-    const int row = blockIdx.x, tid = threadIdx.x;
+    const int row = (int)block_number(), tid = threadIdx.x;
+    if (row >= a.n_rows) return;
     const bool rotates = a.rope_theta > 0.0f;
     if (rotates && tid < 64) cs[tid] = turn(a.positions[row], turns.per_position[tid]);
     __syncthreads();
@@ -297,7 +298,8 @@ __global__ __launch_bounds__(256) void append_bf16(const jup_paged_pool_t pool, 
 
 // Check mode: a thread per pair.
 __global__ __launch_bounds__(256) void append_f32(const jup_paged_pool_t pool, const jup_paged_append_t a, int shift, const Turns turns) {
-    const int row = blockIdx.x, half = pool.head_dim / 2;
+    const int row = (int)block_number(), half = pool.head_dim / 2;
+    if (row >= a.n_rows) return;
     const bool rotates = a.rope_theta > 0.0f;
     const int position = rotates ? a.positions[row] : 0;
     const int slot = a.slots[row];
@@ -359,9 +361,9 @@ hipError_t launch_paged_append(const jup_paged_pool_t& pool, const jup_paged_app
     }
     const int shift = log2_of(pool.page_size);
     if (pool.dtype == JUP_BF16)
-        hipLaunchKernelGGL(append_bf16, dim3(a.n_rows), dim3(256), 0, s, pool, a, shift, turns);
+        hipLaunchKernelGGL(append_bf16, grid_of(a.n_rows), dim3(256), 0, s, pool, a, shift, turns);
     else
-        hipLaunchKernelGGL(append_f32, dim3(a.n_rows), dim3(256), 0, s, pool, a, shift, turns);
+        hipLaunchKernelGGL(append_f32, grid_of(a.n_rows), dim3(256), 0, s, pool, a, shift, turns);
     return hipGetLastError();
 }
 

@@ -883,6 +883,50 @@ def test_two_streams_at_once():
     assert all(torch.equal(x, y) for run in got for x, y in zip(run, want))
 
 
+@gpu
+def test_more_rows_than_a_launch_has_workgroups_in_a_line():
+    """2^24 rows of two features and more: 2^32 threads if a row had a workgroup of its own in one line of them."""
+    rows = (1 << 24) + 3
+    pools = [torch.zeros((rows // 65536 + 1, 1, 65536, 2), device=DEV) for _ in "kv"]
+    k, v = torch.rand((rows, 1, 2), device=DEV), torch.rand((rows, 1, 2), device=DEV)
+    slots = torch.arange(rows, device=DEV, dtype=torch.int32).flip(0)
+    jp.append(k, v, slots, *pools)
+    for x, pool in zip((k, v), pools):
+        assert torch.equal(pool.view(-1, 2)[:rows], x[:, 0].flip(0)) and not pool.view(-1, 2)[rows:].any()
+
+
+@gpu
+def test_more_rows_and_heads_than_a_launch_has_workgroups_in_a_line():
+    """Check mode has a wave per row and head: 2^26 and more of them."""
+    rows, heads = (1 << 20) + 5, 64
+    q = torch.rand((rows, heads, 2), device=DEV)
+    k, v = torch.zeros((1, 1, 8, 2), device=DEV), torch.rand((1, 1, 8, 2), device=DEV)
+    out = torch.full_like(q, 9.0)
+    jp.attention(q, k, v, ints([0])[None], ints([0, rows]), ints([rows]), rows, scale=1.0, out=out)
+    # (a table of one page of eight: row r sees the first r + 1 positions, the last rows all eight; keys of 0 weigh the same, and sums of
+    # eight numbers below 1 are off by at most 8 x 2^-24)
+    for r in (0, 1, 5, 7, 100, rows // 2, rows - 1):
+        want = v[0, 0, :min(r + 1, 8)].double().mean(0)
+        assert (out[r].double() - want).abs().max() <= 1e-6, r
+    assert ((out[7:] - out[7]).abs() <= 1e-6).all()
+
+
+@gpu
+@pytest.mark.parametrize("max_new", [1, 100])
+def test_more_pieces_of_work_than_a_launch_has_workgroups_in_a_line(workspace, max_new):
+    """2^24 requests times key/value heads, of 256 threads and more each."""
+    n, heads = 16384, 1024
+    gen = torch.Generator().manual_seed(4)
+    q1, k, v = ((torch.randn(shape, generator=gen)).to(DEV, torch.bfloat16) for shape in ((1, heads, 128), (1, heads, 8, 128), (1, heads, 8, 128)))
+    lengths = [1 + i % 8 for i in range(n)]
+    out = torch.full((n, heads, 128), 9.0, dtype=torch.bfloat16, device=DEV)
+    jp.attention(q1.expand(n, heads, 128), k, v, torch.zeros((n, 1), dtype=torch.int32, device=DEV), ints(range(n + 1)), ints(lengths), max_new, workspace, out=out)
+    want, size, most = ref.attention(f64(q1.expand(8, heads, 128)), f64(k), f64(v), np.zeros((8, 1), dtype=np.int64), list(range(9)), lengths[:8], 128 ** -0.5, 8)
+    off = np.abs(f64(out[:8]) - want)
+    assert (off <= (BF16 + (8 + 256 * most + 32) * 2.0 ** -24) * size + BF16 * np.abs(want)).all()
+    assert (out.view(n // 8, 8, heads, 128) == out[:8]).all()
+
+
 # ---- verification ----------------------------------------------------------------------------------------------------------------
 
 
