@@ -51,7 +51,7 @@ typedef struct {
  * with F = *free_count and s the number of pages taken before, the next entry is free_blocks[F - 1 - s].
  *   table           [n_seqs][table_stride], table_width entries used: the taken pages are entered behind the owned[i] first
  *                   entries; all other entries stay as they are
- *   free_blocks     [n_free];  free_count [1]
+ *   free_blocks     [n_free], n_free <= 2^30;  free_count [1]
  *   row_start       out [n_seqs + 1]: prefix sums of n_new
  *   positions       out [max_rows]: position of every row (rows behind the last: 0)
  *   slots           out [max_rows]: block * page_size + place in the block (rows behind the last: -1)
@@ -166,7 +166,8 @@ JUP_API jup_status_t jup_stage_prefill_paged(jup_stage_t *stage, const void *hid
  * the last one, the next token is drawn from w = max(target - draft, 0) there (draft_probs NULL: target without x), or from w = target behind the
  * last draft: the lowest j with w_0 + .. + w_j > u_sample[i] * (w_0 + .. + w_(vocab-1)).  The tokens that come out are then distributed
  * as the target's (uniform u in [0, 1)).  Comparisons and sums are in 64 bits.
- *   target_probs, draft_probs   [n_rows][vocab], rows *_row_stride elements apart; probs_dtype JUP_F32 or JUP_BF16
+ *   target_probs, draft_probs   [n_rows][vocab], n_rows and vocab <= 2^30, rows *_row_stride elements apart; probs_dtype JUP_F32 or
+ *                   JUP_BF16
  *   n_accepted      out [n_seqs]: drafts accepted;  next_token out [n_seqs]
  *   emitted         out [n_rows], may be NULL: rows of a request: its accepted drafts, the next token, then -1
  *   lengths, new_lengths   [n_seqs], may both be NULL: cached positions before the step -> positions that are valid behind it,

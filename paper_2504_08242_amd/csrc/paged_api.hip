@@ -5,6 +5,8 @@ namespace {
 
 using jup::set_error;
 
+constexpr int32_t kMostIndexed = 1 << 30;  // entries that a kernel goes through in steps of a workgroup, in 32 bits
+
 bool off16(const void* p) { return ((uintptr_t)p & 15) != 0; }
 
 // Empty string when the pool is usable, otherwise the reason.
@@ -80,7 +82,8 @@ jup_status_t jup_paged_extend(const jup_paged_extend_t* a, void* stream) {
     if (a->table_width < 0 || (int64_t)a->table_width * a->page_size > INT32_MAX - 255)
         return set_error(JUP_EINVAL, "%s: table_width=%d is negative, or table_width * page_size exceeds 2^31 - 256", me, a->table_width);
     if (a->table_stride < a->table_width) return set_error(JUP_EINVAL, "%s: table_stride is shorter than table_width", me);
-    if (a->n_free < 0 || a->max_rows < 0) return set_error(JUP_EINVAL, "%s: n_free and max_rows must not be negative", me);
+    if (a->n_free < 0 || a->n_free > kMostIndexed) return set_error(JUP_EINVAL, "%s: n_free=%d is outside 0..2^30", me, a->n_free);
+    if (a->max_rows < 0) return set_error(JUP_EINVAL, "%s: max_rows=%d is negative", me, a->max_rows);
     if (!a->free_count || !a->row_start || !a->new_free_count || !a->status)
         return set_error(JUP_EINVAL, "%s: free_count, row_start, new_free_count and status must not be NULL", me);
     if (a->n_free > 0 && !a->free_blocks) return set_error(JUP_EINVAL, "%s: free_blocks is NULL", me);
@@ -155,7 +158,7 @@ jup_status_t jup_verify_drafts(const jup_verify_drafts_t* a, void* stream) {
     if (!a) return set_error(JUP_EINVAL, "%s: args is NULL", me);
     if (a->n_seqs < 0 || a->n_seqs > JUP_PAGED_MAX_SEQS)
         return set_error(JUP_EINVAL, "%s: n_seqs=%d is outside 0..%d", me, a->n_seqs, JUP_PAGED_MAX_SEQS);
-    if (a->n_rows < 0) return set_error(JUP_EINVAL, "%s: n_rows=%d is negative", me, a->n_rows);
+    if (a->n_rows < 0 || a->n_rows > kMostIndexed) return set_error(JUP_EINVAL, "%s: n_rows=%d is outside 0..2^30", me, a->n_rows);
     if (a->vocab <= 0 || a->vocab > (1 << 30)) return set_error(JUP_EINVAL, "%s: vocab=%d is outside 1..2^30", me, a->vocab);
     if (a->probs_dtype != JUP_F32 && a->probs_dtype != JUP_BF16) return set_error(JUP_EINVAL, "%s: probs_dtype must be JUP_F32 or JUP_BF16", me);
     if (a->target_row_stride < 0 || a->draft_row_stride < 0) return set_error(JUP_EINVAL, "%s: strides must not be negative", me);

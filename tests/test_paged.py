@@ -140,6 +140,12 @@ def test_attention_refuses_what_would_overflow(change, word):
     refused(jp._lib().jup_paged_attention(ctypes.byref(pool_args()), ctypes.byref(a), None), word)
 
 
+def test_sizes_that_indices_would_wrap_at_are_refused():
+    L = jp._lib()
+    refused(L.jup_paged_extend(ctypes.byref(extend_args(n_free=(1 << 30) + 1)), None), "n_free")
+    refused(L.jup_verify_drafts(ctypes.byref(verify_args(n_rows=(1 << 30) + 1)), None), "n_rows")
+
+
 def test_null_arguments_and_empty_calls():
     L = jp._lib()
     refused(L.jup_paged_extend(None, None), "NULL")
