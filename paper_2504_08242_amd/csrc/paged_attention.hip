@@ -739,7 +739,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_few(const Attention args
 // waves wait for one another's, as registers leave room for two per SIMD.  Three per SIMD of half the keys each: 970 instead of 1050 TFLOP/s.  One wave per
 // SIMD of 64 rows: 789.  Half the waves a product behind the others: 632 instead of 590 µs.  Four prompts of 700 to 4100 tokens (40 heads, 292 µs,
 // 735 TFLOP/s) have 1240 such tiles of 10 steps each, whose entry and end (15 of 60 µs) nothing overlaps: LDS has room for one workgroup.
-template <int NW, int KP, int NT, int SUB, int RING>
+template <int NW, int KP, int NT, int SUB>
 struct Many {
     static constexpr int kWaves = NW;
     static constexpr int kRows = 32 * NW / KP;
@@ -747,34 +747,23 @@ struct Many {
     static constexpr int kStepTiles = SUB * kSubTiles;
     static constexpr int kStep = kStepTiles * kKT;           // keys of a step
     static constexpr int kHalf = kStepTiles * kTileBytes;    // K tiles, then V tiles
-    static constexpr int kRing = RING;                       // steps in LDS
     static constexpr int kGroups = kStepTiles * 4 / kWaves;  // groups of eight rows that a wave fetches per step: wave, wave + NW
     static_assert(kGroups * kWaves == kStepTiles * 4);
     static constexpr int kRowBytes = 132 * 4;                // a row of a part's sums
-    static constexpr int kSteps = kRing * 2 * kHalf, kSums = 32 * NW * kRowBytes, kQ = 32 * NW * 256;
-    static constexpr int kThere = (kSteps > kSums ? kSteps > kQ ? kSteps : kQ : kSums);  // [kRing][kStepTiles * 4] bytes: which rows of a step's groups are keys
+    static constexpr int kSteps = 2 * 2 * kHalf, kSums = 32 * NW * kRowBytes, kQ = 32 * NW * 256;
+    static constexpr int kThere = (kSteps > kSums ? kSteps > kQ ? kSteps : kQ : kSums);  // [2][kStepTiles * 4] bytes: which rows of a step's groups are keys
     static constexpr int kFlag = kThere + 64;
     static constexpr int kStat = kFlag + 64;                 // [2][waves][32] maxima and sums
     static constexpr int kLds = kStat + (KP > 1 ? 2 * 32 * NW * 4 : 0);
-    static_assert(kLds <= 160 * 1024 && kRing * kStepTiles * 4 <= 64 && kRing >= 2);
-    // queries go through the last places of the ring, the first kFirst steps are fetched beside them
-    static constexpr int kFirst = (kThere - kQ) / (2 * kHalf) < kRing - 1 ? (kThere - kQ) / (2 * kHalf) : kRing - 1;
+    // queries go through the second step's place, the first step is fetched beside them
     static constexpr int kQAt = kThere - kQ;
+    static_assert(kLds <= 160 * 1024 && 2 * kStepTiles * 4 <= 64 && kQAt >= 2 * kHalf);
 };
 
-// Waits until at most `steps` steps' loads of this wave (four or eight each) are in flight.
-template <int LOADS>
-__device__ __forceinline__ void wait_steps(int steps) {
-    if (steps >= 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * LOADS) : "memory");
-    else if (steps == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS) : "memory");
-    else if (steps == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-}
-
-template <int NW, int KP, int NT, int SUB, int RING, int OCC>
+template <int NW, int KP, int NT, int SUB, int OCC>
 __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const Attention args, int least) {
-    typedef Many<NW, KP, NT, SUB, RING> L;
-    constexpr int kRing = L::kRing, kHalf = L::kHalf, kStep = L::kStep, kRows = L::kRows;
+    typedef Many<NW, KP, NT, SUB> L;
+    constexpr int kHalf = L::kHalf, kStep = L::kStep, kRows = L::kRows;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -818,11 +807,11 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const Attention a
     unsigned hole = 0;  // bit: in that slot, some of this wave's rows are no keys
     // K of step i, or V, and which rows are keys
     auto fill = [&](int i, const Ids& ids, bool v_part) __attribute__((always_inline)) {
-        if (v_part) hole &= ~(1u << (i % kRing));
+        if (v_part) hole &= ~(1u << (i & 1));
 #pragma unroll
         for (int g = 0; g < L::kGroups; ++g) {
             const int mine = first_key + i * kStep + 8 * NW * g + 8 * wave, key = min(mine, last_key & ~7);  // (groups behind the last key repeat its own)
-            unsigned slot = lds0 + (unsigned)(i % kRing) * 2 * kHalf + (v_part ? kHalf : 0) + (NW * g + wave) * 2048;
+            unsigned slot = lds0 + (unsigned)(i & 1) * 2 * kHalf + (v_part ? kHalf : 0) + (NW * g + wave) * 2048;
             asm volatile("" : "+v"(slot));  // (see attention_few)
             const unsigned dst = __builtin_amdgcn_readfirstlane(slot);
             const char* base = group_base(a, v_part ? v_pool : k_pool, ids.id[g], key);
@@ -831,8 +820,8 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const Attention a
             if (!v_part) continue;
             const int left = end_key - mine;
             const unsigned there = (unsigned)ids.id[g] >= (unsigned)a.n_blocks || left <= 0 ? 0u : left >= 8 ? 0xFFu : (1u << left) - 1;
-            hole |= there == 0xFFu ? 0u : 1u << (i % kRing);
-            if (lane == 0) lds[L::kThere + (i % kRing) * L::kStepTiles * 4 + NW * g + wave] = (unsigned char)there;
+            hole |= there == 0xFFu ? 0u : 1u << (i & 1);
+            if (lane == 0) lds[L::kThere + (i & 1) * L::kStepTiles * 4 + NW * g + wave] = (unsigned char)there;
         }
     };
     // Queries: this wave's 32 rows go through LDS (the second half of the steps' places) into B operands; rows past the last one repeat it.
@@ -856,7 +845,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const Attention a
             ids = next;
         }
     };
-    for (int i = 0; i < L::kFirst; ++i) fill_next(i, true, true);
+    fill_next(0, true, true);
 
     // Sub-steps (NT tiles per part) before this one: every row of the workgroup sees all their keys.
     constexpr int kSub = L::kSubTiles * kKT;
@@ -865,11 +854,11 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const Attention a
     // does not, values that are no numbers do.
     bool special = false;
     auto clean = [&](int i) __attribute__((always_inline)) {
-        if ((i + 1) * SUB <= open && !((hole >> (i % kRing)) & 1)) return;
+        if ((i + 1) * SUB <= open && !((hole >> (i & 1)) & 1)) return;
 #pragma unroll
         for (int g = 0; g < L::kGroups; ++g) {
-            const unsigned there = lds[L::kThere + (i % kRing) * L::kStepTiles * 4 + NW * g + wave];
-            unsigned char* at = lds + (i % kRing) * 2 * kHalf + kHalf + (NW * g + wave) * 2048 + lane * 16;
+            const unsigned there = lds[L::kThere + (i & 1) * L::kStepTiles * 4 + NW * g + wave];
+            unsigned char* at = lds + (i & 1) * 2 * kHalf + kHalf + (NW * g + wave) * 2048 + lane * 16;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const bool key = (there >> (4 * j + lrow)) & 1;
@@ -897,35 +886,36 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const Attention a
     for (int db = 0; db < 4; ++db)
         v_lane[db] = lds0 + kHalf + vt_row * 256 + ((db ^ (vt_row & 3)) << 6) + (2 * (quad & 1) + ((sl & 3) >> 1)) * 16 + 8 * (sl & 1);
     bf16x8 qf[8];
-    wait_steps<4 * L::kGroups>(min(n, L::kFirst));  // the queries have landed
+    // the queries have landed, the first step's loads may be in flight
+    if (n > 0) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * L::kGroups) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const bf16x8*)(q_lds + (k_lane ^ (32 * ks)));
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();  // every wave has its queries: steps may go there
+    __builtin_amdgcn_s_barrier();  // every wave has its queries: the second step may go there
     asm volatile("" ::: "memory");
-    for (int i = L::kFirst; i < kRing - 1; ++i) fill_next(i, true, true);
 
     for (int i = 0; i < n; ++i) {
         // step i is there for all, and step i - 1 has been read by all
-        wait_steps<4 * L::kGroups>(min(n - 1 - i, kRing - 2));
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         clean(i);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        // Step i + kRing - 1 goes where step i - 1 was.  (Its loads are put between the products: the address path of a CU takes 64 bytes per
+        // Step i + 1 goes where step i - 1 was.  (Its loads are put between the products: the address path of a CU takes 64 bytes per
         // clock, and with all waves' loads behind the meeting every wave would wait for it there.)
 #pragma unroll
       for (int u = 0; u < SUB; ++u) {
         if (i * SUB + u >= mine) {
-            fill_next(i + kRing - 1, u == 0, u == SUB - 1);
+            fill_next(i + 1, u == 0, u == SUB - 1);
             continue;
         }
         const int first_tile = (u * KP + part) * NT;  // of this wave's keys of the sub-step
-        const unsigned char* k_base = lds + (i % kRing) * 2 * kHalf + first_tile * kTileBytes;
-        const unsigned v_slot = (unsigned)(i % kRing) * 2 * kHalf + first_tile * kTileBytes;
+        const unsigned char* k_base = lds + (i & 1) * 2 * kHalf + first_tile * kTileBytes;
+        const unsigned v_slot = (unsigned)(i & 1) * 2 * kHalf + first_tile * kTileBytes;
         const int key0 = first_key + i * kStep + first_tile * kKT;
         unsigned there[NT], whole = ~0u;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) there[t] = *(const unsigned*)(lds + L::kThere + (i % kRing) * L::kStepTiles * 4 + (first_tile + t) * 4);
+        for (int t = 0; t < NT; ++t) there[t] = *(const unsigned*)(lds + L::kThere + (i & 1) * L::kStepTiles * 4 + (first_tile + t) * 4);
 
         // ---- S^T = K Q^T ----
         f32x16 s[NT];
@@ -953,7 +943,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const Attention a
         };
         read_v(0);
 
-        fill_next(i + kRing - 1, u == 0, false);
+        fill_next(i + 1, u == 0, false);
 
         // ---- online softmax (see attention_few) ----
         float sv[16 * NT];
@@ -995,7 +985,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const Attention a
         l_run = l_run * alpha + ps;
         m_run = m_new;
 
-        fill_next(i + kRing - 1, false, u == SUB - 1);
+        fill_next(i + 1, false, u == SUB - 1);
 
         // ---- O^T += V^T P^T ----
 #pragma unroll
@@ -1202,7 +1192,7 @@ template <int R, class K>
 hipError_t launch(K* kernel, int threads, int lds, bool* done, Attention a, long long tiles, int pieces, int places, int least, hipStream_t s) {
     hipError_t e = with_lds(kernel, lds, done);
     if (e != hipSuccess) return e;
-    pieces = a.n_kv_heads > kMostSplitHeads || pieces == 0 ? 0 : (pieces + a.n_kv_heads - 1) / a.n_kv_heads;
+    pieces = a.n_kv_heads > kMostSplitHeads ? 0 : (pieces + a.n_kv_heads - 1) / a.n_kv_heads;
     a.chunk_factor = pieces > 0 ? 1.0001f / pieces : 1e30f;
     a.most_places = places / a.n_kv_heads;
     const long long items = tiles + 2 * pieces, grid = items * a.n_kv_heads;
@@ -1258,9 +1248,9 @@ hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_
     //   8192, 32 heads on 8) 317 / 333 / 438;  160 (1024 tokens) 42 / 31 / 32;  128 (768 behind 1536) 54 / 61 / 57;  96 (512 behind 1536) 43 / 36 / 33.
     const long long groups = (rows / 256 + c.n_seqs) * pool.n_kv_heads;
     static bool done256[64], done128[64], done64[64];
-    hipError_t e = groups >= 384   ? launch<256>(attention_many<8, 1, 2, 2, 2, 2>, 512, Many<8, 1, 2, 2, 2>::kLds, done256, longer, rows / 256 + c.n_seqs, kManyPieces, kManyPlaces, kLeast, s)
-                   : groups >= 112 ? launch<128>(attention_many<8, 2, 2, 1, 2, 2>, 512, Many<8, 2, 2, 1, 2>::kLds, done128, longer, rows / 128 + c.n_seqs, kManyPieces, kManyPlaces, kLeast, s)
-                                   : launch<64>(attention_many<8, 4, 1, 1, 2, 2>, 512, Many<8, 4, 1, 1, 2>::kLds, done64, longer, rows / 64 + c.n_seqs, kManyPieces, kManyPlaces, kLeast, s);
+    hipError_t e = groups >= 384   ? launch<256>(attention_many<8, 1, 2, 2, 2>, 512, Many<8, 1, 2, 2>::kLds, done256, longer, rows / 256 + c.n_seqs, kManyPieces, kManyPlaces, kLeast, s)
+                   : groups >= 112 ? launch<128>(attention_many<8, 2, 2, 1, 2>, 512, Many<8, 2, 2, 1>::kLds, done128, longer, rows / 128 + c.n_seqs, kManyPieces, kManyPlaces, kLeast, s)
+                                   : launch<64>(attention_many<8, 4, 1, 1, 2>, 512, Many<8, 4, 1, 1>::kLds, done64, longer, rows / 64 + c.n_seqs, kManyPieces, kManyPlaces, kLeast, s);
     if (e != hipSuccess || all) return e;
     a.most_rows = kShortRows;  // (one tile each)
     return few(a, 0, c.n_seqs);
