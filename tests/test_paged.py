@@ -570,6 +570,17 @@ def test_old_pages_that_were_dropped(workspace, heads, kv_heads, requests, gone)
     assert got[:requests[0][1]].any()
 
 
+@gpu
+@pytest.mark.parametrize("heads,kv_heads,requests", [(30, 30, [(0, 1)] * 10 + [(2000, 300)]), (20, 20, [(0, 1)] * 20 + [(2000, 200)]), (32, 4, [(3000, 200), (10, 300)]),
+                                                     (64, 64, [(0, 2)] * 7 + [(1500, 100)]), (65, 65, [(0, 2)] * 7 + [(1500, 100)])])
+def test_divided_keys_of_tall_tiles(workspace, heads, kv_heads, requests):
+    """Tiles of 128, 256 and 64 rows: requests of more than 96 rows, more than 512 tiles of 32.  Keys are divided for up to 64 heads."""
+    b = Batch(torch.bfloat16, heads, kv_heads, 32, requests)
+    got = b.run(workspace)
+    b.check(got)
+    assert torch.equal(got, b.run(workspace))
+
+
 def many_requests(n, most_cached, most_new, seed):
     rng = np.random.default_rng(seed)
     requests = [(int(rng.integers(0, most_cached + 1)), int(rng.integers(0, most_new + 1))) for _ in range(n)]
