@@ -944,6 +944,27 @@ def test_more_pieces_of_work_than_a_launch_has_workgroups_in_a_line(workspace, m
     assert (out.view(n // 8, 8, heads, 128) == out[:8]).all()
 
 
+@gpu
+def test_a_call_on_another_stream_is_captured():
+    """A graph whose call is on a stream of its own, replayed with eager calls in between."""
+    batches = [Batch(torch.bfloat16, 4, 2, 16, r) for r in ([(3000, 1), (700, 4)], [(500, 40), (100, 90)])]
+    space, eager = jp.Workspace(DEV), jp.Workspace(DEV)
+    want = [b.run(eager) for b in batches]
+    args = [(b.q, b.k, b.v, torch.from_numpy(b.table).to(DEV, torch.int32), ints(b.row_start), ints(b.lengths), max(b.new), space) for b in batches]
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        outs = [jp.attention(*a, stream=side) for a in args]
+        torch.cuda.current_stream().wait_stream(side)
+    for _ in range(3):
+        for out in outs:
+            out.zero_()
+        graph.replay()
+        assert all(torch.equal(b.run(eager), w) for b, w in zip(batches, want))
+        assert all(torch.equal(out, w) for out, w in zip(outs, want))
+
+
 # ---- verification ----------------------------------------------------------------------------------------------------------------
 
 
