@@ -784,6 +784,15 @@ def test_scores_far_apart(workspace, requests):
 
 
 @gpu
+@pytest.mark.parametrize("requests", [[(3000, 2)], [(2500, 40), (0, 600)]])
+def test_values_near_the_largest(workspace, requests):
+    """2^104 times normal ones: sums of 3000 weights of up to 2^8 stay below 2^128."""
+    b = Batch(torch.bfloat16, 32, 4, 16, requests)
+    b.v *= 2.0 ** 104
+    b.check(b.run(workspace))
+
+
+@gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_lengths_that_make_no_sense_stay_inside_the_buffers(workspace, dtype):
     """Lengths shorter than the new tokens, negative, or beyond the table; rows beyond n_rows."""
