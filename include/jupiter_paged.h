@@ -6,7 +6,9 @@
  * branches by the same number of tokens.  Here a POOL holds pages of page_size positions, a request's BLOCK TABLE names
  * the pages that hold its positions in order, and a call takes the rows of any number of requests, each with any number
  * of new tokens (a RAGGED batch): rows row_start[i] .. row_start[i+1]-1 belong to request i.  Requests (outline branches,
- * Jupiter paper Sec. V-B) that share a prefix name the same pages.  A speculative step (Sec. V-A) is
+ * Jupiter paper Sec. V-B) that share a prefix name the same pages; only pages that the prefix fills may be shared, as a step's
+ * tokens go into the last page of a request while that has room, and nothing copies a page (a branch that begins inside a page
+ * needs a copy of it of its own).  A speculative step (Sec. V-A) is
  *
  *     jup_paged_extend     lengths -> pages, positions, slots                       (once per step)
  *     jup_paged_append     rotary embedding, keys and values into their slots       (every layer; or, for a stage of
@@ -102,6 +104,8 @@ JUP_API jup_status_t jup_paged_append(const jup_paged_pool_t *pool, const jup_pa
  * the positions 0 .. lengths[i] - m + t (lengths count the new tokens, whose keys and values are in the pool), so lengths
  * and row_start are what jup_paged_extend() left.  Query head h reads key/value head h / (n_heads / n_kv_heads).
  *     out = sum_j p_j v_j,  p = softmax_j(scale * q . k_j)
+ * JUP_BF16: p is rounded to bf16 as it meets v; sums are fp32 and divided by sum p at the end, so that they overflow where values
+ * are larger than 2^120 / number of keys.
  * A position whose table entry is outside [0, n_blocks), or that lies behind table_width pages, is not there; a row that
  * sees no position gets zeros.  Values of positions a row does not see do not reach it, whatever they are.  Rows of q and
  * out outside [row_start[0], row_start[n_seqs]) are neither read nor written.

@@ -732,13 +732,14 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_few(const Attention args
 // KP parts of the keys: a workgroup has 256 / KP rows, and KP waves divide the keys of 32 of them and add up through LDS at the
 // end.  One part reads a key for the most rows; more parts make more workgroups of fewer rows, where rows are few or
 // where triangles of different sizes are to be dealt to the CUs.  Where one request's keys are far more than the others', they are divided
-// among workgroups: five requests of 100 to 300 tokens behind 10 to 20000 take 122 µs instead of 342, three of 40 to 500 behind 2000 to 9000
-// 84 instead of 138 (but six of 1 to 600 behind 10 to 32000 660 instead of 603: 320 equal pieces for 256 CUs).
+// among workgroups: five requests of 100 to 300 tokens behind 10 to 20000 take 114 µs instead of 342, three of 40 to 500 behind 2000 to 9000
+// 78 instead of 138 (but six of 1 to 600 behind 10 to 32000 589 instead of 580: 320 equal pieces for 256 CUs).
 // Measured: a prompt of 16384 tokens on 8 heads in 540 µs, 1019 TFLOP/s, matrix cores busy 44 % of the clocks, LDS 22 %.  Without loads
 // from memory it takes 92 % of that, without exponentials 89 %, without LDS reads 73 %, without products 95 %: no one unit binds it, but the
-// waves wait for one another's, as registers leave room for two per SIMD.  Three per SIMD of half the keys each: 970 instead of 1050 TFLOP/s.  One wave per
-// SIMD of 64 rows: 789.  Half the waves a product behind the others: 632 instead of 590 µs.  Four prompts of 700 to 4100 tokens (40 heads, 292 µs,
-// 735 TFLOP/s) have 1240 such tiles of 10 steps each, whose entry and end (15 of 60 µs) nothing overlaps: LDS has room for one workgroup.
+// waves wait for one another's, as registers leave room for two per SIMD.  (The shapes of 128 and 64 rows were not taken apart like this.)
+// Three per SIMD of half the keys each: 970 instead of 1050 TFLOP/s.  One wave per SIMD of 64 rows: 789.  Half the waves a product behind the
+// others: 632 instead of 590 µs.  Four prompts of 700 to 4100 tokens (40 heads, 292 µs, 735 TFLOP/s) have 1240 such tiles of 10 steps each,
+// whose entry and end (15 of 60 µs) nothing overlaps: LDS has room for one workgroup, and a workgroup has one tile.
 template <int NW, int KP, int NT, int SUB>
 struct Many {
     static constexpr int kWaves = NW;
@@ -1158,15 +1159,17 @@ namespace {
 // Calls whose requests have up to 96 rows, or that have no more tiles of 32 rows than fit the chip at once (two per CU), are attention_few's.
 // In µs, attention_few and attention_many: 64 rows behind 1536 on 32 heads 16 / 20, 96 rows 17 / 20, 128 rows (of 128 tiles) 17 / 21, 192 rows 20 / 34;
 // 16 requests of 96 rows behind 500 to 2100 29 / 38; 900 tokens behind 3000 on 16 heads over 2 (452 tiles) 78 / 87; four requests of 100 (416
-// tiles) 34 / 32; 512 tokens behind 1536 (544 tiles) 33 / 33; 20 requests of 128 rows behind 300 to 1000 (2560 tiles) 81 / 74.
+// tiles) 34 / 32 (lost by the rule); 512 tokens behind 1536 (544 tiles) 33 / 33; 20 requests of 128 rows behind 300 to 1000 (2560 tiles) 81 / 74.
 constexpr int kFewRows = 96;
 constexpr int kFewTiles = 512;
 constexpr int kShortRows = 32;
 // Pieces: two workgroups per CU (one token behind 8192 27.4 µs with 768, 27.0 with 512 as with 192 of eight waves), three of
 // eight waves for four CUs (16 requests behind 10 to 8000 on 8 heads 28 µs, with 256 pieces 36).
 constexpr int kFewPieces = 512, kWidePieces = 192;
-// Key tiles that are worth a piece.  One token behind 576 (19 tiles) takes 10.3 µs whole and 12.3 in two pieces; behind 2048 14.3 in pieces of
-// 24 tiles, 12.8 in pieces of 20 or 16; 48 rows behind 1300 15.9, 14.1 and 14.1; 60 rows behind 400 11.1 whole, 13.3 in pieces of 12.
+// Key tiles that the longest piece may have whatever the cost: 20 stay whole, 21 are divided in two of 10 and 11.  One token behind 576 (19
+// tiles) takes 10.3 µs whole and 12.3 in two pieces; behind 2048 14.3 in pieces of 24 tiles, 12.8 in pieces of 20 or 16; 48 rows behind 1300
+// 15.9, 14.1 and 14.1; 60 rows behind 400 11.1 whole, 13.3 in pieces of 12.  Just above 20 tiles the rule loses: one token on 32 heads behind
+// 641, 672, 768, 1024 and 1056 keys takes 12.2, 10.9, 11.1, 11.7 and 12.4 µs in two pieces, 10.7, 9.2, 9.3, 11.2 and 11.8 whole.
 constexpr int kLeast = 20;
 // A workgroup per CU, less what the longest piece may be longer than the average.  With 128, 222 and 333: three requests of 40 to 500 tokens
 // behind 2000 to 9000 86, 84 and 102 µs, five of 100 to 300 behind 10 to 20000 150, 122 and 130.
@@ -1238,7 +1241,8 @@ hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_
     if (most <= kFewRows || (rows / 32 + c.n_seqs) * pool.n_kv_heads <= kFewTiles) return few(a, rows / 16 + c.n_seqs, rows / 32 + c.n_seqs);
     // Up to 32 requests all go to attention_many, of more those of up to 32 rows to a launch of attention_few (an empty one costs 4 µs).  One
     // launch and two: 15 requests of one token behind 4000 and one of 512 61 and 65 µs, 32 of 1 to 300 behind 100 to 3000 171 and 180, 60 of one
-    // behind 2000 and four of 300 142 and 160; 63 of one behind 1000 and one of 512 76 and 66, 63 behind 4000 and one of 256 804 and 760.
+    // behind 2000 and four of 300 142 and 160 (lost by the rule, which knows the number of requests alone); 63 of one behind 1000 and one of 512
+    // 76 and 66, 63 behind 4000 and one of 256 804 and 760.
     const bool all = c.n_seqs <= 32;
     Attention longer = a;
     longer.least_rows = all ? 0 : kShortRows + 1;
@@ -1246,6 +1250,7 @@ hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_
     //   1280 (four prompts, 40 heads) 292 / 320 / 458;  520 (16384 tokens, 8 heads) 542 / 594 / 782;  384 (2900 tokens, 32 heads) 100 / 104 / 141;
     //   360 (2048 tokens, 40 heads) 78 / 76 / 101;  320 (three chunks, 40 heads) 64 / 55 / 74;  288 (2048 tokens, 32 heads) 66 / 57 / 81;  264 (2048 behind
     //   8192, 32 heads on 8) 317 / 333 / 438;  160 (1024 tokens) 42 / 31 / 32;  128 (768 behind 1536) 54 / 61 / 57;  96 (512 behind 1536) 43 / 36 / 33.
+    // (No number of tiles alone decides: 264 and 128 lose 5 and 12 % by the rule.)
     const long long groups = (rows / 256 + c.n_seqs) * pool.n_kv_heads;
     static bool done256[64], done128[64], done64[64];
     hipError_t e = groups >= 384   ? launch<256>(attention_many<8, 1, 2, 2, 2>, 512, Many<8, 1, 2, 2>::kLds, done256, longer, rows / 256 + c.n_seqs, kManyPieces, kManyPlaces, kLeast, s)

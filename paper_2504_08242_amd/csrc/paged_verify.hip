@@ -2,8 +2,10 @@
 //
 // With x the token drafted behind row r: accepted while u_r q_r(x) < p_r(x), both sides exact in 64 bits (products of two
 // 24-bit numbers).  At the first rejection the next token is drawn from w = max(p - q, 0), behind the last draft from p: the
-// lowest j whose running sum exceeds u * sum(w).  Sums are in 64 bits: with up to 2^17 addends of 24 bits in different orders
-// they differ by 1e-16 of the whole, where neighbouring borders are 1e-5 apart and 32-bit sums would be 1e-7 off.
+// lowest j whose running sum exceeds u * sum(w).  Sums are in 64 bits: in any order they are off by at most 2^-53 of the whole for every
+// addition on the longest way through them (a thread's tokens, a wave, the workgroup, the slices: below 128 for 131072 tokens, 1.4e-14, and
+// 65700 for 2^30, 7e-12), where neighbouring borders are about 1 / vocab apart and 32-bit sums would be 6e-8 off for
+// every addition.
 #include "paged.h"
 
 namespace jup {
@@ -147,8 +149,8 @@ __device__ int search(const Weights<T>& w, int lo, int hi, double before, double
 
 // `slices` workgroups per request, each with `length` tokens of the vocabulary.  All of them find the row (a few loads); the one that
 // is done last knows where the border is and goes through its slice again.  Bound by trips to memory behind one another (rows, tokens,
-// their probabilities, the slice, the other slices' sums, the slice with the border): 9.5 µs for one request and 32000 tokens, 11.5 for
-// 16 requests (one workgroup of 1024 threads per request instead: 22); 64 requests and 131072 tokens, 67 MB, take 27.
+// their probabilities, the slice, its sum on the way to memory, the other slices' sums, the slice with the border): 10.0 µs for one request
+// and 32000 tokens, 12.4 for 16 requests (one workgroup of 1024 threads per request instead: 22); 64 requests and 131072 tokens, 67 MB, take 27.
 template <class T, int E>
 __global__ __launch_bounds__(kThreads) void verify(const jup_verify_drafts_t a, int slices, int length, int* count, double* scratch) {
     __shared__ Shared s;

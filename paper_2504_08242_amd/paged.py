@@ -2,7 +2,8 @@
 
 A pool is two tensors ``k_pool`` and ``v_pool`` [n_blocks, n_kv_heads, page_size, head_dim] (one layer each; any strides
 whose last is 1, the same for both), a block table an int32 tensor [n_requests, width], a ragged batch a tensor of rows with
-``row_start`` [n_requests + 1].  One step::
+``row_start`` [n_requests + 1].  Requests may name the same pages for a prefix that they share, as far as it fills them: a page that is
+partly filled is written by the next step.  One step::
 
     step = extend(lengths, n_new, owned, table, free_blocks, free_count, page_size, max_rows)
     for layer in ...:
