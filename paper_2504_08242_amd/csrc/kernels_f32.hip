@@ -18,9 +18,11 @@ __device__ inline float wave_sum(float v) {
 
 // y[t][j] = x[t][j] * g[j] / sqrt(mean_j x^2 + eps); one 256-thread block per row.
 __global__ __launch_bounds__(256) void f32_rmsnorm(const float* __restrict__ x, const float* __restrict__ g,
-                                                   float* __restrict__ y, int d, float eps) {
+                                                   float* __restrict__ y, int n, int d, float eps) {
     __shared__ float part[4];
-    const float* xr = x + (size_t)blockIdx.x * d;
+    const size_t row = block_number();
+    if (row >= (size_t)n) return;
+    const float* xr = x + row * d;
     float ss = 0.f;
     for (int j = threadIdx.x; j < d; j += 256) ss += xr[j] * xr[j];
     ss = wave_sum(ss);
@@ -28,7 +30,7 @@ __global__ __launch_bounds__(256) void f32_rmsnorm(const float* __restrict__ x, 
     __syncthreads();
     const float tot = part[0] + part[1] + part[2] + part[3];
     const float inv = 1.0f / sqrtf(tot / (float)d + eps);
-    float* yr = y + (size_t)blockIdx.x * d;
+    float* yr = y + row * d;
     for (int j = threadIdx.x; j < d; j += 256) yr[j] = xr[j] * inv * g[j];
 }
 
@@ -96,7 +98,7 @@ __device__ inline const float* kv_row(const KvView& kv, int layer, int which, in
 __global__ void f32_rope_append(float* __restrict__ qkv, int n, int d, int n_heads, int dh, int pos0, float theta,
                                 KvView kv, int layer, const TreeTable* __restrict__ tree) {
     const int half = dh / 2;
-    const long long gid = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+    const long long gid = (long long)block_number() * 256 + threadIdx.x;
     if (gid >= (long long)n * n_heads * half) return;
     const int i = (int)(gid % half);
     const int h = (int)((gid / half) % n_heads);
@@ -160,7 +162,7 @@ __global__ __launch_bounds__(kWave) void f32_attention(const float* __restrict__
 
 // act[t][j] = silu(gate[t][j]) * up[t][j] with gate|up fused as [n, 2f].
 __global__ void f32_swiglu(const float* __restrict__ gu, float* __restrict__ act, int n, int f) {
-    const long long gid = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+    const long long gid = (long long)block_number() * 256 + threadIdx.x;
     if (gid >= (long long)n * f) return;
     const int j = (int)(gid % f);
     const long long t = gid / f;
@@ -204,7 +206,7 @@ hipError_t f32_forward(const jup_stage& st, const float* hidden_in, int n, int p
         const float* g1 = (const float*)(wb + st.pl.g_attn);
         const float* g2 = (const float*)(wb + st.pl.g_mlp);
 
-        hipLaunchKernelGGL(f32_rmsnorm, dim3(n), dim3(256), 0, s, x, g1, xn, d, c.rms_eps);
+        hipLaunchKernelGGL(f32_rmsnorm, grid_of(n), dim3(256), 0, s, x, g1, xn, n, d, c.rms_eps);
         gemm(xn, d, wqkv, qkv, nullptr, 3 * d, n, 3 * d, d, s);
         if (paged) {
             const jup_paged_pool_t pool = paged->layer(l);
@@ -220,16 +222,16 @@ hipError_t f32_forward(const jup_stage& st, const float* hidden_in, int n, int p
             if (e != hipSuccess) return e;
         } else {
             const long long work = (long long)n * H * (dh / 2);
-            hipLaunchKernelGGL(f32_rope_append, dim3((unsigned)((work + 255) / 256)), dim3(256), 0, s, qkv, n, d, H, dh,
+            hipLaunchKernelGGL(f32_rope_append, grid_of((work + 255) / 256), dim3(256), 0, s, qkv, n, d, H, dh,
                                pos, c.rope_theta, kv, l, tree_dev);
             hipLaunchKernelGGL(f32_attention, dim3(n, H), dim3(kWave), 0, s, qkv, o, d, H, dh, pos, kv, l, tree_dev);
         }
         gemm(o, d, wo, x, x, d, n, d, d, s);  // x <- x + o Wo^T (each element read and written by one thread)
-        hipLaunchKernelGGL(f32_rmsnorm, dim3(n), dim3(256), 0, s, x, g2, xn, d, c.rms_eps);
+        hipLaunchKernelGGL(f32_rmsnorm, grid_of(n), dim3(256), 0, s, x, g2, xn, n, d, c.rms_eps);
         gemm(xn, d, wgu, gu, nullptr, 2 * f, n, 2 * f, d, s);
         {
             const long long work = (long long)n * f;
-            hipLaunchKernelGGL(f32_swiglu, dim3((unsigned)((work + 255) / 256)), dim3(256), 0, s, gu, act, n, f);
+            hipLaunchKernelGGL(f32_swiglu, grid_of((work + 255) / 256), dim3(256), 0, s, gu, act, n, f);
         }
         gemm(act, f, wdown, x, x, d, n, d, f, s);
     }

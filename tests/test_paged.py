@@ -1405,5 +1405,43 @@ def test_a_stage_on_another_device_is_refused(workspace):
         jp.prefill(elsewhere, x, step, k, k, table, 4, workspace)
 
 
+@gpu
+def test_a_stage_over_more_activations_than_a_launch_has_threads_in_a_line(workspace):
+    """Check mode has a thread per row and feature of the MLP: 2^32 and more of them.  The second half of the requests alone gives the same bits."""
+    from paper_2504_08242_amd import synth_inputs as si
+    cfg = dict(si.TINY, n_layers=1, d_model=64, n_heads=1, d_ffn=4096)
+    n, rows = 16384, 64 * 16384 + 64
+    stage = jb.Stage(cfg, "f32", jb.upload_layers(si.make_layers(cfg, seed=3), "f32"), rows)
+    x = torch.randn((rows, 64), generator=torch.Generator(device=DEV).manual_seed(3), device=DEV)
+
+    def run(x, new):
+        k, v = (torch.zeros((1, len(new) + 1, 1, 64, 64), device=DEV) for _ in "kv")
+        table, none = torch.full((len(new), 2), -1, dtype=torch.int32, device=DEV), [0] * len(new)
+        step = jp.extend(ints(none), ints(new), ints(none), table, ints(range(len(new) + 1)), ints([len(new) + 1]), 64, x.shape[0])
+        assert step.status.item() == 0
+        return jp.prefill(stage, x, step, k, v, table, max(new))
+
+    whole = run(x, [128] + [64] * (n - 1))
+    assert torch.equal(run(x[-64 * 8192:].contiguous(), [64] * 8192), whole[-64 * 8192:])
+    assert torch.equal(run(x[:64 * 8193], [128] + [64] * 8191), whole[:64 * 8193])
+
+
+@gpu
+def test_a_stage_over_more_rows_than_a_launch_has_workgroups_in_a_line():
+    """2^24 rows and more, in check mode.  No row has a slot and the pool is zero: what is left is x + down(silu(gate n) up n), n = x / rms."""
+    cfg = dict(n_layers=1, d_model=2, n_heads=1, head_dim=2, d_ffn=1, rms_eps=1e-5, rope_theta=1e4)
+    weight = {n: torch.ones((2,) if n.startswith("g_") else (1, 2) if n in ("w_gate", "w_up") else (2, 1) if n == "w_down" else (2, 2), device=DEV) for n in jb.WEIGHT_NAMES}
+    rows = (1 << 24) + 70
+    stage = jb.Stage(cfg, "f32", [weight], rows)
+    zero, pool = torch.zeros(rows, dtype=torch.int32, device=DEV), torch.zeros((1, 1, 1, 8, 2), device=DEV)
+    x = torch.randn((rows, 2), generator=torch.Generator(device=DEV).manual_seed(7), device=DEV)
+    got = jp.prefill(stage, x, jp.Step(ints([0, rows]), zero, zero - 1, ints([rows]), None, None, None), pool, pool, ints([0])[None], rows)
+    v = x.double()
+    v = (v / (v.square().mean(-1, keepdim=True) + 1e-5).sqrt()).sum(-1, keepdim=True)   # at most 2.83 in size
+    # roundings: five in each of the two that make v, 14 x 2^-24 with their sum, times the slope of silu(v) v, 5.8; six in that product of up to
+    # 7.6; one of the result
+    assert ((got - (x.double() + torch.nn.functional.silu(v) * v)).abs() <= (81 + 46 + 8) * 2.0 ** -24 + 2.0 ** -24 * x.abs()).all()
+
+
 def test_a_missing_stage_is_refused():
     refused(jp._lib().jup_stage_prefill_paged(None, FAKE, 2, ctypes.byref(jp._Batch()), FAKE, None), "stage")
