@@ -18,6 +18,11 @@
  *
  * Lengths, tables and tokens stay on the GPU: the host waits for nothing, and a captured step can be replayed.
  *
+ * A pool may hold 8-bit codes and scales in place of bf16 values (jup_paged_append8, jup_paged_attention8, jup_paged_read8,
+ * jup_stage_prefill_paged8): half the bytes, which is what decoding behind long caches waits for.  Where requests are the beams
+ * of a search, jup_beam_select() ends a step in place of jup_verify_drafts(), and jup_paged_reorder() with jup_paged_copy()
+ * makes the tables that the next one begins with; the same two let a request branch inside a page.
+ *
  * Conventions (beside those of jupiter_stage.h)
  *   - Pointers inside the argument structs are DEVICE pointers; the structs themselves are host memory, read during the
  *     call.  Strides count elements.
@@ -44,8 +49,26 @@ typedef struct {
     void *k, *v;
     int64_t block_stride, head_stride, slot_stride;
     int32_t n_blocks, page_size, n_kv_heads, head_dim;
-    int32_t dtype; /* JUP_F32 or JUP_BF16 */
+    int32_t dtype; /* JUP_F32 or JUP_BF16; of the calls that take scales JUP_I8 or JUP_E4M3 */
 } jup_paged_pool_t;
+
+/*
+ * Pools in 8 bits.  k and v hold codes of one byte (strides count them), JUP_I8: two's complement, JUP_E4M3: sign, 4 bits of
+ * exponent, 3 of fraction, no infinities.  Code i of (block, head, slot) stands for code * scale, with the scale of that head and
+ * slot at block * block_stride + head * head_stride + slot of scales->k or scales->v (fp32).  What jup_paged_append8() writes, of the
+ * 128 values x_i of a head:
+ *     m = max(2^-100, max_i |x_i|),  scale = m / T,  code_i = the one nearest to x_i * (T / m), ties to even
+ * in fp32, with T = 127 (JUP_I8) or 448 (JUP_E4M3): a value is off by at most scale / 2, or (JUP_E4M3) 2^-4 of itself where that is
+ * more than scale * 2^-10.  A head with an infinity or a NaN gets scale NaN and codes 0.
+ * Such pools need head_dim 128, tensors that are 16-byte aligned, strides of codes that are multiples of 16 and strides of scales that
+ * are multiples of 4; the rows that go with them (q, k, v and results) are JUP_BF16.
+ */
+typedef enum { JUP_I8 = 3, JUP_E4M3 = 4 } jup_code_t;
+typedef struct {
+    float *k, *v;
+    int64_t block_stride, head_stride;
+    int64_t layer_stride; /* between the layers of a stage; used by jup_stage_prefill_paged8() and jup_paged_copy() alone */
+} jup_paged_scales_t;
 
 /*
  * Block tables, positions and slots of a step.  Request i holds lengths[i] positions in the first owned[i] entries of its
@@ -133,7 +156,32 @@ typedef struct {
 } jup_paged_attention_t;
 JUP_API jup_status_t jup_paged_attention(const jup_paged_pool_t *pool, const jup_paged_attention_t *args, void *stream);
 
-/* Bytes of a workspace that serves every call of jup_paged_attention() and jup_verify_drafts(). */
+/*
+ * The same for pools in 8 bits.  Append: k is rotated in fp32 and quantised without another rounding.  Attention: the scale of a key
+ * multiplies its score, that of a value its probability, and the product is what is rounded to bf16; codes are exact in bf16.  A score or a
+ * value of a key that a row does not see does not reach it, whatever codes and scales hold.  JUP_I8 codes of -128 and JUP_E4M3 codes that are
+ * no numbers, which jup_paged_append8() does not write, count as what they are.  Errors: JUP_EINVAL, JUP_EDEVICE.
+ */
+JUP_API jup_status_t jup_paged_append8(const jup_paged_pool_t *pool, const jup_paged_scales_t *scales, const jup_paged_append_t *args, void *stream);
+JUP_API jup_status_t jup_paged_attention8(const jup_paged_pool_t *pool, const jup_paged_scales_t *scales, const jup_paged_attention_t *args, void *stream);
+
+/*
+ * Rows out of their slots: row r of k and v is what the pool holds at slots[r], or zeros where that is outside the pool.
+ *   k, v            element i of (row, head) at row * row_stride + head * head_stride + i.  JUP_BF16, or JUP_F32 of a JUP_F32 pool.  Each
+ *                   may be NULL
+ * jup_paged_read8(): code * scale, rounded once.  Errors: JUP_EINVAL, JUP_EDEVICE.
+ */
+typedef struct {
+    int32_t n_rows;
+    void *k, *v;
+    int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+    const int32_t *slots;
+} jup_paged_read_t;
+JUP_API jup_status_t jup_paged_read(const jup_paged_pool_t *pool, const jup_paged_read_t *args, void *stream);
+JUP_API jup_status_t jup_paged_read8(const jup_paged_pool_t *pool, const jup_paged_scales_t *scales, const jup_paged_read_t *args, void *stream);
+
+/* Bytes of a workspace that serves every call of jup_paged_attention(), jup_paged_attention8(), jup_verify_drafts(), jup_beam_select() and
+ * jup_paged_reorder(). */
 JUP_API size_t jup_paged_workspace_bytes(void);
 
 /*
@@ -159,6 +207,10 @@ typedef struct {
 } jup_paged_batch_t;
 JUP_API jup_status_t jup_stage_prefill_paged(jup_stage_t *stage, const void *hidden_in, int32_t n_rows, const jup_paged_batch_t *batch,
                                              void *hidden_out, void *stream);
+
+/* The same over a pool in 8 bits (of the bf16 and 4-bit stages); batch->pool.dtype JUP_I8 or JUP_E4M3. */
+JUP_API jup_status_t jup_stage_prefill_paged8(jup_stage_t *stage, const void *hidden_in, int32_t n_rows, const jup_paged_batch_t *batch,
+                                              const jup_paged_scales_t *scales, void *hidden_out, void *stream);
 
 /*
  * Verification of drafted tokens (Sec. V-A step 4).  Row r of request i holds an input token of the step: the last one
@@ -197,6 +249,85 @@ typedef struct {
     size_t workspace_bytes;
 } jup_verify_drafts_t;
 JUP_API jup_status_t jup_verify_drafts(const jup_verify_drafts_t *args, void *stream);
+
+/*
+ * The end of a step of a beam search.  Request i has n_beams beams, rows i * n_beams .. of logits and scores.  Its candidates are
+ * (beam b, token j) with score  scores[b] + logits[b][j] - log sum_k exp(logits[b][k]),  of a beam that has ended (ended[b] not 0)
+ * the one candidate (b, end_token) with scores[b].  The n_keep best of them come out, best first; equal scores: the lower beam, then the
+ * lower token.  Scores are compared in 64 bits; exponentials are fp32 with their sums in 64: a score is off by about 2^-24.
+ *   logits          [n_seqs * n_beams][vocab], rows row_stride apart; logits_dtype JUP_F32 or JUP_BF16.  One that is NaN or +infinity
+ *                   counts as -infinity, and is no candidate
+ *   scores          [n_seqs * n_beams]: sums of log probabilities.  A beam whose score is not finite has no candidates
+ *   ended           [n_seqs * n_beams], may be NULL: none has.  Rows of beams that have ended are not read
+ *   parents         out [n_seqs * n_keep]: the candidate's beam, as a row of logits (what jup_paged_reorder() takes);
+ *   tokens, new_scores, new_ended  out [n_seqs * n_keep]: new_ended is 1 where ended was, or the token is end_token (-1: none is)
+ *   Where a request has fewer than n_keep candidates the others are parent -1, token -1, score -infinity, new_ended 0.
+ * n_beams and n_keep are 1 .. JUP_BEAM_MOST, vocab 1 .. 2^30, n_seqs * n_beams <= JUP_PAGED_MAX_SEQS.  new_ended may be NULL.  Outputs overlap nothing
+ * else (scores and ended are read behind the first outputs).  workspace: as in jup_paged_attention().  Errors: JUP_EINVAL, JUP_EDEVICE.
+ */
+#define JUP_BEAM_MOST 64
+typedef struct {
+    int32_t n_seqs, n_beams, n_keep, vocab, logits_dtype, end_token;
+    const void *logits;
+    int64_t row_stride;
+    const float *scores;
+    const int32_t *ended;
+    int32_t *parents, *tokens;
+    float *new_scores;
+    int32_t *new_ended;
+    void *workspace;
+    size_t workspace_bytes;
+} jup_beam_select_t;
+JUP_API jup_status_t jup_beam_select(const jup_beam_select_t *args, void *stream);
+
+/*
+ * Block tables of requests that go on from others: request i of n_out becomes what request parents[i] of n_in was (-1: an empty one).
+ * With L positions, the L / page_size pages that these fill are shared.  A page that they fill in part is the parent's own: the lowest i with that
+ * parent takes it over, every other one gets a free page and a copy of it is due (jup_paged_copy).  Pages that are in some request's
+ * owned[] entries and in none of the new tables go back on the stack, behind what is left of it, in the order of their numbers.
+ * So all requests that have pages of the pool are in the call (one that stays what it is: parents[i] = i), or their pages are marked in held.
+ *   table           [n_in][table_stride], table_width entries used; new_table [n_out][new_table_stride], new_table_width entries: those
+ *                   behind a request's pages are set to -1.  They do not overlap
+ *   lengths, owned  [n_in]; new_lengths, new_owned out [n_out]: the parent's length, the pages that it fills or begins
+ *   free_blocks     [n_free], n_free <= 2^28: the stack has room for every block, so blocks are numbers below n_free;  free_count [1]
+ *   new_free_blocks out [n_free] (may be free_blocks: else all of it is copied);  new_free_count out [1] (may be free_count)
+ *   held            [n_free] bytes, may be NULL: blocks that are not 0 there do not go back
+ *   copy_from, copy_to  out [n_out]: the page to copy and its copy, or -1
+ *   status          out [1]: 0, or the smallest of
+ *                     1  a parent outside -1 .. n_in - 1, or of one of the parents: a negative length, owned outside 0 .. table_width, or fewer
+ *                        pages than its length needs; *free_count outside [0, n_free]
+ *                     2  a request needs more than new_table_width pages
+ *                     4  more copies than there are free blocks
+ *                   Then the new requests are empty (lengths and owned 0, tables and copies -1) and the stack is as before: the
+ *                   old tables still hold.
+ * Entries of a table that are no blocks are copied as they are and never go back.  n_in, n_out <= JUP_PAGED_MAX_SEQS.
+ * workspace: as in jup_paged_attention().  Errors: JUP_EINVAL, JUP_EDEVICE.
+ */
+typedef struct {
+    int32_t n_in, n_out, page_size, table_width, new_table_width, n_free;
+    int64_t table_stride, new_table_stride;
+    const int32_t *parents, *table, *lengths, *owned, *free_blocks, *free_count;
+    const uint8_t *held;
+    int32_t *new_table, *new_lengths, *new_owned, *new_free_blocks, *new_free_count, *copy_from, *copy_to, *status;
+    void *workspace;
+    size_t workspace_bytes;
+} jup_paged_reorder_t;
+JUP_API jup_status_t jup_paged_reorder(const jup_paged_reorder_t *args, void *stream);
+
+/*
+ * Pages copied: of every layer's k and v (and scales), page copy_from[i] to page copy_to[i], all slots of it, or the first
+ * lengths[i] mod page_size where lengths is given (none where that is 0).  Nothing happens where one of the two is outside the pool.  No page is
+ * the target of two copies, or both source and target.
+ *   pool, scales    of the first layer, any dtype (scales NULL for JUP_F32 and JUP_BF16); a layer's k and v lie layer_stride elements
+ *                   behind the one's before it
+ * Errors: JUP_EINVAL, JUP_EDEVICE.
+ */
+typedef struct {
+    int32_t n_copies, n_layers;
+    int64_t layer_stride;
+    const int32_t *copy_from, *copy_to, *lengths;
+} jup_paged_copy_t;
+JUP_API jup_status_t jup_paged_copy(const jup_paged_pool_t *pool, const jup_paged_scales_t *scales, const jup_paged_copy_t *args, void *stream);
 
 #ifdef __cplusplus
 }

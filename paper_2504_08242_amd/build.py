@@ -9,7 +9,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libjupiter_stage.so")
 SOURCES = ["jup_api.hip", "kernels_f32.hip", "bf16_forward.hip", "bf16_gemm.hip", "bf16_attention.hip",
            "bf16_misc.hip", "kv_ops.hip", "jup_plan.hip", "w4_gemm.hip", "w4_wide.hip", "row_gemm.hip", "diag.hip",
-           "paged_api.hip", "paged_tables.hip", "paged_attention.hip", "paged_verify.hip"]
+           "paged_api.hip", "paged_tables.hip", "paged_attention.hip", "paged_verify.hip",
+           "paged_codes.hip", "paged_attention8.hip", "paged_beams.hip", "paged_reorder.hip"]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++20", "--offload-arch=gfx950", "-fPIC", "-fvisibility=hidden",

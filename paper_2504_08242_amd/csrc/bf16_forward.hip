@@ -211,10 +211,11 @@ hipError_t bf16_forward(const jup_stage& st, const void* hidden_in, int n, int p
                 rows_of.k = rows_kv.own; rows_of.v = (const u16*)rows_kv.own + (size_t)n * d;
                 rows_of.k_row_stride = rows_of.v_row_stride = 128;
                 rows_of.k_head_stride = rows_of.v_head_stride = (int64_t)n * 128;
-                e = launch_paged_append(pool, rows_of, s);
+                const bool codes = paged->scales.k != nullptr;
+                e = codes ? launch_paged_append8(pool, paged->layer_scales(l), rows_of, s) : launch_paged_append(pool, rows_of, s);
                 jup_paged_attention_t call = paged->attention;
                 call.q = q; call.out = o; call.q_row_stride = d; call.q_head_stride = 128;
-                if (e == hipSuccess) e = launch_paged_attention(pool, call, s, d >> 5);
+                if (e == hipSuccess) e = codes ? launch_paged_attention8(pool, paged->layer_scales(l), call, s, d >> 5) : launch_paged_attention(pool, call, s, d >> 5);
             } else if (bt) e = launch_branch_attention(q, o, bt->n_tok, bt->n_branches, d, H, bt_dev, max_keys, l, s, att, from_memory);
             else e = launch_chunk_attention(q, o, n, d, H, pos, kv, l, s, att, from_memory, tree_dev, shared);
         }

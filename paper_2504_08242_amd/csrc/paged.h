@@ -29,6 +29,16 @@ __device__ __forceinline__ unsigned block_number() { return blockIdx.y << kLineB
 hipError_t launch_paged_extend(const jup_paged_extend_t& a, hipStream_t s);
 hipError_t launch_paged_append(const jup_paged_pool_t& pool, const jup_paged_append_t& a, hipStream_t s);
 
+// ---- pools in 8 bits (paged_codes.hip, paged_attention8.hip) ----------------------------------------------------------
+hipError_t launch_paged_append8(const jup_paged_pool_t& pool, const jup_paged_scales_t& scales, const jup_paged_append_t& a, hipStream_t s);
+hipError_t launch_paged_read(const jup_paged_pool_t& pool, const jup_paged_scales_t* scales, const jup_paged_read_t& a, hipStream_t s);  // (of any pool)
+hipError_t launch_paged_attention8(const jup_paged_pool_t& pool, const jup_paged_scales_t& scales, const jup_paged_attention_t& a, hipStream_t s, int tiled = 0);
+
+// ---- beams (paged_beams.hip, paged_reorder.hip) --------------------------------------------------------------------------
+hipError_t launch_beam_select(const jup_beam_select_t& a, hipStream_t s);
+hipError_t launch_paged_reorder(const jup_paged_reorder_t& a, hipStream_t s);
+hipError_t launch_paged_copy(const jup_paged_pool_t& pool, const jup_paged_scales_t* scales, const jup_paged_copy_t& a, hipStream_t s);
+
 // ---- attention (paged_attention.hip) --------------------------------------------------------------------------------
 // tiled (JUP_BF16 only): 0, or out is [n_rows, n_heads * 128] in the layout of a projection's operand (tiled_offset), this many stages
 hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_attention_t& a, hipStream_t s, int tiled = 0);
@@ -42,14 +52,21 @@ hipError_t launch_verify_drafts(const jup_verify_drafts_t& a, hipStream_t s);
 struct PagedStep {
     jup_paged_pool_t pool;   // the first layer's
     int64_t layer_stride;    // elements
+    jup_paged_scales_t scales;  // the first layer's; k null: a pool of values
     const int32_t *positions, *slots;
     jup_paged_attention_t attention;
     jup_paged_pool_t layer(int l) const {
         jup_paged_pool_t p = pool;
-        const size_t at = (size_t)l * layer_stride * (pool.dtype == JUP_F32 ? 4 : 2);
+        const size_t at = (size_t)l * layer_stride * (pool.dtype == JUP_F32 ? 4 : scales.k ? 1 : 2);
         p.k = (char*)pool.k + at;
         p.v = (char*)pool.v + at;
         return p;
+    }
+    jup_paged_scales_t layer_scales(int l) const {
+        jup_paged_scales_t x = scales;
+        x.k += (size_t)l * scales.layer_stride;
+        x.v += (size_t)l * scales.layer_stride;
+        return x;
     }
 };
 

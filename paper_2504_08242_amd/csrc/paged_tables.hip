@@ -6,7 +6,7 @@
 // Sums saturate: what the arrays hold is the caller's, and a sum that wraps would pass the checks.
 // Bound by latencies (loads, prefix sum, search, loads, stores): pages and rows are looked up four at a time.  Eight requests of five
 // tokens take 4.4 µs, 1024 requests of one to 230 9.5 in two launches.
-#include "paged.h"
+#include "paged_rows.h"
 
 namespace jup {
 namespace {
@@ -229,35 +229,6 @@ __global__ __launch_bounds__(256) void extend_rows(const jup_paged_extend_t a, i
 }
 
 // ---- rows into their slots -----------------------------------------------------------------------------------------------
-// The rotation turns the pair (x_i, x_(i + D/2)) by position * theta^(-2i/D).  The host hands over the turns per position,
-// theta^(-2i/D) / 2 pi in 64 bits (one pow() and products), and a thread takes the fraction of a turn that is left in 64
-// bits too: at position 10^6 the angle has lost 10^-10 of a turn.  Sine and cosine are fp32, as is the rotation; one rounding
-// at the end.
-struct Turns {
-    double per_position[128];
-};
-__device__ __forceinline__ float2 turn(int position, double per_position) {
-    const double t = (double)position * per_position;
-    float s, c;
-    sincospif(2.0f * (float)(t - rint(t)), &s, &c);
-    return make_float2(c, s);
-}
-
-__device__ __forceinline__ void rotate8(const u32x4 lo, const u32x4 hi, const float2* cs, u32x4& out_lo, u32x4& out_hi) {
-    float x[8], y[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float a = bf2f((u16)(lo[e / 2] >> (16 * (e & 1)))), b = bf2f((u16)(hi[e / 2] >> (16 * (e & 1))));
-        x[e] = a * cs[e].x - b * cs[e].y;
-        y[e] = b * cs[e].x + a * cs[e].y;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        out_lo[e] = pack_bf16x2(x[2 * e], x[2 * e + 1]);
-        out_hi[e] = pack_bf16x2(y[2 * e], y[2 * e + 1]);
-    }
-}
-
 // One workgroup per row: 64 threads make the row's turns, then eight threads have a head of q, k or v each (two pieces of 16 bytes,
 // 64 elements apart).  Bound by memory: prompts of 365 MB in and out take 69 µs, 5.3 TB/s (a large copy: 4.9 to 5.2).
 __global__ __launch_bounds__(256) void append_bf16(const jup_paged_pool_t pool, const jup_paged_append_t a, int shift, const Turns turns) {
@@ -352,13 +323,7 @@ hipError_t launch_paged_extend(const jup_paged_extend_t& a, hipStream_t s) {
 }
 
 hipError_t launch_paged_append(const jup_paged_pool_t& pool, const jup_paged_append_t& a, hipStream_t s) {
-    Turns turns;
-    const int half = pool.head_dim / 2;
-    if (a.rope_theta > 0.0f) {
-        const double step = pow((double)a.rope_theta, -1.0 / half);
-        double t = 0.15915494309189533577;  // 1 / 2 pi
-        for (int i = 0; i < half; ++i, t *= step) turns.per_position[i] = t;
-    }
+    const Turns turns = turns_of(a.rope_theta, pool.head_dim);
     const int shift = log2_of(pool.page_size);
     if (pool.dtype == JUP_BF16)
         hipLaunchKernelGGL(append_bf16, grid_of(a.n_rows), dim3(256), 0, s, pool, a, shift, turns);

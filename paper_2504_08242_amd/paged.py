@@ -12,6 +12,14 @@ partly filled is written by the next step.  One step::
     # ... or, for a stage of this package: hidden = prefill(stage, hidden, step, k_pools, v_pools, table, max_new, workspace)
     verdict = verify(tokens, target_probs, step.row_start, u_accept, u_sample, workspace, lengths=lengths)
 
+A pool in 8 bits is two tensors of codes, int8 or float8_e4m3fn, and two of their scales, float32 [n_blocks, n_kv_heads, page_size], which
+``append``, ``attention``, ``prefill``, ``read`` and ``copy_pages`` take as ``scales=(k_scale, v_scale)``; the rows that go with it are bfloat16.  ``read``
+gets rows back out of their slots.  Where requests are the beams of a search a step ends, and the next one begins, with::
+
+    beams = beam_select(logits, scores, n_keep, workspace)
+    after = reorder(beams.parents.view(-1), table, step.lengths, step.owned, free_blocks, step.free_count, page_size, workspace)
+    copy_pages(after.copy_from, after.copy_to, k_pools, v_pools, lengths=after.lengths)
+
 Argument marshalling only: every operator is a HIP kernel of the library.  The calls are asynchronous on ``stream`` (default: the
 current one of the tensors' device) and read nothing back.  On another stream than the current one, that stream waits for what made
 the tensors that are handed in, and the caller keeps them until the call is done; results that the call makes itself are that stream's.
@@ -67,6 +75,31 @@ class _Batch(ctypes.Structure):
         ("workspace_bytes", _sz)]
 
 
+class _Scales(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("block_stride", _i64), ("head_stride", _i64), ("layer_stride", _i64)]
+
+
+class _Read(ctypes.Structure):
+    _fields_ = [("n_rows", _i32), ("k", _vp), ("v", _vp)] + [
+        (n, _i64) for n in ("k_row_stride", "k_head_stride", "v_row_stride", "v_head_stride")] + [("slots", _vp)]
+
+
+class _Beam(ctypes.Structure):
+    _fields_ = [(n, _i32) for n in ("n_seqs", "n_beams", "n_keep", "vocab", "logits_dtype", "end_token")] + [("logits", _vp), ("row_stride", _i64)] + [
+        (n, _vp) for n in ("scores", "ended", "parents", "tokens", "new_scores", "new_ended", "workspace")] + [("workspace_bytes", _sz)]
+
+
+class _Reorder(ctypes.Structure):
+    _fields_ = [(n, _i32) for n in ("n_in", "n_out", "page_size", "table_width", "new_table_width", "n_free")] + [
+        ("table_stride", _i64), ("new_table_stride", _i64)] + [
+        (n, _vp) for n in ("parents", "table", "lengths", "owned", "free_blocks", "free_count", "held", "new_table", "new_lengths", "new_owned",
+                           "new_free_blocks", "new_free_count", "copy_from", "copy_to", "status", "workspace")] + [("workspace_bytes", _sz)]
+
+
+class _Copy(ctypes.Structure):
+    _fields_ = [("n_copies", _i32), ("n_layers", _i32), ("layer_stride", _i64), ("copy_from", _vp), ("copy_to", _vp), ("lengths", _vp)]
+
+
 # The structs as one pack() each: a ctypes object of 25 fields takes longer to fill than the GPU to answer a small call.
 _FORMATS = {_i32: "i", _i64: "q", _vp: "P", _f32: "f", _sz: "N"}
 
@@ -84,6 +117,7 @@ def _packer(struct_type):
 
 
 _pack_pool, _pack_extend, _pack_append, _pack_attention, _pack_verify = map(_packer, (_Pool, _Extend, _Append, _Attention, _Verify))
+_pack_scales, _pack_read, _pack_beam, _pack_reorder, _pack_copy = map(_packer, (_Scales, _Read, _Beam, _Reorder, _Copy))
 
 _bound = None
 
@@ -99,6 +133,14 @@ def _lib():
             "jup_paged_workspace_bytes": (_sz, []),
             "jup_stage_prefill_paged": (_i32, [_vp, _vp, _i32, _vp, _vp, _vp]),
             "jup_verify_drafts": (_i32, [_vp, _vp]),
+            "jup_paged_append8": (_i32, [_vp] * 4),
+            "jup_paged_attention8": (_i32, [_vp] * 4),
+            "jup_paged_read": (_i32, [_vp] * 3),
+            "jup_paged_read8": (_i32, [_vp] * 4),
+            "jup_stage_prefill_paged8": (_i32, [_vp, _vp, _i32, _vp, _vp, _vp, _vp]),
+            "jup_beam_select": (_i32, [_vp, _vp]),
+            "jup_paged_reorder": (_i32, [_vp, _vp]),
+            "jup_paged_copy": (_i32, [_vp] * 4),
         }.items():
             fn = getattr(L, name)
             fn.restype, fn.argtypes = res, args
@@ -108,9 +150,14 @@ def _lib():
 
 Step = collections.namedtuple("Step", "row_start positions slots lengths owned free_count status")
 Verdict = collections.namedtuple("Verdict", "n_accepted next_token emitted lengths")
+Beams = collections.namedtuple("Beams", "parents tokens scores ended")
+Reordered = collections.namedtuple("Reordered", "table lengths owned free_blocks free_count copy_from copy_to status")
+
+JUP_I8, JUP_E4M3 = 3, 4
 
 _F32, _BF16, _I32, _CONTIGUOUS = torch.float32, torch.bfloat16, torch.int32, torch.contiguous_format
 _DTYPES = {_F32: jb.JUP_F32, _BF16: jb.JUP_BF16}
+_CODES = {torch.int8: JUP_I8, torch.float8_e4m3fn: JUP_E4M3}
 
 
 # (messages are made where they are needed: in a call of a few microseconds they would be half of it)
@@ -159,19 +206,56 @@ def _heads(name, t, dtype, at, rows, heads, dim, written=False):
     return t.data_ptr(), row, head
 
 
-def _pool(k_pool, v_pool):
-    """(struct, dtype, GPU number, heads, head size) of a pool."""
+def _used(t):
+    """Strides, 0 for an axis of one entry: its own says nothing."""
+    return tuple(step if size > 1 else 0 for step, size in zip(t.stride(), t.shape))
+
+
+def _pool(k_pool, v_pool, scales=None, layers=None):
+    """(struct, struct of the scales or None, dtype of rows, GPU number, heads, head size) of a pool.  layers: that of a stage's first layer,
+    with the scales' stride between layers."""
     dtype, at, shape = k_pool.dtype, k_pool.get_device(), k_pool.shape
-    if dtype not in _DTYPES or len(shape) != 4 or at < 0:
-        raise ValueError("k_pool must be a float32 or bfloat16 tensor [n_blocks, n_kv_heads, page_size, head_dim] on the GPU")
+    if scales is None:
+        if dtype not in _DTYPES or len(shape) != 4 or at < 0:
+            raise ValueError("k_pool must be a float32 or bfloat16 tensor [n_blocks, n_kv_heads, page_size, head_dim] on the GPU (with scales an int8 "
+                             "or float8_e4m3fn one)")
+    elif dtype not in _CODES or len(shape) != 4 or at < 0:
+        raise ValueError("k_pool must be an int8 or float8_e4m3fn tensor [n_blocks, n_kv_heads, page_size, head_dim] on the GPU, as there are scales")
     if v_pool.dtype is not dtype or v_pool.shape != shape or v_pool.get_device() != at:
         raise ValueError("v_pool must have the type, shape and device of k_pool")
-    strides = k_pool.stride()
-    if v_pool.stride() != strides or strides[3] != 1:
-        raise ValueError("k_pool and v_pool must have the same strides, the last one 1")
     blocks, heads, page, dim = shape
-    return (_pack_pool(k_pool.data_ptr(), v_pool.data_ptr(), strides[0], strides[1], strides[2], blocks, page, heads, dim, _DTYPES[dtype]),
-            dtype, at, heads, dim)
+    if scales is None:
+        strides = k_pool.stride()
+        if v_pool.stride() != strides or strides[3] != 1:
+            raise ValueError("k_pool and v_pool must have the same strides, the last one 1")
+        return (_pack_pool(k_pool.data_ptr(), v_pool.data_ptr(), strides[0], strides[1], strides[2], blocks, page, heads, dim, _DTYPES[dtype]),
+                None, dtype, at, heads, dim)
+    k_scale, v_scale = scales
+    for x in scales:
+        if x.dtype is not _F32 or x.get_device() != at or x.shape != shape[:3]:
+            raise ValueError(f"scales must be two float32 tensors {list(shape[:3])} on cuda:{at}, not {x.dtype} {list(x.shape)} on {x.device}")
+    strides, (block, head, step) = _used(k_pool), _used(k_scale)
+    if _used(v_pool) != strides or (strides[3] != 1 and dim > 1):
+        raise ValueError("k_pool and v_pool must have the same strides, the last one 1")
+    if _used(v_scale) != (block, head, step) or (step != 1 and page > 1):
+        raise ValueError("the scales must have the same strides, the last one 1")
+    return (_pack_pool(k_pool.data_ptr(), v_pool.data_ptr(), strides[0], strides[1], strides[2], blocks, page, heads, dim, _CODES[dtype]),
+            _pack_scales(k_scale.data_ptr(), v_scale.data_ptr(), block, head, layers or 0), _BF16, at, heads, dim)
+
+
+def _layers(k_pools, v_pools, scales):
+    """(pool of the first layer, its scales, strides between layers of the pool and of the scales) of tensors with an axis of layers."""
+    if k_pools.dim() != 5 or v_pools.shape != k_pools.shape or (k_pools.shape[0] > 1 and v_pools.stride(0) != k_pools.stride(0)):
+        raise ValueError("k_pools and v_pools must be tensors [n_layers, n_blocks, n_heads, page_size, head_dim] of the same strides")
+    if k_pools.shape[0] == 0:
+        raise ValueError("there are no layers")
+    if scales is None:
+        return (k_pools[0], v_pools[0]), None, k_pools.stride(0), 0
+    k_scale, v_scale = scales
+    if k_scale.dim() != 4 or k_scale.shape != k_pools.shape[:4] or v_scale.shape != k_scale.shape or (
+            k_scale.shape[0] > 1 and v_scale.stride(0) != k_scale.stride(0)):
+        raise ValueError(f"scales must be two float32 tensors {list(k_pools.shape[:4])} of the same strides")
+    return (k_pools[0], v_pools[0]), (k_scale[0], v_scale[0]), k_pools.stride(0), k_scale.stride(0)
 
 
 _current_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice  # (the tensors are on the GPU: it is initialised)
@@ -249,10 +333,11 @@ def extend(lengths, n_new, owned, table, free_blocks, free_count, page_size, max
     return Step(row_start, positions, slots, new_lengths, new_owned, new_count, status)
 
 
-def append(k, v, slots, k_pool, v_pool, positions=None, rope_theta=None, q=None, q_out=None, stream=None):
+def append(k, v, slots, k_pool, v_pool, positions=None, rope_theta=None, q=None, q_out=None, scales=None, stream=None):
     """Rows k, v [rows, n_kv_heads, head_dim] into their slots (jup_paged_append), k rotated at ``positions`` if rope_theta is
-    given; q [rows, n_heads, head_dim] is rotated into q_out (may be q; default: a new tensor), which is returned."""
-    pool, dtype, at, kv_heads, dim = _pool(k_pool, v_pool)
+    given; q [rows, n_heads, head_dim] is rotated into q_out (may be q; default: a new tensor), which is returned.  scales: of a pool in 8
+    bits (jup_paged_append8): the rows are quantised as they are written."""
+    pool, scale, dtype, at, kv_heads, dim = _pool(k_pool, v_pool, scales)
     rows = k.shape[0]
     k_at, *k_strides = _heads("k", k, dtype, at, rows, kv_heads, dim)
     v_at, *v_strides = _heads("v", v, dtype, at, rows, kv_heads, dim)
@@ -276,16 +361,43 @@ def append(k, v, slots, k_pool, v_pool, positions=None, rope_theta=None, q=None,
             out_at, *out_strides = _heads("q_out", q_out, dtype, at, rows, heads, dim, written=True)
     elif q_out is not None:
         raise ValueError("q_out goes with q")
-    _call(_lib().jup_paged_append, at, stream, pool,
-          _pack_append(rows, heads, q_at, k_at, v_at, out_at, *q_strides, *k_strides, *v_strides, *out_strides, positions_at, slots_at, theta))
+    args = _pack_append(rows, heads, q_at, k_at, v_at, out_at, *q_strides, *k_strides, *v_strides, *out_strides, positions_at, slots_at, theta)
+    if scale is None:
+        _call(_lib().jup_paged_append, at, stream, pool, args)
+    else:
+        _call(_lib().jup_paged_append8, at, stream, pool, scale, args)
     return q_out
 
 
-def attention(q, k_pool, v_pool, table, row_start, lengths, max_new, workspace=None, scale=None, out=None, stream=None):
+def read(slots, k_pool, v_pool, scales=None, k_out=None, v_out=None, stream=None):
+    """Rows out of their slots (jup_paged_read): k_out, v_out [rows, n_kv_heads, head_dim] (default: new tensors), zeros for slots outside the
+    pool.  scales: of a pool in 8 bits, whose rows come back as bfloat16."""
+    pool, scale, dtype, at, heads, dim = _pool(k_pool, v_pool, scales)
+    rows = slots.numel()
+    outs, places, strides = [], [], []
+    for name, out in (("k_out", k_out), ("v_out", v_out)):
+        if out is None:
+            out = _new(stream, at, lambda: torch.empty((rows, heads, dim), dtype=dtype, device=k_pool.device))
+            place, *stride = out.data_ptr(), heads * dim, dim
+        else:
+            place, *stride = _heads(name, out, dtype, at, rows, heads, dim, written=True)
+        outs.append(out)
+        places.append(place)
+        strides += stride
+    args = _pack_read(rows, *places, *strides, _ints("slots", slots, at, rows))
+    if scale is None:
+        _call(_lib().jup_paged_read, at, stream, pool, args)
+    else:
+        _call(_lib().jup_paged_read8, at, stream, pool, scale, args)
+    return tuple(outs)
+
+
+def attention(q, k_pool, v_pool, table, row_start, lengths, max_new, workspace=None, scale=None, out=None, scales=None, stream=None):
     """Attention of the rows q [rows, n_heads, head_dim] of a ragged batch over the pages (jup_paged_attention): out, of q's
     shape (default: a new tensor, whose rows outside the batch are not set).  lengths count the new tokens.  max_new: the most new tokens
-    a request is expected to have.  workspace: a ``Workspace`` (not needed by float32 pools); scale: 1 / sqrt(head_dim) if None."""
-    pool, dtype, at, kv_heads, dim = _pool(k_pool, v_pool)
+    a request is expected to have.  workspace: a ``Workspace`` (not needed by float32 pools); scale: 1 / sqrt(head_dim) if None; scales: of a
+    pool in 8 bits (jup_paged_attention8)."""
+    pool, code_scales, dtype, at, kv_heads, dim = _pool(k_pool, v_pool, scales)
     n = lengths.numel()
     if q.dim() != 3:
         raise ValueError("q must be a tensor [rows, n_heads, head_dim]")
@@ -297,23 +409,28 @@ def attention(q, k_pool, v_pool, table, row_start, lengths, max_new, workspace=N
     else:
         out_at, *out_strides = _heads("out", out, dtype, at, rows, heads, dim, written=True)
     tables, width, stride = _table(table, at, n)
-    _call(_lib().jup_paged_attention, at, stream, pool,
-          _pack_attention(n, rows, heads, int(max_new), width, stride, q_at, out_at, *q_strides, *out_strides,
-                          _ints("row_start", row_start, at, n + 1), _ints("lengths", lengths, at, n), tables,
-                          1.0 / math.sqrt(dim) if scale is None else scale,
-                          *(_scratch(workspace, at, stream) if workspace is not None or dtype is not _F32 else (0, 0))))
+    args = _pack_attention(n, rows, heads, int(max_new), width, stride, q_at, out_at, *q_strides, *out_strides,
+                           _ints("row_start", row_start, at, n + 1), _ints("lengths", lengths, at, n), tables,
+                           1.0 / math.sqrt(dim) if scale is None else scale,
+                           *(_scratch(workspace, at, stream) if workspace is not None or dtype is not _F32 else (0, 0)))
+    if code_scales is None:
+        _call(_lib().jup_paged_attention, at, stream, pool, args)
+    else:
+        _call(_lib().jup_paged_attention8, at, stream, pool, code_scales, args)
     return out
 
 
-def prefill(stage, hidden_in, step, k_pools, v_pools, table, max_new, workspace=None, hidden_out=None, stream=None):
+def prefill(stage, hidden_in, step, k_pools, v_pools, table, max_new, workspace=None, hidden_out=None, scales=None, stream=None):
     """A ``binding.Stage`` over the rows hidden_in [rows, d_model] of a ragged batch (jup_stage_prefill_paged): hidden_out (default: a new
-    tensor).  step: what ``extend`` returned; k_pools, v_pools [n_layers, n_blocks, n_heads, page_size, head_dim]."""
+    tensor).  step: what ``extend`` returned; k_pools, v_pools [n_layers, n_blocks, n_heads, page_size, head_dim]; scales: of pools in 8
+    bits, [n_layers, n_blocks, n_heads, page_size] each (jup_stage_prefill_paged8)."""
     if k_pools.dim() != 5 or v_pools.shape != k_pools.shape or k_pools.shape[0] != stage.cfg["n_layers"] or (
             k_pools.shape[0] > 1 and v_pools.stride(0) != k_pools.stride(0)):
         raise ValueError(f"k_pools and v_pools must be tensors [{stage.cfg['n_layers']}, n_blocks, n_heads, page_size, head_dim] of the same strides")
     if k_pools.shape[0] == 0:
         raise ValueError("a stage without layers has no pools")
-    packed, dtype, at, _, _ = _pool(k_pools[0], v_pools[0])
+    first, first_scales, layer_stride, scale_stride = _layers(k_pools, v_pools, scales)
+    packed, code_scales, dtype, at, _, _ = _pool(*first, first_scales, scale_stride)
     n, rows, width = step.lengths.numel(), hidden_in.shape[0], stage.cfg["d_model"]
     for name, t in (("hidden_in", hidden_in), ("hidden_out", hidden_in if hidden_out is None else hidden_out)):
         if t.dtype is not dtype or t.get_device() != at or t.shape != (rows, width) or not t.is_contiguous():
@@ -324,13 +441,13 @@ def prefill(stage, hidden_in, step, k_pools, v_pools, table, max_new, workspace=
         raise ValueError(f"the step has positions of {step.positions.numel()} rows, hidden_in {rows}")
     tables, table_width, stride = _table(table, at, n)
     scratch = _scratch(workspace, at, stream) if workspace is not None or dtype is not _F32 else (0, 0)
-    batch = _Batch(_Pool.from_buffer_copy(packed), k_pools.stride(0), n, int(max_new), table_width, stride, _ints("row_start", step.row_start, at, n + 1),
+    batch = _Batch(_Pool.from_buffer_copy(packed), layer_stride, n, int(max_new), table_width, stride, _ints("row_start", step.row_start, at, n + 1),
                    _ints("lengths", step.lengths, at, n), tables, _ints("positions", step.positions, at, step.positions.numel()),
                    _ints("slots", step.slots, at, step.slots.numel()), *scratch)
     if hidden_out is None:
         hidden_out = _new(stream, at, lambda: torch.empty_like(hidden_in))
-    fn = _lib().jup_stage_prefill_paged
-    _call(lambda handle: fn(stage.handle, hidden_in.data_ptr(), rows, ctypes.byref(batch), hidden_out.data_ptr(), handle), at, stream)
+    fn, given = (_lib().jup_stage_prefill_paged, ()) if code_scales is None else (_lib().jup_stage_prefill_paged8, (code_scales,))
+    _call(lambda handle: fn(stage.handle, hidden_in.data_ptr(), rows, ctypes.byref(batch), *given, hidden_out.data_ptr(), handle), at, stream)
     return hidden_out
 
 
@@ -378,3 +495,83 @@ def verify(tokens, target_probs, row_start, u_accept, u_sample, workspace, draft
                        draft, target_stride, draft_stride, _uniforms("u_accept", u_accept, at, rows), _uniforms("u_sample", u_sample, at, n),
                        base, base + 4 * n, base + 8 * n, lengths_at, after_at, *_scratch(workspace, at, stream)))
     return Verdict(n_accepted, next_token, emitted, new_lengths)
+
+
+def _floats(name, t, at, n):
+    if t.dtype is not _F32 or t.get_device() != at or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous float32 tensor of {n} on cuda:{at}, not {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def beam_select(logits, scores, n_keep, workspace, end_token=-1, ended=None, stream=None):
+    """The best continuations over the beams and the vocabulary (jup_beam_select): ``Beams(parents, tokens, scores, ended)``, [n_requests,
+    n_keep] each, best first.  scores [n_requests, n_beams] float32, sums of log probabilities; logits [n_requests * n_beams, vocab] float32 or
+    bfloat16; ended [n_requests, n_beams] int32: not 0 where a beam has come to end_token."""
+    dtype, at = logits.dtype, logits.get_device()
+    if dtype not in _DTYPES or logits.dim() != 2 or at < 0:
+        raise ValueError("logits must be a float32 or bfloat16 tensor [rows, vocab] on the GPU")
+    if scores.dim() != 2 or scores.numel() != logits.shape[0]:
+        raise ValueError(f"scores must be a tensor [n_requests, n_beams] of as many as there are rows of logits ({logits.shape[0]}), not {list(scores.shape)}")
+    (n, beams), (rows, vocab), keep = scores.shape, logits.shape, int(n_keep)
+    logits_at, stride = _probs("logits", logits, dtype, at, rows, vocab)
+    scores_at = _floats("scores", scores, at, rows)
+    if ended is not None and ended.shape != scores.shape:
+        raise ValueError(f"ended must have the shape of scores, not {list(ended.shape)}")
+    ended_at = 0 if ended is None else _ints("ended", ended, at, n, beams)
+    if not 0 < keep <= 64:
+        raise ValueError(f"n_keep={keep} is outside 1..64")
+    made = _new(stream, at, lambda: torch.empty((4, n, keep), dtype=_I32, device=logits.device))
+    parents, tokens, new_scores, new_ended = made.unbind()
+    base, size = made.data_ptr(), 4 * n * keep
+    _call(_lib().jup_beam_select, at, stream,
+          _pack_beam(n, beams, keep, vocab, _DTYPES[dtype], int(end_token), logits_at, stride, scores_at, ended_at, base, base + size, base + 2 * size,
+                     base + 3 * size, *_scratch(workspace, at, stream)))
+    return Beams(parents, tokens, new_scores.view(_F32), new_ended)
+
+
+def reorder(parents, table, lengths, owned, free_blocks, free_count, page_size, workspace, held=None, width=None, in_place=False, stream=None):
+    """Block tables of requests that go on from others (jup_paged_reorder): ``Reordered(table, lengths, owned, free_blocks, free_count, copy_from,
+    copy_to, status)``, int32 tensors of parents.numel() requests.  parents: rows of ``table``, or -1; free_blocks has room for every block of the
+    pool; held: uint8, one per entry of free_blocks, not 0 for blocks that others hold; width: of the new table (default: table's).
+    in_place: free_blocks and free_count are updated themselves.  The copies that are due: ``copy_pages``."""
+    at, n, n_in, n_free = parents.get_device(), parents.numel(), lengths.numel(), free_blocks.numel()
+    if at < 0:
+        raise ValueError("parents must be on the GPU")
+    parents_at = _ints("parents", parents, at, n)
+    tables, old_width, stride = _table(table, at, n_in)
+    inputs = (_ints("lengths", lengths, at, n_in), _ints("owned", owned, at, n_in), _ints("free_blocks", free_blocks, at, n_free),
+              _ints("free_count", free_count, at, 1))
+    if held is not None and (held.dtype is not torch.uint8 or held.get_device() != at or held.shape != (n_free,) or not held.is_contiguous()):
+        raise ValueError(f"held must be a contiguous uint8 tensor [{n_free}] on cuda:{at}, not {held.dtype} {list(held.shape)} on {held.device}")
+    width = old_width if width is None else int(width)
+    if width < 0:
+        raise ValueError("width must not be negative")
+    sizes = [n, n, n, n, 1, n * width] + ([] if in_place else [1, n_free])
+    made = _new(stream, at, lambda: parents.new_empty(sum(sizes)))
+    new_lengths, new_owned, copy_from, copy_to, status, new_table, *new = made.split_with_sizes(sizes)
+    new_table = new_table.view(n, width)
+    new_count, new_free = (free_count, free_blocks) if in_place else new
+    base = made.data_ptr()
+    status_at = base + 16 * n
+    table_at = status_at + 4
+    after = (inputs[2], inputs[3]) if in_place else (table_at + 4 * n * width + 4, table_at + 4 * n * width)
+    _call(_lib().jup_paged_reorder, at, stream,
+          _pack_reorder(n_in, n, int(page_size), old_width, width, n_free, stride, width, parents_at, tables, *inputs,
+                        0 if held is None else held.data_ptr(), table_at, base, base + 4 * n, *after, base + 8 * n, base + 12 * n, status_at,
+                        *_scratch(workspace, at, stream)))
+    return Reordered(new_table, new_lengths, new_owned, new_free, new_count, copy_from, copy_to, status)
+
+
+def copy_pages(copy_from, copy_to, k_pools, v_pools, lengths=None, scales=None, stream=None):
+    """Pages copy_from[i] to copy_to[i] of every layer (jup_paged_copy), whole ones, or with lengths the first lengths[i] mod page_size slots.
+    k_pools, v_pools, scales: of one layer, or with an axis of layers in front."""
+    if k_pools.dim() == 5:
+        first, first_scales, layer_stride, scale_stride = _layers(k_pools, v_pools, scales)
+        layers = k_pools.shape[0]
+    else:
+        first, first_scales, layer_stride, scale_stride, layers = (k_pools, v_pools), scales, 0, 0, 1
+    pool, code_scales, _, at, _, _ = _pool(*first, first_scales, scale_stride)
+    n = copy_from.numel()
+    _call(_lib().jup_paged_copy, at, stream, pool, code_scales,
+          _pack_copy(n, layers, layer_stride, _ints("copy_from", copy_from, at, n), _ints("copy_to", copy_to, at, n),
+                     0 if lengths is None else _ints("lengths", lengths, at, n)))
