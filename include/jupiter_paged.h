@@ -159,7 +159,7 @@ JUP_API jup_status_t jup_paged_attention(const jup_paged_pool_t *pool, const jup
 /*
  * The same for pools in 8 bits.  Append: k is rotated in fp32 and quantised without another rounding.  Attention: the scale of a key
  * multiplies its score, that of a value its probability, and the product is what is rounded to bf16; codes are exact in bf16.  A score or a
- * value of a key that a row does not see does not reach it, whatever codes and scales hold.  JUP_I8 codes of -128 and JUP_E4M3 codes that are
+ * value of a key that a row does not see does not reach it, whatever codes and scales hold; nor does a value whose probability is 0 in fp32.  JUP_I8 codes of -128 and JUP_E4M3 codes that are
  * no numbers, which jup_paged_append8() does not write, count as what they are.  Errors: JUP_EINVAL, JUP_EDEVICE.
  */
 JUP_API jup_status_t jup_paged_append8(const jup_paged_pool_t *pool, const jup_paged_scales_t *scales, const jup_paged_append_t *args, void *stream);

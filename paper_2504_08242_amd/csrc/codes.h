@@ -52,4 +52,9 @@ __device__ __forceinline__ u32x2 bf16_of(unsigned w) {
     }
 }
 
+// x * y, 0 where x or y is (the instruction by its intrinsic, which has no builtin: the compiler knows what waits it needs).
+__device__ float product_or_0(float x, float y) __asm("llvm.amdgcn.fmul.legacy");
+// A probability times the scale of its value: 0 where the probability is, whatever the scale holds (a key that the row does not see).
+__device__ __forceinline__ float scaled(float p, float scale) { return product_or_0(p, scale); }
+
 }  // namespace jup

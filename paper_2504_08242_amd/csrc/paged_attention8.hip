@@ -1,89 +1,317 @@
-// Attention of the new tokens of a ragged batch over a pool in 8 bits (include/jupiter_paged.h).
-#include "codes.h"
+// Attention of the new tokens of a ragged batch over a paged cache of 8-bit codes (include/jupiter_paged.h); rows, tiles and pieces:
+// paged_work.h.
+//
+// Codes are exact in bf16, so products are those of bf16 operands.  Scores are sums over a key's codes times the key's scale; a value's scale goes
+// with its probability, s_j p_j, which is rounded to bf16 as the operand of the second product: 2^-8 of it, as in a cache of bf16 values.
+#include "paged_many.h"
 
 namespace jup {
 namespace {
 
-// One wave per (row, query head): 64 keys at a time, a lane has a key's score, then two columns of the output.
-template <int CODE>
-__global__ __launch_bounds__(64) void attention_plain(const jup_paged_pool_t pool, const jup_paged_scales_t scales, const jup_paged_attention_t a, int shift, int tiled) {
-    __shared__ float q[128];
-    const int lane = threadIdx.x, row = (int)(block_number() / (unsigned)a.n_heads), head = (int)block_number() - row * a.n_heads;
-    if (row >= a.n_rows) return;
-    const int kv_head = head / (a.n_heads / pool.n_kv_heads);
-    int lo = 0, hi = a.n_seqs;  // the request: the last one that begins at or before the row
-    if (row < a.row_start[0]) return;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.row_start[mid] <= row) lo = mid;
-        else hi = mid;
+constexpr int kTileBytes = kKT * 128;  // a K or V tile: 32 rows of 128 codes
+
+// Transposing 8-byte LDS read: within each group of 16 lanes, lane i receives as byte r byte (i & 7) of the 8 bytes addressed by lane
+// 2r + (i >> 3) of the group.
+__device__ __forceinline__ u32x2 read_tr8(unsigned lds_address) {
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    typedef __attribute__((address_space(3))) i32x2* lds_ptr;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_ptr)(size_t)lds_address));
+}
+
+// 4 bytes per lane straight into LDS (see load_to_lds_16).
+__device__ inline void load_to_lds_4(const void* gptr, unsigned lds_base) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(gptr), "s"(lds_base) : "memory", "m0");
+}
+
+// A 16-byte piece of a row of values in a masked tile; there: the row is a key.  True: something was taken out of it.
+__device__ __forceinline__ bool clean_piece8(unsigned char* at, bool there) {
+    u32x4 v = *(const u32x4*)at;
+    const bool taken = clean_codes(v, there);
+    if (taken || !there) *(u32x4*)at = v;
+    return taken;
+}
+
+// ---- few rows ----------------------------------------------------------------------------------------------------------------
+// As attention_few: a tile has QW = 16 or 32 rows, and the waves divide the piece's key tiles, each alone with its own places in LDS.  A tile is half
+// as long in bytes, so a wave has places for two, and as many bytes are in flight on a CU.
+// LDS tiles, rows of 128 bytes in 8 chunks of 16:  K: chunk ch of row r at position ch ^ (r / 2 & 7);  V: at ch ^ turn(r), such that the rows of a
+// transposing read lie in different banks.  Behind them the scales of the tile's keys and values, 32 each.
+// K is read 16 codes at a time, two steps of the product: step (j, s) has the features 16 (chunk of j) + 8 s .. + 7, and queries are read so too.
+template <int QW, int NW>
+struct Few8 {
+    static constexpr int kScales = 2 * kTileBytes;             // of a place: K tile, V tile, scales
+    static constexpr int kPlace = kScales + 256;
+    static constexpr int kWave = 2 * kPlace;
+    static constexpr int kQ = NW * kWave;                      // the tile of rows: 256 bytes each, chunk ch at position ch ^ (r & 15)
+    static constexpr int kStat = kQ + QW * 256;                // [2][waves][QW] maxima and sums
+    static constexpr int kLds = kStat + 2 * NW * QW * 4;
+    static_assert(NW * QW * 132 * 4 <= kStat, "merge regions overlap the statistics");
+    static_assert((8 / NW) * kLds <= 160 * 1024, "two workgroups of four waves share a CU");
+    // position of 16-byte chunk ch of V row r: ch ^ turn(r)
+    static __device__ __forceinline__ int turn(int r) {
+        return QW == 16 ? ((r >> 1) & 3) | ((r >> 4) & 1) << 2 : ((r >> 1) & 1) << 1 | ((r >> 3) & 1) << 2;
     }
-    const int end = a.row_start[lo + 1];
-    if (row >= end) return;
-    const long long last = min((long long)a.lengths[lo] - (end - row), ((long long)a.table_width << shift) - 1);
-    const int* table = a.table + lo * a.table_stride;
-    for (int i = lane; i < 128; i += 64) q[i] = bf2f(((const u16*)a.q)[row * a.q_row_stride + head * a.q_head_stride + i]);
-    __syncthreads();
-    float m = -INFINITY, l = 0.f, acc[2] = {0.f, 0.f};
-    for (long long first = 0; first <= last; first += 64) {
-        const long long key = first + lane;
-        long long at = -1;
-        float s = -INFINITY, v_scale = 0.f;
-        if (key <= last) {
-            const int block = table[key >> shift];
-            if (block >= 0 && block < pool.n_blocks) {
-                const long long in = key & ((1 << shift) - 1), scale_at = block * scales.block_stride + kv_head * scales.head_stride + in;
-                at = block * pool.block_stride + kv_head * pool.head_stride + in * pool.slot_stride;
-                const u8* k = (const u8*)pool.k + at;
-                float sum = 0.f;
-                for (int i = 0; i < 128; i += 4) {
-                    float x[4];
-                    numbers_of<CODE>(*(const unsigned*)(k + i), x);
-                    for (int e = 0; e < 4; ++e) sum = __builtin_fmaf(q[i + e], x[e], sum);
+};
+
+template <int CODE, int QW, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void attention_few8(const Attention8 args, int least) {
+    typedef Few8<QW, NW> L;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & (QW - 1), hh = lane / QW;
+    const int kv_head = (int)(block_number() % (unsigned)args.n_kv_heads), item = (int)(block_number() / (unsigned)args.n_kv_heads);
+    Work w;
+    if (!find_work<QW>(args, item, least, w)) return;
+    w.make_uniform();
+    const Attention8 a = args_again<Attention8>();
+    const int G = a.group.d;
+    const int rows = min(QW, w.tokens * G - w.tile * QW);
+    const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_byte_address(lds));
+
+    // the rows of q into LDS; past the last one, that one again
+    {
+        const int lrow = lane >> 4, lp = lane & 15;
+        for (int r0 = 4 * wave; r0 < QW; r0 += 4 * NW) {
+            const int r = r0 + lrow;
+            const int row = w.tile * QW + min(r, rows - 1), token = a.group.of(row);
+            const u16* from = a.q + (long long)(w.begin + token) * a.q_row + (long long)(kv_head * G + row - token * G) * a.q_head;
+            load_to_lds_16(from + (lp ^ (r & 15)) * 8, lds0 + L::kQ + r0 * 256);
+        }
+    }
+    const int last_key = w.keys - 1;
+    const int my_token = a.group.of(w.tile * QW + min(c, rows - 1));
+    const int q_abs = w.before + my_token;                                          // the last key this lane's row sees
+    const int first_token = a.group.of(w.tile * QW);
+    const int first_masked = (int)max((long long)w.before + first_token + 1, 0ll) / kKT;  // tiles before it: every row sees every key
+    const int* table_row = (const int*)uniform_ptr((const char*)(a.table + w.seq * a.table_row));
+    const u8* k_pool = (const u8*)a.k + kv_head * a.head;
+    const u8* v_pool = (const u8*)a.v + kv_head * a.head;
+    const unsigned row_bytes = (unsigned)a.slot;
+    const float* my_scales = (lane < 32 ? a.k_scale : a.v_scale) + kv_head * a.scale_head;  // (a lane has a key's or a value's)
+    const int lrow = lane >> 3, lp = lane & 7;
+
+    // where tile number n (of this wave) lies: places take turns
+    auto place = [&](int n) __attribute__((always_inline)) { return lds0 + wave * L::kWave + (n & 1) * L::kPlace; };
+    auto fill = [&](int tile, int n, const Blocks& b, bool v_part) __attribute__((always_inline)) {
+        unsigned slot = place(n) + (v_part ? kTileBytes : 0);
+        asm volatile("" : "+v"(slot));  // (see attention_few)
+        const unsigned dst = __builtin_amdgcn_readfirstlane(slot);
+        if (!v_part) {
+            const int g = (lane >> 3) & 3, block = g == 0 ? b.id[0] : g == 1 ? b.id[1] : g == 2 ? b.id[2] : b.id[3];
+            const int at = (unsigned)block < (unsigned)a.n_blocks ? block : 0;
+            load_to_lds_4(my_scales + at * a.scale_block + ((tile * kKT + (lane & 31)) & ((1 << a.shift) - 1)), dst + L::kScales);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {  // eight rows (1 KB): lane i lands at row 8j + (i >> 3), position i & 7
+            const char* base = group_base(a, v_part ? v_pool : k_pool, b.id[j], tile * kKT + 8 * j);
+            const int r = 8 * j + lrow;
+            load_to_lds_16(base, lrow * row_bytes + (lp ^ (v_part ? L::turn(r) : (r >> 1) & 7)) * 16, dst + j * 1024);
+        }
+    };
+    // loads of a tile, in order: scales and K (5), V (4); two tiles are on their way
+    int tile = w.tile_lo + wave, n = 0;
+    Blocks here{}, next{}, third{};
+    if (tile < w.tile_hi) {
+        here = blocks_of(a, table_row, tile, last_key);
+        if (tile + NW < w.tile_hi) next = blocks_of(a, table_row, tile + NW, last_key);
+        fill(tile, 0, here, false);
+        fill(tile, 0, here, true);
+        if (tile + NW < w.tile_hi) {
+            fill(tile + NW, 1, next, false);
+            fill(tile + NW, 1, next, true);
+            if (tile + 2 * NW < w.tile_hi) third = blocks_of(a, table_row, tile + 2 * NW, last_key);
+            asm volatile("s_waitcnt vmcnt(18)" ::: "memory");  // the rows of q have landed, the tiles are on their way
+        } else {
+            asm volatile("s_waitcnt vmcnt(9)" ::: "memory");
+        }
+    } else {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+
+    constexpr int KS = QW == 16 ? 4 : 8;   // MFMA steps over the head's 128 features
+    constexpr int NS = QW == 16 ? 8 : 16;  // scores of a tile per lane
+    constexpr int DB = QW == 16 ? 8 : 4;   // output blocks of QW features
+    constexpr int NR = QW == 16 ? 4 : 16;  // registers of one
+    typedef float acc_t __attribute__((ext_vector_type(NR)));
+    // step 2 j + s has the features 16 ch + 8 s .., ch = hh + 4 j (QW = 16) or hh + 2 j
+    constexpr int kNext = QW == 16 ? 4 : 2;
+    bf16x8 qf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+        qf[ks] = *(const bf16x8*)(lds + L::kQ + c * 256 + (((2 * (hh + kNext * (ks >> 1)) + (ks & 1)) ^ (c & 15)) * 16));
+    acc_t oacc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < NR; ++r) oacc[db][r] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+    const unsigned k_lane = c * 128 + ((hh ^ ((c >> 1) & 7)) * 16);
+    // transposing reads: lane 2 r + x of a group of 16 addresses half x of row r's chunk; rows are keys in the order of the scores
+    const int quad = lane >> 4, s = lane & 15;
+    const int vt_row = QW == 16 ? 4 * quad + 16 * (s >> 3) + ((s >> 1) & 3) : 4 * (quad >> 1) + 8 * (s >> 3) + ((s >> 1) & 3);
+    const unsigned v_lane = kTileBytes + vt_row * 128 + (((QW == 16 ? 0 : quad & 1) ^ L::turn(vt_row)) * 16) + 8 * (s & 1);
+    auto key_of = [](int r) { return (QW == 16 ? 16 : 8) * (r >> 2) + (r & 3); };  // of the lane's score r, less 4 hh
+    bool special = false;  // codes that are no numbers were taken out of a tile (of this lane's pieces)
+
+    for (; tile < w.tile_hi; tile += NW, ++n) {
+        const bool more = tile + NW < w.tile_hi, further = tile + 2 * NW < w.tile_hi;
+        const unsigned there = rows_there(a, here, tile, last_key);
+        const unsigned my_place = place(n);
+        const unsigned char* k_base = lds + (my_place - lds0);
+        if (more) asm volatile("s_waitcnt vmcnt(13)" ::: "memory");  // the scales and the K tile have landed
+        else asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+
+        // ---- S^T = K Q^T, and both kinds of scales ----
+        float sv[NS], vs[NS];
+        {
+            f32x4 ks[NS / 4], vx[NS / 4];
+#pragma unroll
+            for (int x = 0; x < NS / 4; ++x) {
+                ks[x] = *(const f32x4*)(k_base + L::kScales + ((QW == 16 ? 16 : 8) * x + 4 * hh) * 4);
+                vx[x] = *(const f32x4*)(k_base + L::kScales + 128 + ((QW == 16 ? 16 : 8) * x + 4 * hh) * 4);
+            }
+            u32x4 kc[4];
+            if constexpr (QW == 16) {
+#pragma unroll
+                for (int f = 0; f < 4; ++f) kc[f] = *(const u32x4*)(k_base + (f >> 1) * 2048 + (k_lane ^ (64 * (f & 1))));  // key half, j
+                f32x4 sacc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    const int half = x & 1, step = x >> 1;
+                    const u32x4 k4 = kc[2 * half + (step >> 1)];
+                    sacc[half] = mfma16(operand<CODE>(k4[2 * (step & 1)], k4[2 * (step & 1) + 1]), qf[step], sacc[half]);
                 }
-                s = sum * scales.k[scale_at] * a.scale;
-                v_scale = scales.v[scale_at];
+#pragma unroll
+                for (int r = 0; r < NS; ++r) sv[r] = sacc[r >> 2][r & 3];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) kc[j] = *(const u32x4*)(k_base + (k_lane ^ (32 * j)));
+                f32x16 sacc;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sacc[r] = 0.f;
+#pragma unroll
+                for (int step = 0; step < 8; ++step)
+                    sacc = mfma32(operand<CODE>(kc[step >> 1][2 * (step & 1)], kc[step >> 1][2 * (step & 1) + 1]), qf[step], sacc);
+#pragma unroll
+                for (int r = 0; r < NS; ++r) sv[r] = sacc[r];
+            }
+#pragma unroll
+            for (int r = 0; r < NS; ++r) {
+                sv[r] *= ks[r >> 2][r & 3];
+                vs[r] = vx[r >> 2][r & 3];
             }
         }
-        float top = s;
-        const bool nan = s != s;
-        for (int by = 32; by > 0; by >>= 1) top = fmaxf(top, __shfl_xor(top, by, 64));
-        const float m_new = fmaxf(m, top);
-        if (m_new == -INFINITY && !__any(nan)) continue;
-        const float back = m == -INFINITY ? 0.f : expf(m - m_new);
-        const float p = at < 0 ? 0.f : expf(s - m_new);
-        float sum = p;
-        for (int by = 32; by > 0; by >>= 1) sum += __shfl_xor(sum, by, 64);
-        l = l * back + sum;
-        m = m_new;
-        acc[0] *= back;
-        acc[1] *= back;
-        const float pv = at < 0 ? 0.f : p * v_scale;
-        for (int j = 0; j < 64; ++j) {
-            const long long from = __shfl(at, j, 64);
-            const float w = __shfl(pv, j, 64);
-            if (from < 0) continue;
-            float x[4];
-            numbers_of<CODE>(((const u8*)pool.v)[from + lane] | ((const u8*)pool.v)[from + 64 + lane] << 8, x);
-            acc[0] = __builtin_fmaf(w, x[0], acc[0]);
-            acc[1] = __builtin_fmaf(w, x[1], acc[1]);
+        if (further) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the K tile and the scales have been read
+            fill(tile + 2 * NW, n, third, false);
+        }
+
+        // ---- online softmax (see attention_few) ----
+        const bool masked = tile >= first_masked || there != ~0u;
+        if (masked) {
+            int quarter = 4 * hh;
+            asm volatile("" : "+v"(quarter));
+#pragma unroll
+            for (int r = 0; r < NS; ++r) {
+                const int key = quarter + key_of(r);
+                if (tile * kKT + key > q_abs || !((there >> key) & 1)) sv[r] = -INFINITY;
+            }
+        }
+        float mt = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < NS; ++r) mt = fmaxf(mt, sv[r]);
+        if constexpr (QW == 16) mt = max_across_rows(mt);
+        mt = max_across_halves(mt) * a.scale_log2e;  // the scale is positive
+        const bool grow = mt > m_run + 8.0f;
+        const float m_new = grow ? mt : m_run;
+        const float m_safe = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = grow ? __builtin_amdgcn_exp2f(m_run - m_safe) : 1.0f;
+        const bool rescale = grow && m_run != -INFINITY;
+        float ps = 0.f;
+        bf16x8 pf[NS / 8];
+#pragma unroll
+        for (int r = 0; r < NS; ++r) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[r], a.scale_log2e, -m_safe));
+            ps += p;
+            pf[r >> 3][r & 7] = (__bf16)scaled(p, vs[r]);  // the operand of the second product: 2^-8 of each
+        }
+        l_run = l_run * alpha + ps;
+        m_run = m_new;
+        if (__any(rescale)) {
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int r = 0; r < NR; ++r) oacc[db][r] *= alpha;
+        }
+
+        // ---- O^T += V^T P^T ----
+        if (further) asm volatile("s_waitcnt vmcnt(14)" ::: "memory");  // V has landed
+        else if (more) asm volatile("s_waitcnt vmcnt(9)" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (CODE == JUP_E4M3 && masked) {
+            asm volatile("");
+#pragma unroll
+            for (int j = 0; j < 4; ++j)  // rows 8j .. 8j + 7
+                special |= clean_piece8(lds + (my_place - lds0) + kTileBytes + j * 1024 + lane * 16, (there >> (8 * j + lrow)) & 1);
+        }
+#pragma unroll
+        for (int f = 0; f < 8; ++f) {
+            // QW = 32: feature block f / 2, key half f % 2; QW = 16: feature block f, all 32 keys
+            const u32x2 codes = read_tr8(my_place + (QW == 16 ? v_lane ^ (16 * f) : (v_lane ^ (32 * (f / 2))) + (f % 2) * 2048));
+            const bf16x8 v = operand<CODE>(codes[0], codes[1]);
+            if constexpr (QW == 16) oacc[f] = mfma16(v, pf[0], oacc[f]);
+            else oacc[f / 2] = mfma32(v, pf[f % 2], oacc[f / 2]);
+        }
+        here = next;
+        next = third;
+        if (further) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the V tile has been read
+            fill(tile + 2 * NW, n, next, true);
+            if (tile + 3 * NW < w.tile_hi) third = blocks_of(a, table_row, tile + 3 * NW, last_key);
         }
     }
-    for (int x = 0; x < 2; ++x) {
-        const int i = lane + 64 * x;
-        u16* out = (u16*)a.out + (tiled ? (long long)tiled_offset(row, head * 16 + (i >> 3), tiled) + (i & 7) : row * a.out_row_stride + head * a.out_head_stride + i);
-        *out = f2bf(l == 0.f ? 0.f : acc[x] / l);
+
+    if (CODE == JUP_E4M3 && __any(special)) {  // once in a blue moon
+        for (tile = w.tile_lo + wave; tile < w.tile_hi; tile += NW) {
+            const Blocks b = blocks_of(a, table_row, tile, last_key);
+            const unsigned there = rows_there(a, b, tile, last_key);
+            if (tile < first_masked && there == ~0u) continue;
+            for (int k = 0; k < kKT; ++k) {
+                if (!((there >> k) & 1)) continue;
+                const char* row = group_base(a, v_pool, table_row[(tile * kKT + k) >> a.shift], tile * kKT + (k & ~7)) + (k & 7) * row_bytes;
+                if (!row_not_finite<CODE>(row)) continue;
+#pragma unroll
+                for (int x = 0; x < (QW == 16 ? 8 : 16); ++x) {
+                    const int db = QW == 16 ? x : x >> 2, r = QW == 16 ? 0 : 4 * (x & 3);
+                    add_not_finite<CODE>(oacc[db], r, row, (QW == 16 ? 16 * x : 8 * x) + 4 * hh, tile * kKT + k <= q_abs);
+                }
+            }
+        }
     }
+
+    // ---- the waves' sums put together ----
+    merge_few<QW, NW, L::kStat>(w, kv_head, rows, c, hh, m_run, l_run, oacc, lds);
 }
+
+template <int CODE>
+struct Kernels8 {
+    template <int QW, int NW> static auto few() { return attention_few8<CODE, QW, NW>; }
+    template <int QW, int NW> static constexpr int few_lds() { return Few8<QW, NW>::kLds; }
+    template <int KP, int NT, int SUB> static auto many() { return attention_many<CODE, 8, KP, NT, SUB, 2>; }
+    template <int KP, int NT, int SUB> static constexpr int many_lds() { return Many<8, KP, NT, SUB, true>::kLds; }
+};
 
 }  // namespace
 
-hipError_t launch_paged_attention8(const jup_paged_pool_t& pool, const jup_paged_scales_t& scales, const jup_paged_attention_t& a, hipStream_t s, int tiled) {
-    const int shift = log2_of(pool.page_size);
-    const dim3 grid = grid_of((long long)a.n_rows * a.n_heads);
-    if (pool.dtype == JUP_I8) hipLaunchKernelGGL(attention_plain<JUP_I8>, grid, dim3(64), 0, s, pool, scales, a, shift, tiled);
-    else hipLaunchKernelGGL(attention_plain<JUP_E4M3>, grid, dim3(64), 0, s, pool, scales, a, shift, tiled);
-    return hipGetLastError();
+hipError_t launch_paged_attention8(const jup_paged_pool_t& pool, const jup_paged_scales_t& scales, const jup_paged_attention_t& c, hipStream_t s, int tiled) {
+    Attention8 a{};
+    set_call(a, pool, c, tiled);
+    a.k_scale = scales.k; a.v_scale = scales.v;
+    a.scale_block = scales.block_stride; a.scale_head = scales.head_stride;
+    return pool.dtype == JUP_I8 ? launch_tiles<Kernels8<JUP_I8>>(a, c, s) : launch_tiles<Kernels8<JUP_E4M3>>(a, c, s);
 }
 
 }  // namespace jup
