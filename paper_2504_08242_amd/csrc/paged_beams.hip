@@ -12,7 +12,7 @@ typedef unsigned long long u64;
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMost = JUP_BEAM_MOST;
-constexpr float kLog2e = 1.4426950408889634f, kLog2eRest = 1.9259629911266175e-08f;  // log2(e) = the sum, to 2^-50
+constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ u64 key_of(float x, int token) {  // x finite, -0 as 0
     const unsigned bits = __float_as_uint(x + 0.0f);
@@ -36,38 +36,71 @@ __device__ __forceinline__ u64 left(const u64* at) {
 // counted, all lanes at once) and the last of these is the limit for those that follow.  Indices only rise: what equals the limit is behind it.
 constexpr int kStep = 64 * 8;  // logits of a wave at a time, at most
 struct Best {
-    u64 found[64 + kStep], kept[kMost];
+    u64 found[kMost + kMost / 2 + kStep + 8], kept[kMost];
 };
+// Candidates that are put in order: the limit rises, and fewer logits are looked at again; but each time costs a microsecond or less of a wave.
+__device__ __forceinline__ int enough(int keep) { return keep + max(8, keep / 2); }
 __device__ __forceinline__ void in_order() {  // LDS accesses of a wave are in order; so are the compiler's
     __builtin_amdgcn_wave_barrier();
     asm volatile("" ::: "memory");
 }
+__device__ __forceinline__ int lanes_below(u64 lanes) {  // how many of them are before this one
+    return __builtin_amdgcn_mbcnt_hi((unsigned)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)lanes, 0));
+}
+// How many of n keys are above one; eight at a time, the places behind the last hold 0.
+__device__ __forceinline__ int above(const u64* keys, int n, u64 key) {
+    typedef u64 u64x2 __attribute__((ext_vector_type(2)));
+    int rank = 0;
+    for (int j = 0; j < n; j += 8) {
+        u64x2 x[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) x[y] = *(const u64x2*)(keys + j + 2 * y);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) rank += (x[y][0] > key) + (x[y][1] > key);
+    }
+    return rank;
+}
 __device__ __forceinline__ int keep_best(Best& b, int n, int keep, float& limit) {
     const int lane = threadIdx.x & 63;
+    if (lane < 8) b.found[n + lane] = 0;
     in_order();
-    if (n <= 64) {  // (a candidate per lane)
-        const u64 mine = lane < n ? b.found[lane] : 0;
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += b.found[j] > mine;
-        in_order();
-        if (lane < n && rank < keep) b.found[rank] = mine;
-    } else {
-        for (int i = lane; i < n; i += 64) {
-            const u64 mine = b.found[i];
-            int rank = 0;
-            for (int j = 0; j < n; ++j) rank += b.found[j] > mine;
-            if (rank < keep) b.kept[rank] = mine;
-        }
-        in_order();
-        if (lane < min(n, keep)) b.found[lane] = b.kept[lane];
+    for (int i = lane; i < n; i += 64) {
+        const u64 mine = b.found[i];
+        const int rank = above(b.found, n, mine);
+        if (rank < keep) b.kept[rank] = mine;
     }
     in_order();
     n = min(n, keep);
-    if (n == keep) limit = fmaxf(limit, value_of(b.found[n - 1]));
+    if (lane < n) b.found[lane] = b.kept[lane];
+    in_order();
+    if (n == keep) limit = fmaxf(limit, __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(value_of(b.found[n - 1])))));
     return n;
 }
 
-struct Shared {
+// The largest of a wave; the least of the largest of its groups of `group` lanes (a power of two).  Every lane gets the same, and the compiler knows.
+__device__ __forceinline__ float pair_up(float x, int by, bool largest) {
+    float y;
+    if (by == 1) y = dpp_move<0xB1>(x);
+    else if (by == 2) y = dpp_move<0x4E>(x);
+    else if (by == 4) y = dpp_move<0x141>(x);  // (the four lanes that are alike, mirrored)
+    else if (by == 8) y = dpp_move<0x140>(x);
+    else if (by == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        return largest ? fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])) : fminf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    } else {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        return largest ? fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])) : fminf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    return largest ? fmaxf(x, y) : fminf(x, y);
+}
+__device__ __forceinline__ float least_of_groups(float x, int group) {
+#pragma unroll
+    for (int by = 1; by < 64; by *= 2) x = pair_up(x, by, by < group);
+    return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
+}
+__device__ __forceinline__ float wave_max(float x) { return least_of_groups(x, 64); }
+
+struct __attribute__((aligned(16))) Shared {
     Best best[kWaves];
     int n[kWaves];
     float m[kWaves];
@@ -77,7 +110,7 @@ struct Shared {
 
 // The last one done has all rows' statistics and keys.  A candidate, larger is better: its score as an integer of the same order, then the lower beam and
 // token.
-struct Candidate {
+struct __attribute__((aligned(16))) Candidate {
     u64 score, place;
     __device__ __forceinline__ bool operator>(const Candidate& o) const { return score > o.score || (score == o.score && place > o.place); }
 };
@@ -87,8 +120,14 @@ __device__ __forceinline__ Candidate candidate_of(double score, int beam, int to
 }
 __device__ __forceinline__ double score_of(u64 bits) { return __builtin_bit_cast(double, bits ^ ((bits >> 63) ? 1ull << 63 : ~0ull)); }
 
+constexpr int kMostLists = 1024;  // slices of a request's rows
 struct Merge {
-    Candidate best[kWaves][kMost + 64];
+    union {
+        Candidate best[kWaves][kMost + 64];
+        Candidate all[kThreads];
+    };
+    double part[kMostLists];
+    float m[kMostLists];
     double log_sum[kMost], score[kMost];
     int ended[kMost], n[kWaves];
 };
@@ -113,11 +152,12 @@ struct Logits<u16> {
     static __device__ __forceinline__ float value(u16 x) { return bf2f(x); }
 };
 
-// `slices` workgroups per row, each with `length` logits of it.
+// `slices` workgroups per row, each with `length` logits of it, U pieces of 16 bytes per thread at a time.
 template <class T, int U>
 __global__ __launch_bounds__(kThreads) void select(const jup_beam_select_t a, int slices, int length, int* count, u64* scratch) {
     typedef Logits<T> L;
     constexpr int V = L::V;
+    typedef typename L::vec vec;
     __shared__ Lds lds;
     Shared& s = lds.s;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -127,113 +167,145 @@ __global__ __launch_bounds__(kThreads) void select(const jup_beam_select_t a, in
     u64* mine = scratch + ((long long)row * slices + slice) * kLeft;
     const float so_far = a.scores[row];
     const bool reads = fabsf(so_far) < INFINITY && !(a.ended && a.ended[row]);
-    // statistics of a thread: the sum of exp(x - m), m one of its first logits
+    // statistics: a lane's sum of exp(x - m); m is the wave's, within 1 of the largest so far
     float m = -INFINITY, limit = -INFINITY;
     double sum = 0.0;
     int n = 0;  // candidates of the wave
     if (reads) {
         const T* x = (const T*)a.logits + row * a.row_stride;
         const int end = min((slice + 1) * length, a.vocab);
-        for (int j0 = slice * length; j0 < end; j0 += kThreads * V * U) {
-            typename L::vec raw[U];
+        constexpr int kAll = kThreads * V * U;
+        auto load = [&](int j0, vec* raw) __attribute__((always_inline)) {
+            // (no lane has branches of its own: with them the loads in flight cannot be told apart, and each is waited for at once)
+            if (j0 + kAll <= end) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int j = j0 + (u * kThreads + tid) * V;
-                if (j + V <= end) {
-                    raw[u] = *(const typename L::vec*)(x + j);
-                } else {
+                for (int u = 0; u < U; ++u) raw[u] = *(const vec*)(x + j0 + (u * kThreads + tid) * V);
+            } else {
 #pragma unroll
-                    for (int e = 0; e < V; ++e) raw[u][e] = j + e < end ? x[j + e] : (T)(sizeof(T) == 2 ? 0xFF80 : -INFINITY);
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                float v[V], top = -INFINITY;
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    v[e] = L::value(raw[u][e]);
-                    v[e] = v[e] < INFINITY ? v[e] : -INFINITY;  // (NaN too)
-                    top = fmaxf(top, v[e]);
-                }
-                // (m need not be the largest: sums have room for 2^86 times as much, and lo keeps far exponentials exact)
-                const float m_new = top > m + 60.0f ? top : m;
-                if (m_new > -INFINITY) {
-                    float part = 0.f;
+                for (int u = 0; u < U; ++u) {
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
-                        // exp(d) = 2^(hi + lo), lo what the product hi loses
-                        const float d = v[e] - m_new, hi = d * kLog2e, lo = __builtin_fmaf(d, kLog2eRest, __builtin_fmaf(d, kLog2e, -hi));
-                        const float p = __builtin_amdgcn_exp2f(hi);
-                        part += d > -104.0f ? __builtin_fmaf(p * lo, 0.69314718f, p) : 0.f;
+                        const int j = j0 + (u * kThreads + tid) * V + e;
+                        const T value = x[min(j, end - 1)];
+                        raw[u][e] = j < end ? value : (T)(sizeof(T) == 2 ? 0xFF80 : -INFINITY);
                     }
-                    sum = m_new > m ? (m > -INFINITY ? sum * exp((double)m - (double)m_new) : 0.0) + part : sum + part;
-                    m = m_new;
+                }
+            }
+        };
+        vec raw[U], next[U];
+        load(slice * length, raw);
+        for (int j0 = slice * length; j0 < end; j0 += kAll) {
+            if (j0 + kAll < end) load(j0 + kAll, next);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float v[V], top;
+                auto look = [&](bool clean) __attribute__((always_inline)) {  // clean: NaN and +infinity become -infinity
+                    top = -INFINITY;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        v[e] = L::value(raw[u][e]);
+                        if (clean) v[e] = v[e] < INFINITY ? v[e] : -INFINITY;
+                        top = fmaxf(top, v[e]);
+                    }
+                };
+                auto add = [&]() __attribute__((always_inline)) {
+                    float part[2] = {0.f, 0.f};
+#pragma unroll
+                    for (int e = 0; e < V; ++e) part[e & 1] += __builtin_amdgcn_exp2f((v[e] - m) * kLog2e);
+                    return part[0] + part[1];
+                };
+                look(false);
+                bool cleaned = false;
+                if (__any(!(top <= m + 1.0f))) {  // the first time, and a few times more (or an infinity, or nothing but NaN)
+                    look(true);
+                    cleaned = true;
+                    const float most = wave_max(top);
+                    if (most > m + 1.0f) {
+                        if (m > -INFINITY) sum *= exp((double)m - (double)most);
+                        m = most;
+                    }
+                }
+                if (m > -INFINITY) {
+                    float part = add();
+                    if (__any(!(part < INFINITY))) {  // NaN among numbers
+                        look(true);
+                        cleaned = true;
+                        part = add();
+                    }
+                    sum += part;
                 }
                 const bool first = limit == -INFINITY;
                 if (first && n == 0) {
+                    if (!cleaned) look(true);
                     // Lanes in as many groups as are kept, or more: no group's best is below the least of the groups' bests, so that
                     // many logits are not.
-                    float t = top;
                     int group = 64;  // lanes of one
                     while (group > 1 && 64 / group < keep) group >>= 1;
-                    for (int x2 = 1; x2 < group; x2 <<= 1) t = fmaxf(t, __shfl_xor(t, x2, 64));
-                    for (int x2 = group; x2 < 64; x2 <<= 1) t = fminf(t, __shfl_xor(t, x2, 64));
-                    limit = t;
+                    limit = least_of_groups(top, group);
                 }
                 // (in the round that makes the limit what equals it counts)
                 if (!__any(first ? top >= limit && top > -INFINITY : top > limit)) continue;
+                const int j = j0 + (u * kThreads + tid) * V;
+                int mine_counts = 0, at = 0;
+                if (!first) {
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const bool counts = first ? v[e] >= limit && v[e] > -INFINITY : v[e] > limit;
-                    const u64 who = __ballot(counts);
-                    if (counts) s.best[wave].found[n + __builtin_amdgcn_mbcnt_hi((unsigned)(who >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)who, 0))] =
-                        key_of(v[e], j0 + (u * kThreads + tid) * V + e);
-                    n += __popcll(who);
+                    for (int e = V - 1; e >= 0; --e) {
+                        mine_counts += v[e] > limit;
+                        at = v[e] > limit ? e : at;
+                    }
                 }
-                if (n > 64) n = keep_best(s.best[wave], n, keep, limit);
+                if (!first && !__any(mine_counts > 1)) {  // mostly: one of a lane, its largest
+                    const u64 who = __ballot(mine_counts > 0);
+                    if (mine_counts) s.best[wave].found[n + lanes_below(who)] = key_of(top, j + at);
+                    n += __popcll(who);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const bool counts = first ? v[e] >= limit && v[e] > -INFINITY : v[e] > limit;
+                        const u64 who = __ballot(counts);
+                        if (counts) s.best[wave].found[n + lanes_below(who)] = key_of(v[e], j + e);
+                        n += __popcll(who);
+                    }
+                }
+                if (n > enough(keep)) n = keep_best(s.best[wave], n, keep, limit);
             }
+#pragma unroll
+            for (int u = 0; u < U; ++u) raw[u] = next[u];
         }
     }
-    n = keep_best(s.best[wave], n, keep, limit);
-    // the wave's statistics
-    float m_wave = m;
-#pragma unroll
-    for (int by = 32; by > 0; by >>= 1) m_wave = fmaxf(m_wave, __shfl_xor(m_wave, by, 64));
-    sum = m > -INFINITY ? sum * exp((double)m - (double)m_wave) : 0.0;
+    if (n > 64) n = keep_best(s.best[wave], n, keep, limit);
+    if (lane < 8) s.best[wave].found[n + lane] = 0;
 #pragma unroll
     for (int by = 32; by > 0; by >>= 1) sum += __shfl_xor(sum, by, 64);
     if (lane == 0) {
         s.n[wave] = n;
-        s.m[wave] = m_wave;
+        s.m[wave] = m;
         s.sum[wave] = sum;
     }
     __syncthreads();
     // the workgroup's: a thread has a key and counts those above it
-    const int k = tid / kWaves, of = tid % kWaves;
-    int all = 0;
-    float m_all = -INFINITY;
+    {
+        const u64 key = lane < n ? s.best[wave].found[lane] : 0;
+        int rank = 0, all = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        all += s.n[w];
-        m_all = fmaxf(m_all, s.m[w]);
+        for (int w = 0; w < kWaves; ++w) {
+            rank += above(s.best[w].found, s.n[w], key);
+            all += s.n[w];
+        }
+        if (key && rank < keep) leave(mine + 2 + rank, key);
+        if (tid >= all && tid < keep) leave(mine + 2 + tid, 0);
     }
-    if (k < s.n[of]) {
-        const u64 key = s.best[of].found[k];
-        int rank = k;
+    if (wave == 0) {
+        float m_all = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w)
-            if (w != of)
-                for (int j = 0; j < s.n[w] && s.best[w].found[j] > key; ++j) ++rank;
-        if (rank < keep) leave(mine + 2 + rank, key);
-    }
-    if (tid >= all && tid < keep) leave(mine + 2 + tid, 0);
-    if (tid == 0) {
-        double total = 0.0;
+        for (int w = 0; w < kWaves; ++w) m_all = fmaxf(m_all, s.m[w]);
+        double total = lane < kWaves && s.m[lane & (kWaves - 1)] > -INFINITY ? s.sum[lane] * exp((double)s.m[lane] - (double)m_all) : 0.0;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w)
-            if (s.m[w] > -INFINITY) total += s.sum[w] * exp((double)s.m[w] - (double)m_all);
-        leave(mine, __float_as_uint(m_all));
-        leave(mine + 1, __builtin_bit_cast(u64, total));
+        for (int by = kWaves / 2; by > 0; by >>= 1) total += __shfl_xor(total, by, 64);
+        if (lane == 0) {
+            leave(mine, __float_as_uint(m_all));
+            leave(mine + 1, __builtin_bit_cast(u64, total));
+        }
     }
     wait_stores_performed();
     __syncthreads();
@@ -246,85 +318,112 @@ __global__ __launch_bounds__(kThreads) void select(const jup_beam_select_t a, in
     if (!s.flag) return;
     __syncthreads();  // (the flag's place is the merge's)
 
+    // The last one done.  Its loads come from beyond L2, a microsecond away: as many as there are at once.
     Merge& g = lds.m;
-    const int row0 = request * a.n_beams;
+    const int row0 = request * a.n_beams, lists = a.n_beams * slices, candidates = lists * keep;
     const u64* from = scratch + (long long)row0 * slices * kLeft;
+    const bool few = candidates <= kThreads;  // a candidate per thread
+    u64 my_key = 0;
+    if (few && tid < candidates) my_key = left(from + (long long)(tid / keep) * kLeft + 2 + tid % keep);
+    for (int t = tid; t < lists; t += kThreads) {
+        const u64 m_bits = left(from + (long long)t * kLeft), sum_bits = left(from + (long long)t * kLeft + 1);
+        g.m[t] = __uint_as_float((unsigned)m_bits);
+        g.part[t] = __builtin_bit_cast(double, sum_bits);
+    }
     if (tid < a.n_beams) {
-        float top = -INFINITY;
-        for (int x = 0; x < slices; ++x) top = fmaxf(top, __uint_as_float((unsigned)left(from + (tid * slices + x) * kLeft)));
-        double total = 0.0;
-        for (int x = 0; x < slices; ++x) {
-            const u64* at = from + (tid * slices + x) * kLeft;
-            const float part = __uint_as_float((unsigned)left(at));
-            if (part > -INFINITY) total += __builtin_bit_cast(double, left(at + 1)) * exp((double)part - (double)top);
-        }
-        g.log_sum[tid] = (double)top + log(total);
         const float score = a.scores[row0 + tid];
         g.score[tid] = score;
         g.ended[tid] = !(fabsf(score) < INFINITY) ? -1 : a.ended && a.ended[row0 + tid] ? 1 : 0;  // -1: no candidates
     }
     __syncthreads();
-    // Lists (a slice of a beam's row each) are best first: a wave goes through its lists' first entries, then the second ones, and is done where
-    // none of a round is better than the last of what it keeps.
-    const int lists = a.n_beams * slices;
-    auto candidate = [&](int at, int k) -> Candidate {
+    // (a list's sum as a multiple of exp of its beam's largest m, then a beam's sum in the order of its slices)
+    auto most_of = [&](int beam) {
+        float top = -INFINITY;
+        for (int x = 0; x < slices; ++x) top = fmaxf(top, g.m[beam * slices + x]);
+        return top;
+    };
+    for (int t = tid; t < lists; t += kThreads)
+        g.part[t] = g.m[t] > -INFINITY ? g.part[t] * exp((double)g.m[t] - (double)most_of(t / slices)) : 0.0;
+    __syncthreads();
+    if (tid < a.n_beams) {
+        double total = 0.0;
+        for (int x = 0; x < slices; ++x) total += g.part[tid * slices + x];
+        g.log_sum[tid] = (double)most_of(tid) + log(total);
+    }
+    __syncthreads();
+    auto candidate = [&](int at, int k, u64 key) -> Candidate {  // entry k of list `at`
         const int beam = at / slices;
         if (g.ended[beam] != 0) return g.ended[beam] > 0 && at == beam * slices && k == 0 ? candidate_of(g.score[beam], beam, a.end_token) : Candidate{0, 0};
-        const u64 key = left(from + (long long)at * kLeft + 2 + k);
         return key ? candidate_of(g.score[beam] + ((double)value_of(key) - g.log_sum[beam]), beam, token_of(key)) : Candidate{0, 0};
     };
-    int held = 0;  // of this wave's list, best first
-    Candidate* list = g.best[wave];
-    for (int k0 = 0, more = 1; k0 < keep && more; ++k0) {
-        more = 0;
-        for (int at0 = wave * 64; at0 < lists; at0 += kThreads) {
-            const Candidate c = at0 + lane < lists ? candidate(at0 + lane, k0) : Candidate{0, 0};
-            const bool counts = c.score != 0 && (held < keep || c > list[keep - 1]);
-            const u64 who = __ballot(counts);
-            if (!who) continue;
-            more = 1;
-            if (counts) list[held + __builtin_amdgcn_mbcnt_hi((unsigned)(who >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)who, 0))] = c;
-            const int n_list = held + __popcll(who);
-            in_order();
-            // (up to 128: two per lane)
-            Candidate x[2];
-            int rank[2] = {0, 0};
+    Candidate best{0, 0};  // this thread's, and how many are better
+    int rank = 0, found = 0;
+    if (few) {
+        if (tid < candidates) best = candidate(tid / keep, tid % keep, my_key);
+        g.all[tid] = best;
+        __syncthreads();
+        for (int j = 0; j < candidates; j += 8) {  // (eight at a time; the places behind the last hold none)
+            Candidate o[8];
 #pragma unroll
-            for (int y = 0; y < 2; ++y) x[y] = lane + 64 * y < n_list ? list[lane + 64 * y] : Candidate{0, 0};
-            for (int j = 0; j < n_list; ++j) {
-                const Candidate o = list[j];
+            for (int y = 0; y < 8; ++y) o[y] = g.all[j + y];
 #pragma unroll
-                for (int y = 0; y < 2; ++y) rank[y] += o > x[y];
+            for (int y = 0; y < 8; ++y) {
+                rank += o[y] > best;
+                found += o[y].score != 0;
             }
-            in_order();
+        }
+    } else {
+        // Lists are best first: a wave goes through its lists' first entries, then the second ones, and is done where none of a round is better than
+        // the last of what it keeps.
+        int held = 0;  // of this wave's list, best first
+        Candidate* list = g.best[wave];
+        for (int k0 = 0, more = 1; k0 < keep && more; ++k0) {
+            more = 0;
+            for (int at0 = wave * 64; at0 < lists; at0 += kThreads) {
+                const int at = at0 + lane;
+                const Candidate c = at < lists ? candidate(at, k0, left(from + (long long)at * kLeft + 2 + k0)) : Candidate{0, 0};
+                const bool counts = c.score != 0 && (held < keep || c > list[keep - 1]);
+                const u64 who = __ballot(counts);
+                if (!who) continue;
+                more = 1;
+                if (counts) list[held + lanes_below(who)] = c;
+                const int n_list = held + __popcll(who);
+                in_order();
+                // (up to 128: two per lane)
+                Candidate x[2];
+                int r[2] = {0, 0};
 #pragma unroll
-            for (int y = 0; y < 2; ++y)
-                if (lane + 64 * y < n_list && rank[y] < keep) list[rank[y]] = x[y];
-            in_order();
-            held = min(n_list, keep);
+                for (int y = 0; y < 2; ++y) x[y] = lane + 64 * y < n_list ? list[lane + 64 * y] : Candidate{0, 0};
+                for (int j = 0; j < n_list; ++j) {
+                    const Candidate o = list[j];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) r[y] += o > x[y];
+                }
+                in_order();
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+                    if (lane + 64 * y < n_list && r[y] < keep) list[r[y]] = x[y];
+                in_order();
+                held = min(n_list, keep);
+            }
+        }
+        if (lane == 0) g.n[wave] = held;
+        __syncthreads();
+        if (lane < held) best = list[lane];
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            found += g.n[w];
+            for (int j = 0; j < g.n[w]; ++j) rank += g.best[w][j] > best;
         }
     }
-    if (lane == 0) g.n[wave] = held;
-    __syncthreads();
-    int found = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) found += g.n[w];
     const long long out0 = (long long)request * keep;
-    if (k < g.n[of]) {
-        const Candidate c = g.best[of][k];
-        int rank = k;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w)
-            if (w != of)
-                for (int j = 0; j < g.n[w] && g.best[w][j] > c; ++j) ++rank;
-        if (rank < keep) {
-            const u64 place = ~c.place;
-            const int beam = (int)(place >> 32), token = (int)(unsigned)place;
-            a.parents[out0 + rank] = row0 + beam;
-            a.tokens[out0 + rank] = token;
-            a.new_scores[out0 + rank] = (float)score_of(c.score);
-            if (a.new_ended) a.new_ended[out0 + rank] = g.ended[beam] > 0 || (a.end_token >= 0 && token == a.end_token);
-        }
+    if (best.score && rank < keep) {
+        const u64 place = ~best.place;
+        const int beam = (int)(place >> 32), token = (int)(unsigned)place;
+        a.parents[out0 + rank] = row0 + beam;
+        a.tokens[out0 + rank] = token;
+        a.new_scores[out0 + rank] = (float)score_of(best.score);
+        if (a.new_ended) a.new_ended[out0 + rank] = g.ended[beam] > 0 || (a.end_token >= 0 && token == a.end_token);
     }
     if (tid >= found && tid < keep) {
         a.parents[out0 + tid] = -1;
