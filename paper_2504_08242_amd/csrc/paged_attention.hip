@@ -301,8 +301,10 @@ __global__ __launch_bounds__(64) void attention_f32(const jup_paged_pool_t pool,
 }
 
 struct Kernels {
+    static constexpr int kTiles = kFewTiles;
     template <int QW, int NW> static auto few() { return attention_few<QW, NW>; }
     template <int QW, int NW> static constexpr int few_lds() { return Few<QW, NW>::kLds; }
+    template <int QW, int NW> static constexpr int few_pieces() { return NW == 8 ? kWidePieces : kFewPieces; }
     template <int KP, int NT, int SUB> static auto many() { return attention_many<JUP_BF16, 8, KP, NT, SUB, 2>; }
     template <int KP, int NT, int SUB> static constexpr int many_lds() { return Many<8, KP, NT, SUB, false>::kLds; }
 };

@@ -33,20 +33,25 @@ __device__ __forceinline__ bool clean_piece8(unsigned char* at, bool there) {
 
 // ---- few rows ----------------------------------------------------------------------------------------------------------------
 // As attention_few: a tile has QW = 16 or 32 rows, and the waves divide the piece's key tiles, each alone with its own places in LDS.  A tile is half
-// as long in bytes, so a wave has places for two, and as many bytes are in flight on a CU.
+// as long in bytes, so as many bytes are in flight on a CU with two places per wave, or with one and four workgroups on the CU.  That is what 16 rows
+// and four waves have: one workgroup's entry and merge then lie under three others' loads.  In µs, two places and one: 64 requests of one
+// token behind 16 to 8192, 32 heads on 8 73.7 / 70.4 (68.2 with twice as many pieces, 70.1 without a product), 16 of five behind 500 to 2100 41.3 /
+// 35.7; behind 4096 each 114 / 117 (4.7 TB/s).
 // LDS tiles, rows of 128 bytes in 8 chunks of 16:  K: chunk ch of row r at position ch ^ (r / 2 & 7);  V: at ch ^ turn(r), such that the rows of a
 // transposing read lie in different banks.  Behind them the scales of the tile's keys and values, 32 each.
 // K is read 16 codes at a time, two steps of the product: step (j, s) has the features 16 (chunk of j) + 8 s .. + 7, and queries are read so too.
 template <int QW, int NW>
 struct Few8 {
+    static constexpr int kPlaces = QW == 16 && NW == 4 ? 1 : 2;
+    static constexpr int kGroups = QW == 16 && NW == 4 ? 4 : 8 / NW;  // workgroups on a CU
     static constexpr int kScales = 2 * kTileBytes;             // of a place: K tile, V tile, scales
     static constexpr int kPlace = kScales + 256;
-    static constexpr int kWave = 2 * kPlace;
+    static constexpr int kWave = kPlaces * kPlace;
     static constexpr int kQ = NW * kWave;                      // the tile of rows: 256 bytes each, chunk ch at position ch ^ (r & 15)
     static constexpr int kStat = kQ + QW * 256;                // [2][waves][QW] maxima and sums
     static constexpr int kLds = kStat + 2 * NW * QW * 4;
     static_assert(NW * QW * 132 * 4 <= kStat, "merge regions overlap the statistics");
-    static_assert((8 / NW) * kLds <= 160 * 1024, "two workgroups of four waves share a CU");
+    static_assert(kGroups * kLds <= 160 * 1024, "workgroups that share a CU");
     // position of 16-byte chunk ch of V row r: ch ^ turn(r)
     static __device__ __forceinline__ int turn(int r) {
         return QW == 16 ? ((r >> 1) & 3) | ((r >> 4) & 1) << 2 : ((r >> 1) & 1) << 1 | ((r >> 3) & 1) << 2;
@@ -54,7 +59,7 @@ struct Few8 {
 };
 
 template <int CODE, int QW, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void attention_few8(const Attention8 args, int least) {
+__global__ __launch_bounds__(64 * NW, (Few8<QW, NW>::kGroups * NW / 4)) void attention_few8(const Attention8 args, int least) {
     typedef Few8<QW, NW> L;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63;
@@ -91,8 +96,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_few8(const Attention8 ar
     const float* my_scales = (lane < 32 ? a.k_scale : a.v_scale) + kv_head * a.scale_head;  // (a lane has a key's or a value's)
     const int lrow = lane >> 3, lp = lane & 7;
 
+    constexpr int P = L::kPlaces;
     // where tile number n (of this wave) lies: places take turns
-    auto place = [&](int n) __attribute__((always_inline)) { return lds0 + wave * L::kWave + (n & 1) * L::kPlace; };
+    auto place = [&](int n) __attribute__((always_inline)) { return lds0 + wave * L::kWave + (P == 1 ? 0 : (n & 1) * L::kPlace); };
     auto fill = [&](int tile, int n, const Blocks& b, bool v_part) __attribute__((always_inline)) {
         unsigned slot = place(n) + (v_part ? kTileBytes : 0);
         asm volatile("" : "+v"(slot));  // (see attention_few)
@@ -109,7 +115,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_few8(const Attention8 ar
             load_to_lds_16(base, lrow * row_bytes + (lp ^ (v_part ? L::turn(r) : (r >> 1) & 7)) * 16, dst + j * 1024);
         }
     };
-    // loads of a tile, in order: scales and K (5), V (4); two tiles are on their way
+    // loads of a tile, in order: scales and K (5), V (4); P tiles are on their way.  Block numbers: of this tile and the P behind it
     int tile = w.tile_lo + wave, n = 0;
     Blocks here{}, next{}, third{};
     if (tile < w.tile_hi) {
@@ -117,7 +123,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_few8(const Attention8 ar
         if (tile + NW < w.tile_hi) next = blocks_of(a, table_row, tile + NW, last_key);
         fill(tile, 0, here, false);
         fill(tile, 0, here, true);
-        if (tile + NW < w.tile_hi) {
+        if (P == 2 && tile + NW < w.tile_hi) {
             fill(tile + NW, 1, next, false);
             fill(tile + NW, 1, next, true);
             if (tile + 2 * NW < w.tile_hi) third = blocks_of(a, table_row, tile + 2 * NW, last_key);
@@ -161,7 +167,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_few8(const Attention8 ar
         const unsigned there = rows_there(a, here, tile, last_key);
         const unsigned my_place = place(n);
         const unsigned char* k_base = lds + (my_place - lds0);
-        if (more) asm volatile("s_waitcnt vmcnt(13)" ::: "memory");  // the scales and the K tile have landed
+        if (P == 2 && more) asm volatile("s_waitcnt vmcnt(13)" ::: "memory");  // the scales and the K tile have landed
         else asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
 
         // ---- S^T = K Q^T, and both kinds of scales ----
@@ -204,9 +210,10 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_few8(const Attention8 ar
                 vs[r] = vx[r >> 2][r & 3];
             }
         }
-        if (further) {
+        const bool refill = P == 1 ? more : further;
+        if (refill) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the K tile and the scales have been read
-            fill(tile + 2 * NW, n, third, false);
+            fill(tile + P * NW, n, P == 1 ? next : third, false);
         }
 
         // ---- online softmax (see attention_few) ----
@@ -248,8 +255,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_few8(const Attention8 ar
         }
 
         // ---- O^T += V^T P^T ----
-        if (further) asm volatile("s_waitcnt vmcnt(14)" ::: "memory");  // V has landed
-        else if (more) asm volatile("s_waitcnt vmcnt(9)" ::: "memory");
+        if (refill) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(P == 1 ? 5 : 14) : "memory");  // V has landed
+        else if (P == 2 && more) asm volatile("s_waitcnt vmcnt(9)" ::: "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         if (CODE == JUP_E4M3 && masked) {
             asm volatile("");
@@ -266,11 +273,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_few8(const Attention8 ar
             else oacc[f / 2] = mfma32(v, pf[f % 2], oacc[f / 2]);
         }
         here = next;
-        next = third;
-        if (further) {
+        if (P == 2) next = third;
+        if (refill) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the V tile has been read
-            fill(tile + 2 * NW, n, next, true);
-            if (tile + 3 * NW < w.tile_hi) third = blocks_of(a, table_row, tile + 3 * NW, last_key);
+            fill(tile + P * NW, n, P == 1 ? here : next, true);
+            if (tile + (P + 1) * NW < w.tile_hi) (P == 1 ? next : third) = blocks_of(a, table_row, tile + (P + 1) * NW, last_key);
         }
     }
 
@@ -296,10 +303,17 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_few8(const Attention8 ar
     merge_few<QW, NW, L::kStat>(w, kv_head, rows, c, hh, m_run, l_run, oacc, lds);
 }
 
+// Codes become bf16 values once per workgroup of attention_many and once per wave of attention_few8, but there the waves do not meet: tiles of 32 rows are
+// faster up to three rounds of them.  In µs, attention_few8 and attention_many, int8: 512 tokens behind 1536 on 32 heads 45 / 51 (e4m3 36 / 47), 768
+// behind 1536 66 / 84, prompts of 1024 33 / 37, of 2048 on 40 heads (2600 tiles) 113 / 98; 900 tokens on 16 heads on 2 103 / 103.
+constexpr int kFewTiles8 = 1536;
+
 template <int CODE>
 struct Kernels8 {
+    static constexpr int kTiles = kFewTiles8;
     template <int QW, int NW> static auto few() { return attention_few8<CODE, QW, NW>; }
     template <int QW, int NW> static constexpr int few_lds() { return Few8<QW, NW>::kLds; }
+    template <int QW, int NW> static constexpr int few_pieces() { return NW == 8 ? kWidePieces : 256 * Few8<QW, NW>::kGroups; }
     template <int KP, int NT, int SUB> static auto many() { return attention_many<CODE, 8, KP, NT, SUB, 2>; }
     template <int KP, int NT, int SUB> static constexpr int many_lds() { return Many<8, KP, NT, SUB, true>::kLds; }
 };

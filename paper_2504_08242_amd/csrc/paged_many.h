@@ -152,11 +152,8 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const ArgsOf<CODE
 #pragma unroll
             for (int g = 0; g < L::kGroups; ++g) {
                 const int group = NW * g + wave, r = 8 * (group & 3) + crow;
-                u32x4 codes = pending[g];
-                if (v_part) {
-                    const unsigned there = note_keys(i, g, ids, first_key + i * kStep + 8 * group);
-                    if (CODE == JUP_E4M3 && (i * SUB + group / (4 * L::kSubTiles) >= open || there != 0xFFu)) special |= clean_codes(codes, (there >> crow) & 1);
-                }
+                const u32x4 codes = pending[g];
+                if (v_part) note_keys(i, g, ids, first_key + i * kStep + 8 * group);
                 unsigned char* at = lds + (i & 1) * 2 * kHalf + (v_part ? kHalf : 0) + (group >> 2) * kValueTile + r * 256;
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
@@ -249,12 +246,9 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const ArgsOf<CODE
 
     for (int i = 0; i < n; ++i) {
         // step i is there for all, and step i - 1 has been read by all
-        if constexpr (kCodes) {
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        } else {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            clean(i);
-        }
+        if constexpr (kCodes) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if constexpr (CODE != JUP_I8) clean(i);  // (the codes of int8 are numbers, and their scales do not get here)
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         // Step i + 1 goes where step i - 1 was.  (Its loads are put between the products: the address path of a CU takes 64 bytes per

@@ -564,6 +564,7 @@ __device__ __forceinline__ void merge_few(const Work& w, int kv_head, int rows, 
 // In µs, attention_few and attention_many: 64 rows behind 1536 on 32 heads 16 / 20, 96 rows 17 / 20, 128 rows (of 128 tiles) 17 / 21, 192 rows 20 / 34;
 // 16 requests of 96 rows behind 500 to 2100 29 / 38; 900 tokens behind 3000 on 16 heads over 2 (452 tiles) 78 / 87; four requests of 100 (416
 // tiles) 34 / 32 (lost by the rule); 512 tokens behind 1536 (544 tiles) 33 / 33; 20 requests of 128 rows behind 300 to 1000 (2560 tiles) 81 / 74.
+// (Tiles of codes: paged_attention8.hip.)
 constexpr int kFewRows = 96;
 constexpr int kFewTiles = 512;
 constexpr int kShortRows = 32;
@@ -579,7 +580,8 @@ constexpr int kLeast = 20;
 // behind 2000 to 9000 86, 84 and 102 µs, five of 100 to 300 behind 10 to 20000 150, 122 and 130.
 constexpr int kManyPieces = 222;
 constexpr int kMostSplitHeads = 64;  // (more heads than that fill the chip without dividing keys)
-constexpr int kFewPlaces = 2 * (kFewPieces + kMostSplitHeads), kManyPlaces = 4 * (kManyPieces + kMostSplitHeads);
+constexpr int kMostFewPieces = 1024;  // of any kind of pool
+constexpr int kFewPlaces = 2 * (kMostFewPieces + kMostSplitHeads), kManyPlaces = 4 * (kManyPieces + kMostSplitHeads);
 constexpr size_t kPartialBytes = (size_t)(kFewPlaces * 32 > kManyPlaces * 256 ? kFewPlaces * 32 : kManyPlaces * 256) * kPartRow * 4;
 constexpr size_t kPlanBytes = ((size_t)JUP_PAGED_MAX_SEQS + 2) * 8;
 static_assert(kFewPlaces * 4 <= kCountBytes && kManyPlaces * 4 <= kCountBytes);
@@ -629,7 +631,8 @@ inline void set_call(Attention& a, const jup_paged_pool_t& pool, const jup_paged
     a.least_rows = 0; a.most_rows = INT32_MAX;
 }
 
-// K: the kernels of a kind of pool, few<QW, NW>() and many<KP, NT, SUB>(), and the LDS that they take; A: their arguments
+// K: the kernels of a kind of pool, few<QW, NW>() and many<KP, NT, SUB>(), the LDS that they take, pieces that fill the chip, and the most tiles of 32
+// rows per call that are for few(); A: their arguments
 template <class K, class A>
 hipError_t launch_tiles(A a, const jup_paged_attention_t& c, hipStream_t s) {
     const long long rows = (long long)c.n_rows * a.group.d, most = (long long)c.max_new * a.group.d;
@@ -637,12 +640,12 @@ hipError_t launch_tiles(A a, const jup_paged_attention_t& c, hipStream_t s) {
     auto few = [&](A x, long long tiles16, long long tiles32) {
         const long long tiles = most <= 16 ? tiles16 : tiles32;
         if (tiles * a.n_kv_heads <= 256)  // a workgroup per CU at most: of eight waves, and pieces for three CUs in four
-            return most <= 16 ? launch<16>(K::template few<16, 8>(), 512, K::template few_lds<16, 8>(), done16w, x, tiles, kWidePieces, kFewPlaces, kLeast, s)
-                              : launch<32>(K::template few<32, 8>(), 512, K::template few_lds<32, 8>(), done32w, x, tiles, kWidePieces, kFewPlaces, kLeast, s);
-        return most <= 16 ? launch<16>(K::template few<16, 4>(), 256, K::template few_lds<16, 4>(), done16, x, tiles, kFewPieces, kFewPlaces, kLeast, s)
-                          : launch<32>(K::template few<32, 4>(), 256, K::template few_lds<32, 4>(), done32, x, tiles, kFewPieces, kFewPlaces, kLeast, s);
+            return most <= 16 ? launch<16>(K::template few<16, 8>(), 512, K::template few_lds<16, 8>(), done16w, x, tiles, K::template few_pieces<16, 8>(), kFewPlaces, kLeast, s)
+                              : launch<32>(K::template few<32, 8>(), 512, K::template few_lds<32, 8>(), done32w, x, tiles, K::template few_pieces<32, 8>(), kFewPlaces, kLeast, s);
+        return most <= 16 ? launch<16>(K::template few<16, 4>(), 256, K::template few_lds<16, 4>(), done16, x, tiles, K::template few_pieces<16, 4>(), kFewPlaces, kLeast, s)
+                          : launch<32>(K::template few<32, 4>(), 256, K::template few_lds<32, 4>(), done32, x, tiles, K::template few_pieces<32, 4>(), kFewPlaces, kLeast, s);
     };
-    if (most <= kFewRows || (rows / 32 + c.n_seqs) * a.n_kv_heads <= kFewTiles) return few(a, rows / 16 + c.n_seqs, rows / 32 + c.n_seqs);
+    if (most <= kFewRows || (rows / 32 + c.n_seqs) * a.n_kv_heads <= K::kTiles) return few(a, rows / 16 + c.n_seqs, rows / 32 + c.n_seqs);
     // Up to 32 requests all go to attention_many, of more those of up to 32 rows to a launch of attention_few (an empty one costs 4 µs).  One
     // launch and two: 15 requests of one token behind 4000 and one of 512 61 and 65 µs, 32 of 1 to 300 behind 100 to 3000 171 and 180, 60 of one
     // behind 2000 and four of 300 142 and 160 (lost by the rule, which knows the number of requests alone); 63 of one behind 1000 and one of 512

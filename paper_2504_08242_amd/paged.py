@@ -231,14 +231,18 @@ def _pool(k_pool, v_pool, scales=None, layers=None):
         return (_pack_pool(k_pool.data_ptr(), v_pool.data_ptr(), strides[0], strides[1], strides[2], blocks, page, heads, dim, _DTYPES[dtype]),
                 None, dtype, at, heads, dim)
     k_scale, v_scale = scales
+    places = shape[:3]
     for x in scales:
-        if x.dtype is not _F32 or x.get_device() != at or x.shape != shape[:3]:
-            raise ValueError(f"scales must be two float32 tensors {list(shape[:3])} on cuda:{at}, not {x.dtype} {list(x.shape)} on {x.device}")
-    strides, (block, head, step) = _used(k_pool), _used(k_scale)
-    if _used(v_pool) != strides or (strides[3] != 1 and dim > 1):
-        raise ValueError("k_pool and v_pool must have the same strides, the last one 1")
-    if _used(v_scale) != (block, head, step) or (step != 1 and page > 1):
-        raise ValueError("the scales must have the same strides, the last one 1")
+        if x.dtype is not _F32 or x.get_device() != at or x.shape != places:
+            raise ValueError(f"scales must be two float32 tensors {list(places)} on cuda:{at}, not {x.dtype} {list(x.shape)} on {x.device}")
+    strides, (block, head, step) = k_pool.stride(), k_scale.stride()
+    if v_pool.stride() != strides or v_scale.stride() != (block, head, step) or strides[3] != 1 or step != 1 or blocks == 1 or heads == 1 or page == 1:
+        # (the stride of an axis of one entry is not used, and says nothing)
+        strides, (block, head, step) = _used(k_pool), _used(k_scale)
+        if _used(v_pool) != strides or (strides[3] != 1 and dim > 1):
+            raise ValueError("k_pool and v_pool must have the same strides, the last one 1")
+        if _used(v_scale) != (block, head, step) or (step != 1 and page > 1):
+            raise ValueError("the scales must have the same strides, the last one 1")
     return (_pack_pool(k_pool.data_ptr(), v_pool.data_ptr(), strides[0], strides[1], strides[2], blocks, page, heads, dim, _CODES[dtype]),
             _pack_scales(k_scale.data_ptr(), v_scale.data_ptr(), block, head, layers or 0), _BF16, at, heads, dim)
 
@@ -374,22 +378,24 @@ def read(slots, k_pool, v_pool, scales=None, k_out=None, v_out=None, stream=None
     pool.  scales: of a pool in 8 bits, whose rows come back as bfloat16."""
     pool, scale, dtype, at, heads, dim = _pool(k_pool, v_pool, scales)
     rows = slots.numel()
-    outs, places, strides = [], [], []
-    for name, out in (("k_out", k_out), ("v_out", v_out)):
-        if out is None:
-            out = _new(stream, at, lambda: torch.empty((rows, heads, dim), dtype=dtype, device=k_pool.device))
-            place, *stride = out.data_ptr(), heads * dim, dim
-        else:
-            place, *stride = _heads(name, out, dtype, at, rows, heads, dim, written=True)
-        outs.append(out)
-        places.append(place)
-        strides += stride
-    args = _pack_read(rows, *places, *strides, _ints("slots", slots, at, rows))
+    row = heads * dim
+    if k_out is None and v_out is None:
+        k_out, v_out = _new(stream, at, lambda: torch.empty((2, rows, heads, dim), dtype=dtype, device=k_pool.device)).unbind()
+        args = (k_out.data_ptr(), v_out.data_ptr(), row, dim, row, dim)
+    else:
+        if k_out is None:
+            k_out = _new(stream, at, lambda: torch.empty((rows, heads, dim), dtype=dtype, device=k_pool.device))
+        if v_out is None:
+            v_out = _new(stream, at, lambda: torch.empty((rows, heads, dim), dtype=dtype, device=k_pool.device))
+        k_at, *k_strides = _heads("k_out", k_out, dtype, at, rows, heads, dim, written=True)
+        v_at, *v_strides = _heads("v_out", v_out, dtype, at, rows, heads, dim, written=True)
+        args = (k_at, v_at, *k_strides, *v_strides)
+    args = _pack_read(rows, *args, _ints("slots", slots, at, rows))
     if scale is None:
         _call(_lib().jup_paged_read, at, stream, pool, args)
     else:
         _call(_lib().jup_paged_read8, at, stream, pool, scale, args)
-    return tuple(outs)
+    return k_out, v_out
 
 
 def attention(q, k_pool, v_pool, table, row_start, lengths, max_new, workspace=None, scale=None, out=None, scales=None, stream=None):
