@@ -254,7 +254,8 @@ JUP_API jup_status_t jup_verify_drafts(const jup_verify_drafts_t *args, void *st
  * The end of a step of a beam search.  Request i has n_beams beams, rows i * n_beams .. of logits and scores.  Its candidates are
  * (beam b, token j) with score  scores[b] + logits[b][j] - log sum_k exp(logits[b][k]),  of a beam that has ended (ended[b] not 0)
  * the one candidate (b, end_token) with scores[b].  The n_keep best of them come out, best first; equal scores: the lower beam, then the
- * lower token.  Scores are compared in 64 bits; exponentials are fp32 with their sums in 64: a score is off by about 2^-24.
+ * lower token.  Scores are compared in 64 bits (those alike to 2^-44 of them may count as equal); exponentials are fp32 with their sums in 64: a score
+ *  is off by about 2^-23.
  *   logits          [n_seqs * n_beams][vocab], rows row_stride apart; logits_dtype JUP_F32 or JUP_BF16.  One that is NaN or +infinity
  *                   counts as -infinity, and is no candidate
  *   scores          [n_seqs * n_beams]: sums of log probabilities.  A beam whose score is not finite has no candidates
@@ -289,7 +290,7 @@ JUP_API jup_status_t jup_beam_select(const jup_beam_select_t *args, void *stream
  *   table           [n_in][table_stride], table_width entries used; new_table [n_out][new_table_stride], new_table_width entries: those
  *                   behind a request's pages are set to -1.  They do not overlap
  *   lengths, owned  [n_in]; new_lengths, new_owned out [n_out]: the parent's length, the pages that it fills or begins
- *   free_blocks     [n_free], n_free <= 2^28: the stack has room for every block, so blocks are numbers below n_free;  free_count [1]
+ *   free_blocks     [n_free], n_free <= 2^26: the stack has room for every block, so blocks are numbers below n_free;  free_count [1]
  *   new_free_blocks out [n_free] (may be free_blocks: else all of it is copied);  new_free_count out [1] (may be free_count)
  *   held            [n_free] bytes, may be NULL: blocks that are not 0 there do not go back
  *   copy_from, copy_to  out [n_out]: the page to copy and its copy, or -1

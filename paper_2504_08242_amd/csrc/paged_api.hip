@@ -291,7 +291,7 @@ jup_status_t jup_paged_reorder(const jup_paged_reorder_t* a, void* stream) {
         return set_error(JUP_EINVAL, "%s: a table_width is negative, or table_width * page_size exceeds 2^31 - 256", me);
     if (a->table_stride < a->table_width || a->new_table_stride < a->new_table_width)
         return set_error(JUP_EINVAL, "%s: a table_stride is shorter than its table_width", me);
-    if (a->n_free < 0 || a->n_free > (1 << 28)) return set_error(JUP_EINVAL, "%s: n_free=%d is outside 0..2^28", me, a->n_free);
+    if (a->n_free < 0 || a->n_free > (1 << 26)) return set_error(JUP_EINVAL, "%s: n_free=%d is outside 0..2^26", me, a->n_free);
     if (const char* why = check_workspace(a->workspace, a->workspace_bytes); *why) return set_error(JUP_EINVAL, "%s: %s", me, why);
     if (!a->free_count || !a->new_free_count || !a->status)
         return set_error(JUP_EINVAL, "%s: free_count, new_free_count and status must not be NULL", me);

@@ -124,10 +124,10 @@ constexpr int kMostLists = 1024;  // slices of a request's rows
 struct Merge {
     union {
         Candidate best[kWaves][kMost + 64];
-        Candidate all[kThreads];
+        u64 all[kThreads];
     };
     double part[kMostLists];
-    float m[kMostLists];
+    float m[kMostLists], top[kMost];
     double log_sum[kMost], score[kMost];
     int ended[kMost], n[kWaves];
 };
@@ -337,18 +337,20 @@ __global__ __launch_bounds__(kThreads) void select(const jup_beam_select_t a, in
     }
     __syncthreads();
     // (a list's sum as a multiple of exp of its beam's largest m, then a beam's sum in the order of its slices)
-    auto most_of = [&](int beam) {
+    for (int t = tid; t < lists; t += kThreads) {
+        const int first = t / slices * slices;
         float top = -INFINITY;
-        for (int x = 0; x < slices; ++x) top = fmaxf(top, g.m[beam * slices + x]);
-        return top;
-    };
-    for (int t = tid; t < lists; t += kThreads)
-        g.part[t] = g.m[t] > -INFINITY ? g.part[t] * exp((double)g.m[t] - (double)most_of(t / slices)) : 0.0;
+#pragma unroll 4
+        for (int x = 0; x < slices; ++x) top = fmaxf(top, g.m[first + x]);
+        if (t == first) g.top[t / slices] = top;
+        g.part[t] = g.m[t] > -INFINITY ? g.part[t] * exp((double)g.m[t] - (double)top) : 0.0;
+    }
     __syncthreads();
     if (tid < a.n_beams) {
         double total = 0.0;
+#pragma unroll 4
         for (int x = 0; x < slices; ++x) total += g.part[tid * slices + x];
-        g.log_sum[tid] = (double)most_of(tid) + log(total);
+        g.log_sum[tid] = (double)g.top[tid] + log(total);
     }
     __syncthreads();
     auto candidate = [&](int at, int k, u64 key) -> Candidate {  // entry k of list `at`
@@ -360,18 +362,16 @@ __global__ __launch_bounds__(kThreads) void select(const jup_beam_select_t a, in
     int rank = 0, found = 0;
     if (few) {
         if (tid < candidates) best = candidate(tid / keep, tid % keep, my_key);
-        g.all[tid] = best;
+        // One number for each, in the order of the scores; those that are alike to 2^-44 of them are in the order of the lists, which is that of
+        // beams and tokens.
+        const u64 mine = best.score ? (best.score & ~255ull) | (unsigned)(255 - tid) : 0;
+        g.all[tid] = mine;
+        const u64 there = __ballot(mine != 0);
+        if (lane == 0) g.n[wave] = __popcll(there);
         __syncthreads();
-        for (int j = 0; j < candidates; j += 8) {  // (eight at a time; the places behind the last hold none)
-            Candidate o[8];
+        rank = above(g.all, candidates, mine);  // (the places behind the last hold 0)
 #pragma unroll
-            for (int y = 0; y < 8; ++y) o[y] = g.all[j + y];
-#pragma unroll
-            for (int y = 0; y < 8; ++y) {
-                rank += o[y] > best;
-                found += o[y].score != 0;
-            }
-        }
+        for (int w = 0; w < kWaves; ++w) found += g.n[w];
     } else {
         // Lists are best first: a wave goes through its lists' first entries, then the second ones, and is done where none of a round is better than
         // the last of what it keeps.

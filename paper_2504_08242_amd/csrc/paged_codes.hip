@@ -44,7 +44,7 @@ __global__ __launch_bounds__(256) void append_codes(const jup_paged_pool_t pool,
         if (h < heads) {
             const u16* from = (const u16*)a.q + row * a.q_row_stride + h * a.q_head_stride;
             u16* to = (u16*)a.q_out + row * a.q_out_row_stride + h * a.q_out_head_stride;
-            u32x4 lo = *(const u32x4*)(from + piece), hi = *(const u32x4*)(from + piece + 64);
+            u32x4 lo = __builtin_nontemporal_load((const u32x4*)(from + piece)), hi = __builtin_nontemporal_load((const u32x4*)(from + piece + 64));
             rotate8(lo, hi, cs + piece, lo, hi);
             *(u32x4*)(to + piece) = lo;
             *(u32x4*)(to + piece + 64) = hi;
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(256) void append_codes(const jup_paged_pool_t pool,
         if (!keys) h -= pool.n_kv_heads;
         const u16* from = keys ? (const u16*)a.k + row * a.k_row_stride + h * a.k_head_stride : (const u16*)a.v + row * a.v_row_stride + h * a.v_head_stride;
         u8* to = (u8*)(keys ? pool.k : pool.v) + place + h * pool.head_stride;
-        const u32x4 lo = *(const u32x4*)(from + piece), hi = *(const u32x4*)(from + piece + 64);
+        const u32x4 lo = __builtin_nontemporal_load((const u32x4*)(from + piece)), hi = __builtin_nontemporal_load((const u32x4*)(from + piece + 64));
         float x[8], y[8];
         if (keys && rotates) {
             rotate8(lo, hi, cs + piece, x, y);
@@ -104,8 +104,8 @@ __global__ __launch_bounds__(256) void read_codes(const jup_paged_pool_t pool, c
             out[e >> 1][(e & 1) * 2] = there ? pack_bf16x2(x[0] * scale, x[1] * scale) : 0u;
             out[e >> 1][(e & 1) * 2 + 1] = there ? pack_bf16x2(x[2] * scale, x[3] * scale) : 0u;
         }
-        *(u32x4*)(to + piece) = out[0];
-        *(u32x4*)(to + piece + 8) = out[1];
+        __builtin_nontemporal_store(out[0], (u32x4*)(to + piece));
+        __builtin_nontemporal_store(out[1], (u32x4*)(to + piece + 8));
     }
 }
 

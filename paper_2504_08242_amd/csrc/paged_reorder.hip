@@ -1,7 +1,8 @@
 // Tables of requests that go on from others, and copies of their pages (include/jupiter_paged.h).
 //
-// Three launches: who takes what (one workgroup, while others clear two bit maps of the blocks); table rows, the old tables' blocks marked in
-// one map and the new ones' in the other; blocks that are in the first alone go back on the stack, in the order of their numbers.
+// Who takes what is one workgroup's work; then table rows are written, with the blocks of the old tables marked in one map and those of the new ones in
+// another; then blocks that are in the first alone go back on the stack, in the order of their numbers.  Three launches, or one workgroup for it all
+// where there is little of it.
 #include "paged.h"
 
 namespace jup {
@@ -9,14 +10,10 @@ namespace {
 
 constexpr int kPart = 1024;
 
-// In the workspace, behind the arrival counters.
-struct Scratch {
-    int* first;               // [n_in]: the lowest request that goes on from it
-    unsigned *before, *after; // bit maps of the blocks
+// The workgroup's scratch; first: the lowest request that goes on from each, in the workspace.
+struct Plan {
+    int sums[kPart / 64], worst;
 };
-__host__ __device__ inline int words_of(int n_free) { return (n_free + 31) / 32; }
-
-__device__ __forceinline__ int owned_of(const jup_paged_reorder_t& a, int i) { return min(max(a.owned[i], 0), a.table_width); }
 
 // Sums of the threads before this one, and of all.
 __device__ int scan_part(int mine, int& all, int* lds) {
@@ -40,16 +37,12 @@ __device__ int scan_part(int mine, int& all, int* lds) {
     return before + run - mine;
 }
 
-__global__ __launch_bounds__(kPart) void reorder_plan(const jup_paged_reorder_t a, int shift, Scratch x) {
+// Lengths, pages and copies of the new requests, the status, and what is left of the stack (new_free_count).  One workgroup of kPart threads; what it
+// writes is there for all of them behind it.  Returns the status.
+__device__ int make_plan(const jup_paged_reorder_t& a, int shift, int* first, Plan& s) {
     const int tid = threadIdx.x;
-    if (blockIdx.x > 0) {
-        const int words = words_of(a.n_free);
-        for (int w = (blockIdx.x - 1) * kPart + tid; w < words; w += (gridDim.x - 1) * kPart) x.before[w] = x.after[w] = 0;
-        return;
-    }
-    __shared__ int lds[kPart / 64], worst;
-    if (tid == 0) worst = 5;
-    for (int i = tid; i < a.n_in; i += kPart) __hip_atomic_store(x.first + i, INT32_MAX, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (tid == 0) s.worst = 5;
+    for (int i = tid; i < a.n_in; i += kPart) __hip_atomic_store(first + i, INT32_MAX, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     wait_stores_performed();
     __syncthreads();
     const int F = *a.free_count, P = 1 << shift;
@@ -65,10 +58,10 @@ __global__ __launch_bounds__(kPart) void reorder_plan(const jup_paged_reorder_t 
         const int need = (int)(((long long)length + P - 1) >> shift);
         if (length < 0 || owned < 0 || owned > a.table_width || need > owned) why = 1;
         else if (need > a.new_table_width) why = min(why, 2);
-        atomicMin(x.first + p, i);
+        atomicMin(first + p, i);
     }
     wait_stores_performed();  // (atomics that return nothing count as stores)
-    if (why < 5) atomicMin(&worst, why);
+    if (why < 5) atomicMin(&s.worst, why);
     __syncthreads();
     // copies: of a page that is partly filled, for all but the first
     auto copied = [&](int i, int& p, int& length) {
@@ -79,23 +72,23 @@ __global__ __launch_bounds__(kPart) void reorder_plan(const jup_paged_reorder_t 
             return 0;
         }
         length = a.lengths[p];
-        return (length & (P - 1)) != 0 && __hip_atomic_load(x.first + p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != i ? 1 : 0;
+        return (length & (P - 1)) != 0 && __hip_atomic_load(first + p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != i ? 1 : 0;
     };
     int copies = 0;
     for (int part = 0; part < a.n_out; part += kPart) {
         int p, length, all;
         const int mine = copied(part + tid, p, length);
-        scan_part(mine, all, lds);
+        scan_part(mine, all, s.sums);
         copies += all;
     }
-    if (tid == 0 && worst == 5 && copies > F) worst = 4;
+    if (tid == 0 && s.worst == 5 && copies > F) s.worst = 4;
     __syncthreads();
-    const int status = worst == 5 ? 0 : worst;
+    const int status = s.worst == 5 ? 0 : s.worst;
     int done = 0;
     for (int part = 0; part < a.n_out; part += kPart) {
         const int i = part + tid;
         int p, length, all;
-        const int mine = copied(i, p, length), at = done + scan_part(mine, all, lds);
+        const int mine = copied(i, p, length), at = done + scan_part(mine, all, s.sums);
         done += all;
         if (i >= a.n_out) continue;
         const bool goes = status == 0 && p >= 0;
@@ -104,66 +97,133 @@ __global__ __launch_bounds__(kPart) void reorder_plan(const jup_paged_reorder_t 
         a.copy_from[i] = goes && mine ? a.table[(long long)p * a.table_stride + (length >> shift)] : -1;
         a.copy_to[i] = goes && mine ? a.free_blocks[F - 1 - at] : -1;
     }
+    wait_stores_performed();
     __syncthreads();  // (free_count may be new_free_count)
     if (tid == 0) {
         *a.status = status;
         *a.new_free_count = status == 0 ? F - copies : F;
     }
+    return status;
 }
 
-__device__ __forceinline__ void mark(unsigned* map, int block, int n_free) {
-    if ((unsigned)block < (unsigned)n_free) atomicOr(map + (block >> 5), 1u << (block & 31));
-}
-
-// A workgroup per old and per new table row, and some for the stack.
-__global__ __launch_bounds__(256) void reorder_rows(const jup_paged_reorder_t a, int shift, Scratch x) {
-    const int tid = threadIdx.x, status = *a.status;
-    int i = (int)blockIdx.x;
-    if (i < a.n_in) {
-        if (status != 0) return;
-        const int* row = a.table + (long long)i * a.table_stride;
-        const int n = owned_of(a, i);
-        for (int j = tid; j < n; j += 256) mark(x.before, row[j], a.n_free);
-        return;
+// Old request i's blocks, new request i's row: `threads` threads, each `mark`s blocks of the pool.
+template <class M>
+__device__ __forceinline__ void old_row(const jup_paged_reorder_t& a, int i, int tid, int threads, M mark) {
+    const int* row = a.table + (long long)i * a.table_stride;
+    const int n = min(max(a.owned[i], 0), a.table_width);
+    for (int j = tid; j < n; j += threads) {
+        const int block = row[j];
+        if ((unsigned)block < (unsigned)a.n_free) mark(block);
     }
-    i -= a.n_in;
-    if (i < a.n_out) {
-        int* to = a.new_table + (long long)i * a.new_table_stride;
-        const int n = a.new_owned[i];  // (0 where nothing goes on)
-        const int* row = a.table + (n > 0 ? (long long)a.parents[i] * a.table_stride : 0);
-        const int length = a.new_lengths[i], page = a.copy_from[i] >= 0 || a.copy_to[i] >= 0 ? length >> shift : -1, copy = a.copy_to[i];
-        for (int j = tid; j < a.new_table_width; j += 256) {
-            const int block = j >= n ? -1 : j == page ? copy : row[j];
-            to[j] = block;
-            mark(x.after, block, a.n_free);
-        }
-        return;
+}
+template <class M>
+__device__ __forceinline__ void new_row(const jup_paged_reorder_t& a, int shift, int i, int tid, int threads, M mark) {
+    int* to = a.new_table + (long long)i * a.new_table_stride;
+    const int n = a.new_owned[i];  // (0 where nothing goes on)
+    const int* row = a.table + (n > 0 ? (long long)a.parents[i] * a.table_stride : 0);
+    const int copy = a.copy_to[i], page = a.copy_from[i] >= 0 || copy >= 0 ? a.new_lengths[i] >> shift : -1;
+    for (int j = tid; j < a.new_table_width; j += threads) {
+        const int block = j >= n ? -1 : j == page ? copy : row[j];
+        to[j] = block;
+        if ((unsigned)block < (unsigned)a.n_free) mark(block);
     }
-    i -= a.n_out;
-    for (int j = i * 256 + tid; j < a.n_free; j += ((int)gridDim.x - a.n_in - a.n_out) * 256) a.new_free_blocks[j] = a.free_blocks[j];
 }
 
-__global__ __launch_bounds__(kPart) void reorder_release(const jup_paged_reorder_t a, Scratch x) {
-    __shared__ int lds[kPart / 64];
-    if (*a.status != 0) return;
-    const int words = words_of(a.n_free), F = *a.new_free_count;
-    int done = F;
+// Blocks that go back: gone(x) has a bit for each of the blocks 32 x .. 32 x + 31 that was in a table and is not any more.  One workgroup.
+template <class G>
+__device__ void release(const jup_paged_reorder_t& a, int left, int* sums, G gone_of) {
+    const int words = (a.n_free + 31) / 32;
+    int done = left;
     for (int part = 0; part < words; part += kPart) {
         const int w = part + (int)threadIdx.x;
-        unsigned gone = w < words ? x.before[w] & ~x.after[w] : 0u;
+        unsigned gone = w < words ? gone_of(w) : 0u;
         if (a.held)
-            for (unsigned left = gone; left; left &= left - 1) {
-                const int bit = __builtin_ctz(left);
+            for (unsigned bits = gone; bits; bits &= bits - 1) {
+                const int bit = __builtin_ctz(bits);
                 if (a.held[w * 32 + bit]) gone &= ~(1u << bit);
             }
         int all;
-        int at = done + scan_part(__popc(gone), all, lds);
+        int at = done + scan_part(__popc(gone), all, sums);
         done += all;
         for (; gone; gone &= gone - 1, ++at)
             if (at < a.n_free) a.new_free_blocks[at] = w * 32 + __builtin_ctz(gone);
     }
-    __syncthreads();  // (everybody has read the count)
     if (threadIdx.x == 0) *a.new_free_count = min(done, a.n_free);
+}
+
+// All of it.  Up to 2^15 blocks, whose maps are bits in LDS; a wave has a table row.
+constexpr int kSmallWords = 1024, kSmallEntries = 16384;
+__global__ __launch_bounds__(kPart) void reorder_small(const jup_paged_reorder_t a, int shift, int* first) {
+    __shared__ Plan s;
+    __shared__ unsigned before[kSmallWords], after[kSmallWords];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    before[tid] = after[tid] = 0;  // (behind the barriers of the plan)
+    if (a.new_free_blocks != a.free_blocks)
+        for (int i = tid; i < a.n_free; i += kPart) a.new_free_blocks[i] = a.free_blocks[i];
+    const int status = make_plan(a, shift, first, s);
+    if (status == 0)
+        for (int i = wave; i < a.n_in; i += kPart / 64) old_row(a, i, lane, 64, [&](int block) { atomicOr(before + (block >> 5), 1u << (block & 31)); });
+    for (int i = wave; i < a.n_out; i += kPart / 64) new_row(a, shift, i, lane, 64, [&](int block) { atomicOr(after + (block >> 5), 1u << (block & 31)); });
+    wait_stores_performed();  // (the stack's copy too: what goes back is written over it)
+    __syncthreads();
+    const int left = *a.new_free_count;
+    __syncthreads();
+    if (status == 0) release(a, left, s.sums, [&](int w) { return before[w] & ~after[w]; });
+}
+
+// Three launches: maps of a byte per block in the workspace, so that marking one needs no atomic.
+struct Maps {
+    int* first;
+    unsigned char *before, *after;
+};
+__host__ __device__ inline long long map_bytes(int n_free) { return ((long long)n_free + 31) / 32 * 32; }
+
+__global__ __launch_bounds__(kPart) void reorder_plan(const jup_paged_reorder_t a, int shift, Maps x) {
+    if (blockIdx.x > 0) {  // these clear the maps (one lies behind the other)
+        const long long pieces = 2 * map_bytes(a.n_free) / 16;
+        for (long long i = (long long)(blockIdx.x - 1) * kPart + threadIdx.x; i < pieces; i += (long long)(gridDim.x - 1) * kPart)
+            ((u32x4*)x.before)[i] = (u32x4){0, 0, 0, 0};
+        return;
+    }
+    __shared__ Plan s;
+    make_plan(a, shift, x.first, s);
+}
+
+// A workgroup per old and per new table row, and some for the stack.
+__global__ __launch_bounds__(128) void reorder_rows(const jup_paged_reorder_t a, int shift, Maps x) {
+    const int tid = threadIdx.x;
+    int i = (int)blockIdx.x;
+    if (i < a.n_in) {
+        if (*a.status == 0) old_row(a, i, tid, 128, [&](int block) { x.before[block] = 1; });
+        return;
+    }
+    i -= a.n_in;
+    if (i < a.n_out) {
+        new_row(a, shift, i, tid, 128, [&](int block) { x.after[block] = 1; });
+        return;
+    }
+    i -= a.n_out;
+    for (int j = i * 128 + tid; j < a.n_free; j += ((int)gridDim.x - a.n_in - a.n_out) * 128) a.new_free_blocks[j] = a.free_blocks[j];
+}
+
+__global__ __launch_bounds__(kPart) void reorder_release(const jup_paged_reorder_t a, Maps x) {
+    __shared__ int sums[kPart / 64];
+    if (*a.status != 0) return;
+    const int left = *a.new_free_count;
+    __syncthreads();  // (everybody has read it)
+    release(a, left, sums, [&](int w) {
+        unsigned gone = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {  // 16 bytes, each 0 or 1
+            const u32x4 b = *(const u32x4*)(x.before + w * 32ll + 16 * h), c = *(const u32x4*)(x.after + w * 32ll + 16 * h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const unsigned d = b[e] & ~c[e];  // bits 0, 8, 16 and 24
+                gone |= ((d * 0x10204080u) >> 28) << (16 * h + 4 * e);
+            }
+        }
+        return gone;
+    });
 }
 
 // A workgroup per (copy, layer, k or v, `heads` heads), pieces of T.
@@ -202,14 +262,21 @@ __global__ __launch_bounds__(256) void copy_pages(const jup_paged_pool_t pool, c
 }  // namespace
 
 hipError_t launch_paged_reorder(const jup_paged_reorder_t& a, hipStream_t s) {
-    const int shift = log2_of(a.page_size), words = words_of(a.n_free);
+    const int shift = log2_of(a.page_size);
     char* at = (char*)a.workspace + kCountBytes;
-    const Scratch x{(int*)at, (unsigned*)(at + JUP_PAGED_MAX_SEQS * 4), (unsigned*)(at + JUP_PAGED_MAX_SEQS * 4) + words};
-    const int clear = (words + kPart - 1) / kPart;
-    hipLaunchKernelGGL(reorder_plan, dim3(1 + (clear > 255 ? 255 : clear)), dim3(kPart), 0, s, a, shift, x);
+    int* first = (int*)at;
+    // One workgroup for it all: up to 16384 table entries and 2^15 blocks.
+    if ((long long)a.n_in * a.table_width + (long long)a.n_out * a.new_table_width <= kSmallEntries && a.n_free <= kSmallWords * 32) {
+        hipLaunchKernelGGL(reorder_small, dim3(1), dim3(kPart), 0, s, a, shift, first);
+        return hipGetLastError();
+    }
+    unsigned char* maps = (unsigned char*)at + JUP_PAGED_MAX_SEQS * 4;
+    const Maps x{first, maps, maps + map_bytes(a.n_free)};
+    const long long clear = (2 * map_bytes(a.n_free) / 16 + kPart - 1) / kPart;
+    hipLaunchKernelGGL(reorder_plan, dim3(1 + (unsigned)(clear > 1023 ? 1023 : clear)), dim3(kPart), 0, s, a, shift, x);
     const int stack = a.new_free_blocks == a.free_blocks ? 0 : (a.n_free + 1023) / 1024;
     const int rows = a.n_in + a.n_out + (stack > 1024 ? 1024 : stack);
-    if (rows > 0) hipLaunchKernelGGL(reorder_rows, dim3((unsigned)rows), dim3(256), 0, s, a, shift, x);
+    if (rows > 0) hipLaunchKernelGGL(reorder_rows, dim3((unsigned)rows), dim3(128), 0, s, a, shift, x);
     hipLaunchKernelGGL(reorder_release, dim3(1), dim3(kPart), 0, s, a, x);
     return hipGetLastError();
 }

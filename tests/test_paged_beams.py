@@ -56,7 +56,7 @@ def test_selection_refuses(change, word):
 @pytest.mark.parametrize("change,word", [
     (dict(n_in=-1), "n_in"), (dict(n_out=16385), "n_out"), (dict(page_size=20), "page_size"), (dict(page_size=4), "page_size"), (dict(table_width=-1), "table_width"),
     (dict(new_table_width=1 << 28, new_table_stride=1 << 28), "2^31"), (dict(table_stride=3), "table_stride"), (dict(new_table_stride=3), "table_stride"),
-    (dict(n_free=-1), "n_free"), (dict(n_free=(1 << 28) + 1), "n_free"), (dict(workspace=None), "workspace"), (dict(free_count=None), "free_count"),
+    (dict(n_free=-1), "n_free"), (dict(n_free=(1 << 26) + 1), "n_free"), (dict(workspace=None), "workspace"), (dict(free_count=None), "free_count"),
     (dict(status=None), "status"), (dict(new_free_blocks=None), "free_blocks"), (dict(owned=None), "owned"), (dict(table=None), "table"),
     (dict(parents=None), "parents"), (dict(new_table=None), "new_table"), (dict(copy_to=None), "copy_to"), (dict(new_table=FAKE), "must not be table")])
 def test_reordering_refuses(change, word):
