@@ -58,8 +58,8 @@ typedef struct {
  * slot at block * block_stride + head * head_stride + slot of scales->k or scales->v (fp32).  What jup_paged_append8() writes, of the
  * 128 values x_i of a head:
  *     m = max(2^-100, max_i |x_i|),  scale = m / T,  code_i = the one nearest to x_i * (T / m), ties to even
- * in fp32, with T = 127 (JUP_I8) or 448 (JUP_E4M3): a value is off by at most scale / 2, or (JUP_E4M3) 2^-4 of itself where that is
- * more than scale * 2^-10.  A head with an infinity or a NaN gets scale NaN and codes 0.
+ * in fp32, with T = 127 (JUP_I8) or 448 (JUP_E4M3): a value is off by at most scale / 2 (JUP_I8), or the larger of 2^-4 of itself and
+ * scale * 2^-10 (JUP_E4M3).  A head with an infinity or a NaN gets scale NaN and codes 0.
  * Such pools need head_dim 128, tensors that are 16-byte aligned, strides of codes that are multiples of 16 and strides of scales that
  * are multiples of 4; the rows that go with them (q, k, v and results) are JUP_BF16.
  */
@@ -157,8 +157,9 @@ typedef struct {
 JUP_API jup_status_t jup_paged_attention(const jup_paged_pool_t *pool, const jup_paged_attention_t *args, void *stream);
 
 /*
- * The same for pools in 8 bits.  Append: k is rotated in fp32 and quantised without another rounding.  Attention: the scale of a key
- * multiplies its score, that of a value its probability, and the product is what is rounded to bf16; codes are exact in bf16.  A score or a
+ * The same for pools in 8 bits.  Append: k is rotated in fp32 and quantised without another rounding; of two rows with the same slot the codes may
+ * be one's and the scale the other's.  Attention: the scale of a key multiplies its score, that of a value its probability, and the product is what is
+ * rounded to bf16 (where max_new * n_heads / n_kv_heads is at most 16, twice: what the first rounding loses too); codes are exact in bf16.  A score or a
  * value of a key that a row does not see does not reach it, whatever codes and scales hold; nor does a value whose probability is 0 in fp32.  JUP_I8 codes of -128 and JUP_E4M3 codes that are
  * no numbers, which jup_paged_append8() does not write, count as what they are.  Errors: JUP_EINVAL, JUP_EDEVICE.
  */

@@ -323,6 +323,9 @@ hipError_t launch_paged_attention(const jup_paged_pool_t& pool, const jup_paged_
 
 }  // namespace jup
 
+// what other calls take of a workspace: maps of 2^26 blocks (paged_reorder.hip), lists of 16384 slices of rows (paged_beams.hip)
+static_assert(jup::kPartialBytes >= JUP_PAGED_MAX_SEQS * 4ull + 2 * (1ull << 26) && jup::kPartialBytes >= JUP_PAGED_MAX_SEQS * (2ull + JUP_BEAM_MOST) * 8);
+
 extern "C" size_t jup_paged_workspace_bytes(void) {
     return jup::kCountBytes + (jup::kPlanBytes + jup::kPartialBytes > jup::kVerifyBytes ? jup::kPlanBytes + jup::kPartialBytes : jup::kVerifyBytes);
 }

@@ -2,7 +2,9 @@
 // paged_work.h.
 //
 // Codes are exact in bf16, so products are those of bf16 operands.  Scores are sums over a key's codes times the key's scale; a value's scale goes
-// with its probability, s_j p_j, which is rounded to bf16 as the operand of the second product: 2^-8 of it, as in a cache of bf16 values.
+// with its probability, s_j p_j, which is rounded to bf16 as the operand of the second product: 2^-8 of it, as in a cache of bf16 values.  Tiles
+// of 16 rows, which wait for memory, take what that rounding loses as a second operand (2^-16 is left): results are then as far from the
+// formula as their own rounding, 1.6e-3 in place of 2.3e-3 of the whole, and calls take 1 to 3 % longer (64 requests of one token 72.6 and 73.7 µs).
 #include "paged_many.h"
 
 namespace jup {
@@ -238,12 +240,17 @@ __global__ __launch_bounds__(64 * NW, (Few8<QW, NW>::kGroups * NW / 4)) void att
         const float alpha = grow ? __builtin_amdgcn_exp2f(m_run - m_safe) : 1.0f;
         const bool rescale = grow && m_run != -INFINITY;
         float ps = 0.f;
-        bf16x8 pf[NS / 8];
+        bf16x8 pf[NS / 8], rest;
 #pragma unroll
         for (int r = 0; r < NS; ++r) {
             const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[r], a.scale_log2e, -m_safe));
             ps += p;
-            pf[r >> 3][r & 7] = (__bf16)scaled(p, vs[r]);  // the operand of the second product: 2^-8 of each
+            const float x = scaled(p, vs[r]);
+            pf[r >> 3][r & 7] = (__bf16)x;  // the operand of the second product: 2^-8 of each
+            if constexpr (QW == 16) {  // and what that loses as another one (not of an infinity)
+                const float lost = x - (float)(__bf16)x;
+                rest[r & 7] = (__bf16)(fabsf(lost) < INFINITY ? lost : 0.f);
+            }
         }
         l_run = l_run * alpha + ps;
         m_run = m_new;
@@ -269,7 +276,7 @@ __global__ __launch_bounds__(64 * NW, (Few8<QW, NW>::kGroups * NW / 4)) void att
             // QW = 32: feature block f / 2, key half f % 2; QW = 16: feature block f, all 32 keys
             const u32x2 codes = read_tr8(my_place + (QW == 16 ? v_lane ^ (16 * f) : (v_lane ^ (32 * (f / 2))) + (f % 2) * 2048));
             const bf16x8 v = operand<CODE>(codes[0], codes[1]);
-            if constexpr (QW == 16) oacc[f] = mfma16(v, pf[0], oacc[f]);
+            if constexpr (QW == 16) oacc[f] = mfma16(v, rest, mfma16(v, pf[0], oacc[f]));
             else oacc[f / 2] = mfma32(v, pf[f % 2], oacc[f / 2]);
         }
         here = next;

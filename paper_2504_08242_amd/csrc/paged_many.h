@@ -148,7 +148,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const ArgsOf<CODE
             if (v_part) hole &= ~(1u << (i & 1));
             else if (lane < 16 * L::kGroups)
                 *(float*)(lds + L::kScales + (i & 1) * 2 * kStep * 4 + (lane & 8 ? kStep * 4 : 0) + (8 * NW * (lane >> 4) + 8 * wave + (lane & 7)) * 4) =
-                    lane & 8 ? pending_scale : pending_scale * a.scale_log2e;
+                    pending_scale;
 #pragma unroll
             for (int g = 0; g < L::kGroups; ++g) {
                 const int group = NW * g + wave, r = 8 * (group & 3) + crow;
@@ -300,7 +300,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const ArgsOf<CODE
         const unsigned char* scales = lds + L::kScales + (i & 1) * 2 * kStep * 4 + (first_tile * kKT + 4 * hh) * 4;  // (pools in 8 bits)
         if constexpr (kCodes) {
 #pragma unroll
-            for (int x = 0; x < 4 * NT; ++x) {  // keys 8 x + 4 hh .. + 3; K's scales have scale_log2e in them
+            for (int x = 0; x < 4 * NT; ++x) {  // keys 8 x + 4 hh .. + 3
                 const f32x4 ks = *(const f32x4*)(scales + x * 32);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sv[4 * x + e] = s[x >> 2][4 * (x & 3) + e] * ks[e];
@@ -323,7 +323,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const ArgsOf<CODE
         float mt = sv[0];
 #pragma unroll
         for (int r = 1; r < 16 * NT; ++r) mt = fmaxf(mt, sv[r]);
-        mt = max_across_halves(mt) * (kCodes ? 1.0f : a.scale_log2e);
+        mt = max_across_halves(mt) * a.scale_log2e;
         const bool grow = mt > m_run + 8.0f;
         const float m_new = grow ? mt : m_run;
         const float m_safe = m_new == -INFINITY ? 0.f : m_new;
@@ -342,7 +342,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const ArgsOf<CODE
                 const f32x4 vx = *(const f32x4*)(scales + kStep * 4 + y * 32);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float x = __builtin_amdgcn_exp2f(sv[4 * y + e] - m_safe);
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[4 * y + e], a.scale_log2e, -m_safe));
                     ps += x;
                     p[y >> 1][4 * (y & 1) + e] = (__bf16)scaled(x, vx[e]);
                 }

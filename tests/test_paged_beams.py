@@ -355,6 +355,18 @@ def test_many_requests_and_blocks(workspace):
 
 
 @gpu
+@pytest.mark.parametrize("rows,n_free", [(32, 32768), (33, 32768), (32, 32769)])
+def test_where_one_launch_ends_and_three_begin(workspace, rows, n_free):
+    rng = np.random.default_rng(rows)
+    lengths = rng.integers(0, 25, 32).tolist()
+    owned = [-(-x // 8) for x in lengths]
+    table = [[i * 3 + j if j < n else -1 for j in range(3)] for i, n in enumerate(owned)]
+    free = rng.permutation(np.arange(96, 32700))[:100].tolist() + [0] * (n_free - 100)
+    for in_place in (False, True):
+        check_reorder(workspace, rng.integers(0, 32, rows).tolist(), table, lengths, owned, free, 100, 8, in_place=in_place)
+
+
+@gpu
 def test_other_rows_of_a_wider_table(workspace):
     wide = torch.arange(60, dtype=torch.int32, device=DEV).view(4, 15)
     got = jp.reorder(ints([1, 1]), wide[:, 3:6], ints([33, 40, 1, 0]), ints([3, 3, 1, 0]), ints([50] * 70), ints([5]), 16, workspace)
