@@ -124,41 +124,49 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const ArgsOf<CODE
     // lanes 0 to 7 and 16 to 23 have one of a key in the first and second group, the eight behind each one of a value.
     u32x4 pending[L::kGroups];
     float pending_scale = 0.f;
-    const int crow = lane >> 3, cp = lane & 7;
+    // (What a lane makes of its number is made again each time: there are no registers to keep it in.)  V's chunks are the other way round, two by two,
+    // in odd rows: a lane's chunks then lie in other banks than its neighbour row's.
+    auto my_lane = [&]() __attribute__((always_inline)) {
+        int x = lane;
+        asm volatile("" : "+v"(x));
+        return x;
+    };
     bool special = false;  // values that are no numbers were taken out
     auto fetch = [&](int i, const Ids& ids, bool v_part) __attribute__((always_inline)) {
+        const int me = my_lane();
 #pragma unroll
         for (int g = 0; g < L::kGroups; ++g) {
             const int key = min(first_key + i * kStep + 8 * NW * g + 8 * wave, last_key & ~7);  // (groups behind the last key repeat its own)
             const char* base = group_base(a, v_part ? v_pool : k_pool, ids.id[g], key);
-            pending[g] = load_at<u32x4>(base, crow * (unsigned)a.slot + cp * 16);
+            pending[g] = load_at<u32x4>(base, (me >> 3) * (unsigned)a.slot + (me & 7) * 16);
         }
         if constexpr (kCodes) {
             if (!v_part) {
-                const int g = (lane >> 4) & 1, block = g == 0 ? ids.id[0] : ids.id[L::kGroups - 1];
+                const int g = (me >> 4) & 1, block = g == 0 ? ids.id[0] : ids.id[L::kGroups - 1];
                 const int key = min(first_key + i * kStep + 8 * NW * g + 8 * wave, last_key & ~7);
                 const long long at = (unsigned)block < (unsigned)a.n_blocks ? block : 0;
-                const float* scales = (lane & 8 ? a.v_scale : a.k_scale) + kv_head * a.scale_head;
-                pending_scale = scales[at * a.scale_block + (key & ((1 << a.shift) - 1)) + (lane & 7)];
+                const float* scales = (me & 8 ? a.v_scale : a.k_scale) + kv_head * a.scale_head;
+                pending_scale = scales[at * a.scale_block + (key & ((1 << a.shift) - 1)) + (me & 7)];
             }
         }
     };
     auto put = [&](int i, const Ids& ids, bool v_part) __attribute__((always_inline)) {
         if constexpr (kCodes) {
+            const int me = my_lane();
             if (v_part) hole &= ~(1u << (i & 1));
-            else if (lane < 16 * L::kGroups)
-                *(float*)(lds + L::kScales + (i & 1) * 2 * kStep * 4 + (lane & 8 ? kStep * 4 : 0) + (8 * NW * (lane >> 4) + 8 * wave + (lane & 7)) * 4) =
+            else if (me < 16 * L::kGroups)
+                *(float*)(lds + L::kScales + (i & 1) * 2 * kStep * 4 + (me & 8 ? kStep * 4 : 0) + (8 * NW * (me >> 4) + 8 * wave + (me & 7)) * 4) =
                     pending_scale;
 #pragma unroll
             for (int g = 0; g < L::kGroups; ++g) {
-                const int group = NW * g + wave, r = 8 * (group & 3) + crow;
+                const int group = NW * g + wave, r = 8 * (group & 3) + (me >> 3);
                 const u32x4 codes = pending[g];
                 if (v_part) note_keys(i, g, ids, first_key + i * kStep + 8 * group);
                 unsigned char* at = lds + (i & 1) * 2 * kHalf + (v_part ? kHalf : 0) + (group >> 2) * kValueTile + r * 256;
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    const int ch = 2 * cp + x;
-                    *(bf16x8*)(at + (v_part ? (((ch >> 2) ^ (r & 3)) << 2) | (ch & 3) : ch ^ (r & 15)) * 16) = operand<CODE>(codes[2 * x], codes[2 * x + 1]);
+                    const int ch = 2 * (me & 7) + x;
+                    *(bf16x8*)(at + (v_part ? (((ch >> 2) ^ (r & 3)) << 2) | ((ch & 3) ^ (r & 1)) : ch ^ (r & 15)) * 16) = operand<CODE>(codes[2 * x], codes[2 * x + 1]);
                 }
             }
         }
@@ -233,7 +241,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const ArgsOf<CODE
     unsigned v_lane[4];
 #pragma unroll
     for (int db = 0; db < 4; ++db)
-        v_lane[db] = lds0 + kHalf + vt_row * 256 + ((db ^ (vt_row & 3)) << 6) + (2 * (quad & 1) + ((sl & 3) >> 1)) * 16 + 8 * (sl & 1);
+        v_lane[db] = lds0 + kHalf + vt_row * 256 + ((db ^ (vt_row & 3)) << 6) + (2 * (quad & 1) + (((sl & 3) >> 1) ^ (kCodes ? vt_row & 1 : 0))) * 16 + 8 * (sl & 1);
     bf16x8 qf[8];
     // the queries have landed, the first step's loads may be in flight
     if (n > 0 && !kCodes) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * L::kGroups) : "memory");
