@@ -23,7 +23,9 @@ __device__ __forceinline__ void widen8(const u32x4 v, float* x) {
     for (int e = 0; e < 8; ++e) x[e] = bf2f((u16)(v[e / 2] >> (16 * (e & 1))));
 }
 
-// One workgroup per row, as append_bf16: 64 threads make the row's turns, then eight threads have a head of q, k or v each.
+// One workgroup per row, as append_bf16: 64 threads make the row's turns, then eight threads have a head of q, k or v each.  Bound by memory: 5940 rows
+// of 40 heads, 306 MB in and out, take 57 µs, 5.4 TB/s; with rows that are read through the caches, where nothing looks for them again, 71.  (A scale is
+// 4 bytes in a line of its own head: 10 MB more are written than there are.)  80 rows of 32 heads take 4.9 µs: slots, rows, stores behind one another.
 template <int CODE>
 __global__ __launch_bounds__(256) void append_codes(const jup_paged_pool_t pool, const jup_paged_scales_t scales, const jup_paged_append_t a, int shift,
                                                     const Turns turns) {
@@ -77,7 +79,8 @@ __global__ __launch_bounds__(256) void append_codes(const jup_paged_pool_t pool,
     }
 }
 
-// One workgroup per row.  Pools in 8 bits: eight threads have a head, 16 codes each.
+// One workgroup per row.  Pools in 8 bits: eight threads have a head, 16 codes each.  Bound by memory: 342 MB in and out take 77 µs, 4.4 TB/s; 82 with
+// results that stay in the caches, where they push out codes that are read yet.
 template <int CODE>
 __global__ __launch_bounds__(256) void read_codes(const jup_paged_pool_t pool, const jup_paged_scales_t scales, const jup_paged_read_t a, int shift) {
     const int row = (int)block_number();

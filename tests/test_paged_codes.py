@@ -526,6 +526,67 @@ def test_two_graphs_and_other_streams(workspace, kind):
     assert torch.equal(got, want[0])
 
 
+@gpu
+@kinds
+def test_blocks_beyond_32_bits(workspace, kind):
+    """Codes 2^31 bytes apart and scales 2^32: rows stored, read, attended over (few and many of them) and copied."""
+    far, heads, page, n_blocks = (1 << 31) + 4096, 2, 16, 4
+    memory = torch.empty(4 * far + (1 << 20), dtype=torch.uint8, device=DEV)
+    shape, strides = (n_blocks, heads, page, 128), (far, page * 128, 128, 1)
+    k_pool, v_pool = (memory.as_strided(shape, strides, at).view(KINDS[kind]) for at in (0, 1 << 16))
+    apart = tuple(memory.view(torch.float32).as_strided((2, heads, page), (far // 2, page, 1), at // 4) for at in (1 << 17, (1 << 17) + 4096))
+    scales = tuple(torch.zeros(shape[:3], device=DEV) for _ in range(2))
+    gen = torch.Generator().manual_seed(2)
+    rows = torch.randn((n_blocks * page, heads, 128), generator=gen).to(DEV, torch.bfloat16)
+    small = [torch.zeros(shape, dtype=torch.uint8, device=DEV).view(KINDS[kind]) for _ in range(2)]
+    near = [torch.zeros(shape[:3], device=DEV) for _ in range(2)]
+    slots = ints(range(n_blocks * page))
+    for pool, x in (((k_pool, v_pool), scales), (small, near)):
+        jp.append(rows, rows.flip(0), slots, *pool, scales=x)
+    assert torch.equal(k_pool.view(torch.uint8), small[0].view(torch.uint8)) and torch.equal(v_pool.view(torch.uint8), small[1].view(torch.uint8))
+    for a, b in zip(jp.read(slots, k_pool, v_pool, scales=scales), jp.read(slots, *small, scales=near)):
+        assert torch.equal(a, b)
+    table = ints([2, 0, 3, 1]).view(1, 4)
+    for new in (1, 33, 60):
+        q = torch.randn((new, 4, 128), generator=gen).to(DEV, torch.bfloat16)
+        call = lambda *pool, scales: jp.attention(q, *pool, table, ints([0, new]), ints([61]), new, workspace, scales=scales)  # noqa: E731
+        assert torch.equal(call(k_pool, v_pool, scales=scales), call(*small, scales=near))
+    # two blocks whose scales are as far apart
+    codes = [x[:2].contiguous() for x in (small[0].view(torch.uint8), small[1].view(torch.uint8))]
+    codes = [x.view(KINDS[kind]) for x in codes]
+    for mine, x in zip(apart, near):
+        mine.copy_(x[:2])
+    for a, b in zip(jp.read(slots[:32], *codes, scales=apart), jp.read(slots[:32], *small, scales=near)):
+        assert torch.equal(a, b)
+    for new in (1, 30):
+        q = torch.randn((new, 4, 128), generator=gen).to(DEV, torch.bfloat16)
+        call = lambda *pool, scales: jp.attention(q, *pool, ints([1, 0]).view(1, 2), ints([0, new]), ints([31]), new, workspace, scales=scales)  # noqa: E731
+        assert torch.equal(call(*codes, scales=apart), call(*small, scales=near))
+    jp.copy_pages(ints([0]), ints([3]), k_pool, v_pool, scales=scales)
+    assert torch.equal(k_pool.view(torch.uint8)[3], small[0].view(torch.uint8)[0]) and torch.equal(scales[1][3], near[1][0])
+
+
+@gpu
+@kinds
+def test_stores_on_another_stream(kind):
+    """Rows stored and read on a stream that is not the current one, twice at once."""
+    gen = torch.Generator().manual_seed(4)
+    k_pool, v_pool, scales = make_codes(kind, 40, 4, 16, "block-head-slot", gen)
+    rows = torch.randn((600, 4, 128), generator=gen).to(DEV, torch.bfloat16)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    halves = ints(range(300)), ints(range(300, 600))
+    for s, x, stream in zip(halves, (rows[:300], rows[300:]), (None, side)):
+        jp.append(x, x, s, k_pool, v_pool, scales=scales, stream=stream)
+    got = jp.read(halves[1], k_pool, v_pool, scales=scales, stream=side)
+    side.synchronize()
+    torch.cuda.synchronize()
+    codes, scale = cref.quantise(rows.float().cpu().numpy(), kind)
+    want = bf16_of(cref.numbers(codes, kind) * scale[..., None].astype(np.float64))
+    assert all(torch.equal(x.cpu(), want[300:]) for x in got)
+    assert all(torch.equal(x.cpu(), want) for x in jp.read(ints(range(600)), k_pool, v_pool, scales=scales))
+
+
 # ---- a stage over pages in 8 bits ------------------------------------------------------------------------------------------------------
 
 
