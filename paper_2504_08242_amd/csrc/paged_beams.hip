@@ -122,10 +122,16 @@ __device__ __forceinline__ Candidate candidate_of(double score, int beam, int to
 __device__ __forceinline__ double score_of(u64 bits) { return __builtin_bit_cast(double, bits ^ ((bits >> 63) ? 1ull << 63 : ~0ull)); }
 
 constexpr int kMostLists = 1024;  // slices of a request's rows
+constexpr int kEach = 4;          // candidates of a thread, where they are looked at all at once
 struct Merge {
     union {
         Candidate best[kWaves][kMost + 64];
-        u64 all[kThreads];
+        struct {
+            u64 all[kThreads];
+            Candidate chosen[kThreads];
+            int counts[kEach][kWaves];
+            float bound[kWaves];
+        };
     };
     double part[kMostLists];
     float m[kMostLists], top[kMost];
@@ -326,9 +332,15 @@ __global__ __launch_bounds__(kThreads) void select(const jup_beam_select_t a, in
     Merge& g = lds.m;
     const int row0 = request * a.n_beams, lists = a.n_beams * slices, candidates = lists * keep;
     const u64* from = scratch + (long long)row0 * slices * kLeft;
-    const bool few = candidates <= kThreads;  // a candidate per thread
-    u64 my_key = 0;
-    if (few && tid < candidates) my_key = left(from + (long long)(tid / keep) * kLeft + 2 + tid % keep);
+    bool few = candidates <= kThreads * kEach;
+    u64 my_keys[kEach];
+    if (few) {
+#pragma unroll
+        for (int y = 0; y < kEach; ++y) {
+            const int c = y * kThreads + tid;
+            my_keys[y] = c < candidates ? left(from + (long long)(c / keep) * kLeft + 2 + c % keep) : 0;
+        }
+    }
     for (int t = tid; t < lists; t += kThreads) {
         const u64 m_bits = left(from + (long long)t * kLeft), sum_bits = left(from + (long long)t * kLeft + 1);
         g.m[t] = __uint_as_float((unsigned)m_bits);
@@ -364,19 +376,73 @@ __global__ __launch_bounds__(kThreads) void select(const jup_beam_select_t a, in
     };
     Candidate best{0, 0};  // this thread's, and how many are better
     int rank = 0, found = 0;
-    if (few) {
-        if (tid < candidates) best = candidate(tid / keep, tid % keep, my_key);
-        // One number for each, in the order of the scores; those that are alike to 2^-44 of them are in the order of the lists, which is that of
-        // beams and tokens.
-        const u64 mine = best.score ? (best.score & ~255ull) | (unsigned)(255 - tid) : 0;
+    // One number for a candidate, in the order of the scores; those that are alike to 2^-44 of them are in the order of the lists, which is that of
+    // beams and tokens.
+    auto number = [](const Candidate& c, int place) { return c.score ? (c.score & ~255ull) | (unsigned)(255 - place) : 0ull; };
+    if (candidates <= kThreads) {  // one of a thread
+        if (tid < candidates) best = candidate(tid / keep, tid % keep, my_keys[0]);
+        const u64 mine = number(best, tid), there = __ballot(mine != 0);
         g.all[tid] = mine;
-        const u64 there = __ballot(mine != 0);
         if (lane == 0) g.n[wave] = __popcll(there);
         __syncthreads();
         rank = above(g.all, candidates, mine);  // (the places behind the last hold 0)
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) found += g.n[w];
-    } else {
+    } else if (few) {
+        // What may be among the best, n_keep at least: as of logits, none below the least of a wave's groups' bests is.
+        Candidate mine[kEach];
+        float value[kEach], top = -INFINITY;
+#pragma unroll
+        for (int y = 0; y < kEach; ++y) {
+            const int c = y * kThreads + tid;
+            mine[y] = c < candidates ? candidate(c / keep, c % keep, my_keys[y]) : Candidate{0, 0};
+            value[y] = mine[y].score ? (float)score_of(mine[y].score) : -INFINITY;
+            top = fmaxf(top, value[y]);
+        }
+        int group = 64;
+        while (group > 1 && 64 / group < keep) group >>= 1;
+        const float bound = least_of_groups(top, group);
+        if (lane == 0) g.bound[wave] = bound;
+        __syncthreads();
+        top = g.bound[0];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, g.bound[w]);
+        u64 who[kEach];
+#pragma unroll
+        for (int y = 0; y < kEach; ++y) {
+            who[y] = __ballot(mine[y].score != 0 && value[y] >= top);
+            if (lane == 0) g.counts[y][wave] = __popcll(who[y]);
+        }
+        __syncthreads();
+        int at[kEach];
+#pragma unroll
+        for (int y = 0; y < kEach; ++y)
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                if (w == wave) at[y] = found + lanes_below(who[y]);
+                found += g.counts[y][w];
+            }
+        few = found <= kThreads;  // (else as many are alike)
+        if (few) {
+            g.all[tid] = 0;
+            __syncthreads();
+#pragma unroll
+            for (int y = 0; y < kEach; ++y)
+                if ((who[y] >> lane) & 1) {
+                    g.all[at[y]] = number(mine[y], at[y]);
+                    g.chosen[at[y]] = mine[y];
+                }
+            __syncthreads();
+            if (tid < found) {
+                best = g.chosen[tid];
+                rank = above(g.all, found, g.all[tid]);
+            }
+        } else {
+            found = 0;
+            __syncthreads();
+        }
+    }
+    if (!few) {
         // Lists are best first: a wave goes through its lists' first entries, then the second ones, and is done where none of a round is better than
         // the last of what it keeps.
         int held = 0;  // of this wave's list, best first
@@ -442,9 +508,13 @@ __global__ __launch_bounds__(kThreads) void select(const jup_beam_select_t a, in
 hipError_t launch_beam_select(const jup_beam_select_t& a, hipStream_t s) {
     const long long rows = (long long)a.n_seqs * a.n_beams;
     auto go = [&](auto kernel, int block) {
-        // Slices of whole steps: as many as give the chip 1024 workgroups, of 4096 logits at least.  512 rows of 131072 with 512, 1024 and 2048
-        // workgroups: 59, 51 and 60 µs.
-        const long long most = rows >= 1024 ? 1 : 1024 / rows;
+        // Slices of whole steps, of 4096 logits at least: as many as give the chip 1024 workgroups (512 rows of 131072 with 512, 1024 and 2048
+        // workgroups: 59, 51 and 60 µs), 512 where more than eight are kept, as every wave begins with a list of that many (32 rows of 131072, 16 kept: 25
+        // and 33), and no more than the last workgroup can look at at once, where that is four at least (one request of eight beams and 131072 tokens 17 µs
+        // in place of 23, of 16 beams and 32000 21 in place of 28).
+        const long long wanted = a.n_keep > 8 ? 512 : 1024, fit = kThreads * kEach / (a.n_beams * a.n_keep);
+        long long most = rows >= wanted ? 1 : wanted / rows;
+        if (fit >= 4 && most > fit) most = fit;
         long long steps = ((a.vocab + block - 1) / block + most - 1) / most;
         const long long least = (4096 + block - 1) / block;
         if (steps < least) steps = least;
