@@ -125,8 +125,8 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const ArgsOf<CODE
     // lanes 0 to 7 and 16 to 23 have one of a key in the first and second group, the eight behind each one of a value.
     u32x4 pending[L::kGroups];
     float pending_scale = 0.f;
-    // (What a lane makes of its number is made again each time: there are no registers to keep it in.)  V's chunks are the other way round, two by two,
-    // in odd rows: a lane's chunks then lie in other banks than its neighbour row's.
+    // (What a lane makes of its number is made again each time: there are no registers to keep it in, and spilled ones cost 15 µs.  Two of eight lanes
+    // store to the same banks; without that, with 8 codes of either half of a row per lane, it takes as long, int8 2 % longer.)
     auto my_lane = [&]() __attribute__((always_inline)) {
         int x = lane;
         asm volatile("" : "+v"(x));
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const ArgsOf<CODE
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     const int ch = 2 * (me & 7) + x;
-                    *(bf16x8*)(at + (v_part ? (((ch >> 2) ^ (r & 3)) << 2) | ((ch & 3) ^ (r & 1)) : ch ^ (r & 15)) * 16) = operand<CODE>(codes[2 * x], codes[2 * x + 1]);
+                    *(bf16x8*)(at + (v_part ? (((ch >> 2) ^ (r & 3)) << 2) | (ch & 3) : ch ^ (r & 15)) * 16) = operand<CODE>(codes[2 * x], codes[2 * x + 1]);
                 }
             }
         }
@@ -242,7 +242,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const ArgsOf<CODE
     unsigned v_lane[4];
 #pragma unroll
     for (int db = 0; db < 4; ++db)
-        v_lane[db] = lds0 + kHalf + vt_row * 256 + ((db ^ (vt_row & 3)) << 6) + (2 * (quad & 1) + (((sl & 3) >> 1) ^ (kCodes ? vt_row & 1 : 0))) * 16 + 8 * (sl & 1);
+        v_lane[db] = lds0 + kHalf + vt_row * 256 + ((db ^ (vt_row & 3)) << 6) + (2 * (quad & 1) + ((sl & 3) >> 1)) * 16 + 8 * (sl & 1);
     bf16x8 qf[8];
     // the queries have landed, the first step's loads may be in flight
     if (n > 0 && !kCodes) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * L::kGroups) : "memory");
