@@ -7,8 +7,8 @@
  * the pages that hold its positions in order, and a call takes the rows of any number of requests, each with any number
  * of new tokens (a RAGGED batch): rows row_start[i] .. row_start[i+1]-1 belong to request i.  Requests (outline branches,
  * Jupiter paper Sec. V-B) that share a prefix name the same pages; only pages that the prefix fills may be shared, as a step's
- * tokens go into the last page of a request while that has room, and nothing copies a page (a branch that begins inside a page
- * needs a copy of it of its own).  A speculative step (Sec. V-A) is
+ * tokens go into the last page of a request while that has room, and jup_paged_extend() copies no page (a branch that begins inside
+ * a page needs a copy of it of its own: jup_paged_reorder() and jup_paged_copy()).  A speculative step (Sec. V-A) is
  *
  *     jup_paged_extend     lengths -> pages, positions, slots                       (once per step)
  *     jup_paged_append     rotary embedding, keys and values into their slots       (every layer; or, for a stage of
