@@ -160,8 +160,8 @@ JUP_API jup_status_t jup_paged_attention(const jup_paged_pool_t *pool, const jup
  * The same for pools in 8 bits.  Append: k is rotated in fp32 and quantised without another rounding; of two rows with the same slot the codes may
  * be one's and the scale the other's.  Attention: the scale of a key multiplies its score, that of a value its probability, and the product is what is
  * rounded to bf16 (where max_new * n_heads / n_kv_heads is at most 16, twice: what the first rounding loses too); codes are exact in bf16.  A score or a
- * value of a key that a row does not see does not reach it, whatever codes and scales hold; nor does a value whose probability is 0 in fp32.  JUP_I8 codes of -128 and JUP_E4M3 codes that are
- * no numbers, which jup_paged_append8() does not write, count as what they are.  Errors: JUP_EINVAL, JUP_EDEVICE.
+ * value of a key that a row does not see does not reach it, whatever codes and scales hold; nor does a value whose probability is 0 in fp32.  JUP_I8
+ * codes of -128 and JUP_E4M3 codes that are no numbers, which jup_paged_append8() does not write, count as what they are.  Errors: JUP_EINVAL, JUP_EDEVICE.
  */
 JUP_API jup_status_t jup_paged_append8(const jup_paged_pool_t *pool, const jup_paged_scales_t *scales, const jup_paged_append_t *args, void *stream);
 JUP_API jup_status_t jup_paged_attention8(const jup_paged_pool_t *pool, const jup_paged_scales_t *scales, const jup_paged_attention_t *args, void *stream);
@@ -255,8 +255,8 @@ JUP_API jup_status_t jup_verify_drafts(const jup_verify_drafts_t *args, void *st
  * The end of a step of a beam search.  Request i has n_beams beams, rows i * n_beams .. of logits and scores.  Its candidates are
  * (beam b, token j) with score  scores[b] + logits[b][j] - log sum_k exp(logits[b][k]),  of a beam that has ended (ended[b] not 0)
  * the one candidate (b, end_token) with scores[b].  The n_keep best of them come out, best first; equal scores: the lower beam, then the
- * lower token.  Scores are compared in 64 bits (those alike to 2^-44 of them may count as equal); exponentials are fp32 with their sums in 64: a score
- *  is off by about 2^-23.
+ * lower token.  Within a beam logits are compared, else scores in 64 bits, where of two that are alike to 2^-44 of themselves either may come first;
+ * exponentials are fp32 with their sums in 64: a score is off by about 2^-23.
  *   logits          [n_seqs * n_beams][vocab], rows row_stride apart; logits_dtype JUP_F32 or JUP_BF16.  One that is NaN or +infinity
  *                   counts as -infinity, and is no candidate
  *   scores          [n_seqs * n_beams]: sums of log probabilities.  A beam whose score is not finite has no candidates

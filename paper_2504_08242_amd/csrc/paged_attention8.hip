@@ -311,8 +311,8 @@ __global__ __launch_bounds__(64 * NW, (Few8<QW, NW>::kGroups * NW / 4)) void att
 }
 
 // Codes become bf16 values once per workgroup of attention_many and once per wave of attention_few8, but there the waves do not meet: tiles of 32 rows are
-// faster up to three rounds of them.  In µs, attention_few8 and attention_many, int8: 512 tokens behind 1536 on 32 heads 45 / 51 (e4m3 36 / 47), 768
-// behind 1536 66 / 84, prompts of 1024 33 / 37, of 2048 on 40 heads (2600 tiles) 113 / 98; 900 tokens on 16 heads on 2 103 / 103.
+// faster up to three rounds of them.  In µs, attention_few8 and attention_many, int8: 512 tokens behind 1536 on 32 heads 43 / 46 (e4m3 36 / 45), 768
+// behind 1536 66 / 81 (58 / 81), prompts of 1024 33 / 36, of 1200 on 40 heads (1520 tiles) 51 / 50, of 2048 (2600 tiles) 113 / 95.
 constexpr int kFewTiles8 = 1536;
 
 template <int CODE>

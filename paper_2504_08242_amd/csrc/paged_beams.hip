@@ -1,4 +1,4 @@
-// The end of a step of a beam search, and tables and pages of requests that go on from others (include/jupiter_paged.h).
+// The end of a step of a beam search (include/jupiter_paged.h).
 //
 // score(b, j) = scores[b] + x_bj - L_b with L_b = m_b + log sum_j exp(x_bj - m_b).  Within a row the order of the scores is that of
 // the logits, so one pass over a row leaves its n_keep largest logits and (m, sum); the workgroup of a request that is done last puts the rows'

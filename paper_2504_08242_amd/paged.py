@@ -294,7 +294,7 @@ def _call(fn, at, stream, *structs):
 
 
 class Workspace:
-    """Scratch of ``attention`` and ``verify`` calls that follow one another (calls that overlap need one each)."""
+    """Scratch of ``attention``, ``verify``, ``beam_select`` and ``reorder`` calls that follow one another (calls that overlap need one each)."""
 
     def __init__(self, device="cuda:0"):
         self.buf = torch.zeros(_lib().jup_paged_workspace_bytes(), dtype=torch.uint8, device=device)
