@@ -206,60 +206,62 @@ def _heads(name, t, dtype, at, rows, heads, dim, written=False):
     return t.data_ptr(), row, head
 
 
-def _used(t):
+def _used(strides, shape):
     """Strides, 0 for an axis of one entry: its own says nothing."""
-    return tuple(step if size > 1 else 0 for step, size in zip(t.stride(), t.shape))
+    return tuple(step if size > 1 else 0 for step, size in zip(strides, shape))
 
 
-def _pool(k_pool, v_pool, scales=None, layers=None):
-    """(struct, struct of the scales or None, dtype of rows, GPU number, heads, head size) of a pool.  layers: that of a stage's first layer,
-    with the scales' stride between layers."""
-    dtype, at, shape = k_pool.dtype, k_pool.get_device(), k_pool.shape
+def _pool(k_pool, v_pool, scales=None, layered=False):
+    """(struct, struct of the scales or None, dtype of rows, GPU number, heads, head size) of a pool; layered: of the first layer of tensors that
+    _layers() has looked at."""
+    dtype, at, shape, strides, v_strides = k_pool.dtype, k_pool.get_device(), k_pool.shape, k_pool.stride(), v_pool.stride()
+    if layered:
+        shape, strides, v_strides = shape[1:], strides[1:], v_strides[1:]
     if scales is None:
         if dtype not in _DTYPES or len(shape) != 4 or at < 0:
             raise ValueError("k_pool must be a float32 or bfloat16 tensor [n_blocks, n_kv_heads, page_size, head_dim] on the GPU (with scales an int8 "
                              "or float8_e4m3fn one)")
     elif dtype not in _CODES or len(shape) != 4 or at < 0:
         raise ValueError("k_pool must be an int8 or float8_e4m3fn tensor [n_blocks, n_kv_heads, page_size, head_dim] on the GPU, as there are scales")
-    if v_pool.dtype is not dtype or v_pool.shape != shape or v_pool.get_device() != at:
+    if v_pool.dtype is not dtype or v_pool.shape != k_pool.shape or v_pool.get_device() != at:
         raise ValueError("v_pool must have the type, shape and device of k_pool")
     blocks, heads, page, dim = shape
     if scales is None:
-        strides = k_pool.stride()
-        if v_pool.stride() != strides or strides[3] != 1:
+        if v_strides != strides or strides[3] != 1:
             raise ValueError("k_pool and v_pool must have the same strides, the last one 1")
         return (_pack_pool(k_pool.data_ptr(), v_pool.data_ptr(), strides[0], strides[1], strides[2], blocks, page, heads, dim, _DTYPES[dtype]),
                 None, dtype, at, heads, dim)
     k_scale, v_scale = scales
-    places = shape[:3]
+    places = k_pool.shape[:-1]
     for x in scales:
         if x.dtype is not _F32 or x.get_device() != at or x.shape != places:
             raise ValueError(f"scales must be two float32 tensors {list(places)} on cuda:{at}, not {x.dtype} {list(x.shape)} on {x.device}")
-    strides, (block, head, step) = k_pool.stride(), k_scale.stride()
-    if v_pool.stride() != strides or v_scale.stride() != (block, head, step) or strides[3] != 1 or step != 1 or blocks == 1 or heads == 1 or page == 1:
+    k_steps, v_steps, layer = k_scale.stride(), v_scale.stride(), 0
+    if layered:
+        layer, k_steps, v_steps = k_steps[0], k_steps[1:], v_steps[1:]
+    if v_strides != strides or v_steps != k_steps or strides[3] != 1 or k_steps[2] != 1 or blocks == 1 or heads == 1 or page == 1:
         # (the stride of an axis of one entry is not used, and says nothing)
-        strides, (block, head, step) = _used(k_pool), _used(k_scale)
-        if _used(v_pool) != strides or (strides[3] != 1 and dim > 1):
+        strides, k_steps = _used(strides, shape), _used(k_steps, shape)
+        if _used(v_strides, shape) != strides or (strides[3] != 1 and dim > 1):
             raise ValueError("k_pool and v_pool must have the same strides, the last one 1")
-        if _used(v_scale) != (block, head, step) or (step != 1 and page > 1):
+        if _used(v_steps, shape) != k_steps or (k_steps[2] != 1 and page > 1):
             raise ValueError("the scales must have the same strides, the last one 1")
     return (_pack_pool(k_pool.data_ptr(), v_pool.data_ptr(), strides[0], strides[1], strides[2], blocks, page, heads, dim, _CODES[dtype]),
-            _pack_scales(k_scale.data_ptr(), v_scale.data_ptr(), block, head, layers or 0), _BF16, at, heads, dim)
+            _pack_scales(k_scale.data_ptr(), v_scale.data_ptr(), k_steps[0], k_steps[1], layer), _BF16, at, heads, dim)
 
 
 def _layers(k_pools, v_pools, scales):
-    """(pool of the first layer, its scales, strides between layers of the pool and of the scales) of tensors with an axis of layers."""
+    """Stride between the layers of tensors with an axis of layers in front."""
     if k_pools.dim() != 5 or v_pools.shape != k_pools.shape or (k_pools.shape[0] > 1 and v_pools.stride(0) != k_pools.stride(0)):
         raise ValueError("k_pools and v_pools must be tensors [n_layers, n_blocks, n_heads, page_size, head_dim] of the same strides")
     if k_pools.shape[0] == 0:
         raise ValueError("there are no layers")
-    if scales is None:
-        return (k_pools[0], v_pools[0]), None, k_pools.stride(0), 0
-    k_scale, v_scale = scales
-    if k_scale.dim() != 4 or k_scale.shape != k_pools.shape[:4] or v_scale.shape != k_scale.shape or (
-            k_scale.shape[0] > 1 and v_scale.stride(0) != k_scale.stride(0)):
-        raise ValueError(f"scales must be two float32 tensors {list(k_pools.shape[:4])} of the same strides")
-    return (k_pools[0], v_pools[0]), (k_scale[0], v_scale[0]), k_pools.stride(0), k_scale.stride(0)
+    if scales is not None:
+        k_scale, v_scale = scales
+        if k_scale.dim() != 4 or k_scale.shape != k_pools.shape[:4] or v_scale.shape != k_scale.shape or (
+                k_scale.shape[0] > 1 and v_scale.stride(0) != k_scale.stride(0)):
+            raise ValueError(f"scales must be two float32 tensors {list(k_pools.shape[:4])} of the same strides")
+    return k_pools.stride(0)
 
 
 _current_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice  # (the tensors are on the GPU: it is initialised)
@@ -380,7 +382,7 @@ def read(slots, k_pool, v_pool, scales=None, k_out=None, v_out=None, stream=None
     rows = slots.numel()
     row = heads * dim
     if k_out is None and v_out is None:
-        k_out, v_out = _new(stream, at, lambda: torch.empty((2, rows, heads, dim), dtype=dtype, device=k_pool.device)).unbind()
+        k_out, v_out = _new(stream, at, lambda: k_pool.new_empty((2, rows, heads, dim), dtype=dtype)).unbind()
         args = (k_out.data_ptr(), v_out.data_ptr(), row, dim, row, dim)
     else:
         if k_out is None:
@@ -435,8 +437,8 @@ def prefill(stage, hidden_in, step, k_pools, v_pools, table, max_new, workspace=
         raise ValueError(f"k_pools and v_pools must be tensors [{stage.cfg['n_layers']}, n_blocks, n_heads, page_size, head_dim] of the same strides")
     if k_pools.shape[0] == 0:
         raise ValueError("a stage without layers has no pools")
-    first, first_scales, layer_stride, scale_stride = _layers(k_pools, v_pools, scales)
-    packed, code_scales, dtype, at, _, _ = _pool(*first, first_scales, scale_stride)
+    layer_stride = _layers(k_pools, v_pools, scales)
+    packed, code_scales, dtype, at, _, _ = _pool(k_pools, v_pools, scales, True)
     n, rows, width = step.lengths.numel(), hidden_in.shape[0], stage.cfg["d_model"]
     for name, t in (("hidden_in", hidden_in), ("hidden_out", hidden_in if hidden_out is None else hidden_out)):
         if t.dtype is not dtype or t.get_device() != at or t.shape != (rows, width) or not t.is_contiguous():
@@ -571,12 +573,9 @@ def reorder(parents, table, lengths, owned, free_blocks, free_count, page_size, 
 def copy_pages(copy_from, copy_to, k_pools, v_pools, lengths=None, scales=None, stream=None):
     """Pages copy_from[i] to copy_to[i] of every layer (jup_paged_copy), whole ones, or with lengths the first lengths[i] mod page_size slots.
     k_pools, v_pools, scales: of one layer, or with an axis of layers in front."""
-    if k_pools.dim() == 5:
-        first, first_scales, layer_stride, scale_stride = _layers(k_pools, v_pools, scales)
-        layers = k_pools.shape[0]
-    else:
-        first, first_scales, layer_stride, scale_stride, layers = (k_pools, v_pools), scales, 0, 0, 1
-    pool, code_scales, _, at, _, _ = _pool(*first, first_scales, scale_stride)
+    layered = k_pools.dim() == 5
+    layers, layer_stride = (k_pools.shape[0], _layers(k_pools, v_pools, scales)) if layered else (1, 0)
+    pool, code_scales, _, at, _, _ = _pool(k_pools, v_pools, scales, layered)
     n = copy_from.numel()
     _call(_lib().jup_paged_copy, at, stream, pool, code_scales,
           _pack_copy(n, layers, layer_stride, _ints("copy_from", copy_from, at, n), _ints("copy_to", copy_to, at, n),
