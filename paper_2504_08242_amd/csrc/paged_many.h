@@ -120,9 +120,11 @@ __global__ __launch_bounds__(64 * NW, OCC) void attention_many(const ArgsOf<CODE
         }
     };
     // Codes are fetched into registers, half a step ahead of their use, and go into LDS as the bf16 values that they are: once for all waves, where
-    // a conversion behind LDS would be made by every wave that reads them.  (Four prompts of 700 to 4100 tokens, e4m3, take 336 µs, bf16 values 292.  What
-    // comes on top, measured one at a time at 371 µs, when some registers were still spilled: conversions and stores to LDS 46, scales 33, loads 28.)  A lane has 16 codes of a row of each of its wave's groups; of the scales
-    // lanes 0 to 7 and 16 to 23 have one of a key in the first and second group, the eight behind each one of a value.
+    // a conversion behind LDS would be made by every wave that reads them.  (Four prompts of 700 to 4100 tokens, e4m3, take 338 µs, bf16 values 292.  What
+    // comes on top, measured one at a time at 371 µs, when some registers were still spilled: conversions and stores to LDS 46, scales 33, loads 28.
+    // Values put behind the products take 349, both kinds fetched a whole step ahead 354, and there int8 runs out of registers.)
+    // A lane has 16 codes of a row of each of its wave's groups; of the scales lanes 0 to 7 and 16 to 23 have one of a key in the first and second
+    // group, the eight behind each one of a value.
     u32x4 pending[L::kGroups];
     float pending_scale = 0.f;
     // (What a lane makes of its number is made again each time: there are no registers to keep it in, and spilled ones cost 15 µs.  Two of eight lanes
