@@ -162,7 +162,7 @@ struct Logits<u16> {
 // `slices` workgroups per row, each with `length` logits of it, U pieces of 16 bytes per thread at a time (the next ones are on their way meanwhile; with
 // two in place of four 64 rows of 32000 in bf16 take 17 µs in place of 14, 512 of 131072 48 in place of 47).
 // Four rows of 32000 fp32 logits take 12 µs: 8 up to the arrival, 4 for the last workgroup, trips to memory most of it (with slices of 2048 logits
-// 14, as twice as many lists are put together).  512 rows of 131072 in bf16, of which a fifth are not read, 107 MB, take 46: reading alone takes 28 (3.8
+// 14, as twice as many lists are put together).  512 rows of 131072 in bf16, of which a fifth are not read, 107 MB, take 45: reading alone takes 28 (3.8
 // TB/s, as workgroups of rows that are not read leave holes), exponentials 5 of the others and candidates 10 (without either, less than the sum).
 template <class T, int U>
 __global__ __launch_bounds__(kThreads) void select(const jup_beam_select_t a, int slices, int length, int* count, u64* scratch) {

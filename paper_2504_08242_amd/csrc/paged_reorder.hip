@@ -10,9 +10,11 @@ namespace {
 
 constexpr int kPart = 1024;
 
-// The workgroup's scratch; first: the lowest request that goes on from each, in the workspace.
+// The workgroup's scratch.  first: the lowest request that goes on from each, in the workspace where there are more of them (the plan of 512 beams took
+// 6.0 µs with it there, and what a thread knows of its request read again; 5.0 so).
+constexpr int kNear = 2048;
 struct Plan {
-    int sums[kPart / 64], worst;
+    int sums[kPart / 64], worst, first[kNear];
 };
 
 // Sums of the threads before this one, and of all.
@@ -41,12 +43,17 @@ __device__ int scan_part(int mine, int& all, int* lds) {
 // writes is there for all of them behind it.  Returns the status.
 __device__ int make_plan(const jup_paged_reorder_t& a, int shift, int* first, Plan& s) {
     const int tid = threadIdx.x;
+    const bool near = a.n_in <= kNear;
     if (tid == 0) s.worst = 5;
-    for (int i = tid; i < a.n_in; i += kPart) __hip_atomic_store(first + i, INT32_MAX, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (near)
+        for (int i = tid; i < a.n_in; i += kPart) s.first[i] = INT32_MAX;
+    else
+        for (int i = tid; i < a.n_in; i += kPart) __hip_atomic_store(first + i, INT32_MAX, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     wait_stores_performed();
     __syncthreads();
     const int F = *a.free_count, P = 1 << shift;
     int why = F < 0 || F > a.n_free ? 1 : 5;
+    int my_parent = -1, my_length = 0;  // of request tid
     for (int i = tid; i < a.n_out; i += kPart) {
         const int p = a.parents[i];
         if (p == -1) continue;
@@ -58,21 +65,27 @@ __device__ int make_plan(const jup_paged_reorder_t& a, int shift, int* first, Pl
         const int need = (int)(((long long)length + P - 1) >> shift);
         if (length < 0 || owned < 0 || owned > a.table_width || need > owned) why = 1;
         else if (need > a.new_table_width) why = min(why, 2);
-        atomicMin(first + p, i);
+        if (near) atomicMin(s.first + p, i);
+        else atomicMin(first + p, i);
+        if (i == tid) {
+            my_parent = p;
+            my_length = length;
+        }
     }
     wait_stores_performed();  // (atomics that return nothing count as stores)
     if (why < 5) atomicMin(&s.worst, why);
     __syncthreads();
     // copies: of a page that is partly filled, for all but the first
     auto copied = [&](int i, int& p, int& length) {
-        p = i < a.n_out ? a.parents[i] : -1;
-        if (p < 0 || p >= a.n_in) {
-            p = -1;
-            length = 0;
-            return 0;
+        p = my_parent;
+        length = my_length;
+        if (i >= kPart) {
+            p = i < a.n_out ? a.parents[i] : -1;
+            if (p < 0 || p >= a.n_in) p = -1;
+            length = p < 0 ? 0 : a.lengths[p];
         }
-        length = a.lengths[p];
-        return (length & (P - 1)) != 0 && __hip_atomic_load(first + p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != i ? 1 : 0;
+        if (p < 0 || (length & (P - 1)) == 0) return 0;
+        return (near ? s.first[p] : __hip_atomic_load(first + p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) != i ? 1 : 0;
     };
     int copies = 0;
     for (int part = 0; part < a.n_out; part += kPart) {
@@ -172,7 +185,7 @@ __global__ __launch_bounds__(kPart) void reorder_small(const jup_paged_reorder_t
 }
 
 // Three launches: maps of a byte per block in the workspace, so that marking one needs no atomic (maps of bits with atomics: 15.7 µs for the rows of 512
-// beams, 3.1 so).  512 beams of 64 requests: 6.1 + 3.1 + 3.3 µs, trips to memory behind one another.
+// beams, 3.1 so).  512 beams of 64 requests: 5.0 + 3.3 + 3.2 µs, trips to memory behind one another.
 struct Maps {
     int* first;
     unsigned char *before, *after;
@@ -267,8 +280,8 @@ hipError_t launch_paged_reorder(const jup_paged_reorder_t& a, hipStream_t s) {
     const int shift = log2_of(a.page_size);
     char* at = (char*)a.workspace + kCountBytes;
     int* first = (int*)at;
-    // One workgroup for it all, a wave per row: up to 64 rows, 16384 table entries and 2^15 blocks.  Four beams of one request take 6.7 µs, in three
-    // launches 10.7 (and the host two launches less).
+    // One workgroup for it all, a wave per row: up to 64 rows, 16384 table entries and 2^15 blocks.  Four beams of one request take 6.1 µs; with another
+    // plan, which took them 6.7, 10.7 in three launches (and the host two launches more).
     if (a.n_in + a.n_out <= kSmallRows && (long long)a.n_in * a.table_width + (long long)a.n_out * a.new_table_width <= kSmallEntries && a.n_free <= kSmallWords * 32) {
         hipLaunchKernelGGL(reorder_small, dim3(1), dim3(kPart), 0, s, a, shift, first);
         return hipGetLastError();

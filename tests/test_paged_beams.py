@@ -355,6 +355,15 @@ def test_many_requests_and_blocks(workspace):
 
 
 @gpu
+@pytest.mark.parametrize("n", [2047, 2048, 2049])
+def test_where_the_plan_leaves_the_workgroups_memory(workspace, n):
+    rng = random.Random(n)
+    table, lengths, owned, free = random_beams(rng, n, 8, 2)
+    parents = [rng.choice([-1, n - 1, 0, rng.randrange(n), rng.randrange(n)]) for _ in range(1500)]
+    check_reorder(workspace, parents, table, lengths, owned, free + [0] * (6 * n + 20 - len(free)), len(free), 8)
+
+
+@gpu
 @pytest.mark.parametrize("rows,n_free", [(32, 32768), (33, 32768), (32, 32769)])
 def test_where_one_launch_ends_and_three_begin(workspace, rows, n_free):
     rng = np.random.default_rng(rows)
