@@ -255,7 +255,8 @@ JUP_API jup_status_t jup_verify_drafts(const jup_verify_drafts_t *args, void *st
  * The end of a step of a beam search.  Request i has n_beams beams, rows i * n_beams .. of logits and scores.  Its candidates are
  * (beam b, token j) with score  scores[b] + logits[b][j] - log sum_k exp(logits[b][k]),  of a beam that has ended (ended[b] not 0)
  * the one candidate (b, end_token) with scores[b].  The n_keep best of them come out, best first; equal scores: the lower beam, then the
- * lower token.  Within a beam logits are compared, else scores in 64 bits, where of two that are alike to 2^-44 of themselves either may come first;
+ * lower token.  Within a beam logits are compared, then tokens, however far from them its score is; else scores in 64 bits, where of two beams'
+ * that are alike to 2^-44 of themselves either may come first;
  * exponentials are fp32 with their sums in 64: a score is off by about 2^-23.
  *   logits          [n_seqs * n_beams][vocab], rows row_stride apart; logits_dtype JUP_F32 or JUP_BF16.  One that is NaN or +infinity
  *                   counts as -infinity, and is no candidate

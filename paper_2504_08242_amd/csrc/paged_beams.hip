@@ -12,6 +12,8 @@ typedef unsigned long long u64;
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMost = JUP_BEAM_MOST;
+constexpr unsigned kTokens = (1u << 30) - 1;
+static_assert(kMost == 64, "six bits of a candidate are its beam");
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ u64 key_of(float x, int token) {  // x finite, -0 as 0
@@ -22,7 +24,6 @@ __device__ __forceinline__ float value_of(u64 key) {
     const unsigned bits = (unsigned)(key >> 32);
     return __uint_as_float(bits ^ ((bits >> 31) ? 0x80000000u : 0xFFFFFFFFu));
 }
-__device__ __forceinline__ int token_of(u64 key) { return (int)~(unsigned)key; }
 
 // What a workgroup leaves of a slice of a row: the statistics and n_keep keys, best first, 0 where there are fewer.
 constexpr int kLeft = 2 + kMost;
@@ -109,17 +110,23 @@ struct __attribute__((aligned(16))) Shared {
     int flag;
 };
 
-// The last one done has all rows' statistics and keys.  A candidate, larger is better: its score as an integer of the same order, then the lower beam and
-// token.
+// The last one done has all rows' statistics and keys.  A candidate, larger is better, 128 bits: its score as an integer of the same order, less its last
+// four bits (2^-48 of it), then the lower beam (6 bits), the larger logit (32) and the lower token (30).  Scores of a beam are its logits' up to rounding, so
+// this is the order of its keys however far from its logits the score is: the order of the lists, and one for all of them.
 struct __attribute__((aligned(16))) Candidate {
     u64 score, place;
     __device__ __forceinline__ bool operator>(const Candidate& o) const { return score > o.score || (score == o.score && place > o.place); }
+    __device__ __forceinline__ int beam() const { return (kMost - 1) ^ (int)((score & 15) << 2 | place >> 62); }
+    __device__ __forceinline__ int token() const { return (int)(~(unsigned)place & kTokens); }
 };
-__device__ __forceinline__ Candidate candidate_of(double score, int beam, int token) {
-    const u64 bits = __builtin_bit_cast(u64, score + 0.0);
-    return {bits ^ ((bits >> 63) ? ~0ull : 1ull << 63), ~((u64)(unsigned)beam << 32 | (unsigned)token)};
+__device__ __forceinline__ Candidate candidate_of(double score, int beam, u64 key) {
+    const u64 bits = __builtin_bit_cast(u64, score + 0.0), order = bits ^ ((bits >> 63) ? ~0ull : 1ull << 63);
+    const u64 back = (u64)((kMost - 1) ^ beam);
+    return {(order & ~15ull) | back >> 2, back << 62 | (key >> 32) << 30 | (key & kTokens)};
 }
-__device__ __forceinline__ double score_of(u64 bits) { return __builtin_bit_cast(double, bits ^ ((bits >> 63) ? 1ull << 63 : ~0ull)); }
+__device__ __forceinline__ double score_of(u64 order) {  // (the last bits are 0 again: an fp32 score comes back as it was)
+    return __builtin_bit_cast(double, (order >> 63) ? (order & ~15ull) ^ 1ull << 63 : ~(order | 15ull));
+}
 
 constexpr int kMostLists = 1024;  // slices of a request's rows
 constexpr int kEach = 4;          // candidates of a thread, where they are looked at all at once
@@ -128,7 +135,7 @@ struct Merge {
         Candidate best[kWaves][kMost + 64];
         struct {
             u64 all[kThreads];
-            Candidate chosen[kThreads];
+            Candidate chosen[kThreads], ordered[kThreads];
             int counts[kEach][kWaves];
             float bound[kWaves];
         };
@@ -136,7 +143,7 @@ struct Merge {
     double part[kMostLists];
     float m[kMostLists], top[kMost];
     double log_sum[kMost], score[kMost];
-    int ended[kMost], n[kWaves];
+    int ended[kMost], n[kWaves], disorder;
 };
 
 union Lds {
@@ -372,21 +379,21 @@ __global__ __launch_bounds__(kThreads) void select(const jup_beam_select_t a, in
     __syncthreads();
     auto candidate = [&](int at, int k, u64 key) -> Candidate {  // entry k of list `at`
         const int beam = at / slices;
-        if (g.ended[beam] != 0) return g.ended[beam] > 0 && at == beam * slices && k == 0 ? candidate_of(g.score[beam], beam, a.end_token) : Candidate{0, 0};
-        return key ? candidate_of(g.score[beam] + ((double)value_of(key) - g.log_sum[beam]), beam, token_of(key)) : Candidate{0, 0};
+        if (g.ended[beam] != 0) return g.ended[beam] > 0 && at == beam * slices && k == 0 ? candidate_of(g.score[beam], beam, key_of(0.f, a.end_token)) : Candidate{0, 0};
+        return key ? candidate_of(g.score[beam] + ((double)value_of(key) - g.log_sum[beam]), beam, key) : Candidate{0, 0};
     };
     Candidate best{0, 0};  // this thread's, and how many are better
     int rank = 0, found = 0;
-    // One number for a candidate, in the order of the scores; those that are alike to 2^-44 of them are in the order of the lists, which is that of
-    // beams and tokens.
+    // One number for a candidate, in the order of the scores; those that are alike to 2^-44 of them are in the order of the lists.
     auto number = [](const Candidate& c, int place) { return c.score ? (c.score & ~255ull) | (unsigned)(255 - place) : 0ull; };
+    if (tid == 0) g.disorder = 0;
     if (candidates <= kThreads) {  // one of a thread
         if (tid < candidates) best = candidate(tid / keep, tid % keep, my_keys[0]);
-        const u64 mine = number(best, tid), there = __ballot(mine != 0);
-        g.all[tid] = mine;
+        const u64 there = __ballot(best.score != 0);
+        g.all[tid] = number(best, tid);
         if (lane == 0) g.n[wave] = __popcll(there);
         __syncthreads();
-        rank = above(g.all, candidates, mine);  // (the places behind the last hold 0)
+        rank = above(g.all, candidates, g.all[tid]);  // (the places behind the last hold 0)
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) found += g.n[w];
     } else if (few) {
@@ -443,7 +450,19 @@ __global__ __launch_bounds__(kThreads) void select(const jup_beam_select_t a, in
             __syncthreads();
         }
     }
-    if (!few) {
+    if (few) {
+        // The order of the lists is not that of a beam's logits where it has several: each is compared with the next one, and if any two are the wrong way
+        // round, all with all.  (That at once, in place of numbers: one request of 131072 tokens, 16 kept, 24.2 µs in place of 18.6.)
+        if (best.score) g.ordered[rank] = best;
+        __syncthreads();
+        if (__any(tid + 1 < found && g.ordered[tid + 1] > g.ordered[tid]) && lane == 0) g.disorder = 1;
+        __syncthreads();
+        if (g.disorder && best.score) {
+            rank = 0;
+#pragma unroll 4
+            for (int j = 0; j < found; ++j) rank += g.ordered[j] > best;
+        }
+    } else {
         // Lists are best first: a wave goes through its lists' first entries, then the second ones, and is done where none of a round is better than
         // the last of what it keeps.
         int held = 0;  // of this wave's list, best first
@@ -489,8 +508,7 @@ __global__ __launch_bounds__(kThreads) void select(const jup_beam_select_t a, in
     }
     const long long out0 = (long long)request * keep;
     if (best.score && rank < keep) {
-        const u64 place = ~best.place;
-        const int beam = (int)(place >> 32), token = (int)(unsigned)place;
+        const int beam = best.beam(), token = best.token();
         a.parents[out0 + rank] = row0 + beam;
         a.tokens[out0 + rank] = token;
         a.new_scores[out0 + rank] = (float)score_of(best.score);

@@ -218,6 +218,62 @@ def test_beams_that_have_ended(workspace, dtype):
     check_select(workspace, logits[8:16], first.scores, 8, end_token=2, ended=first.ended)
 
 
+def beams_apart(x, scores, keep):
+    """(parents, tokens) of one request whose beams' scores are equal or so far apart that no logit brings one past another: beam after beam, by
+    score and number, each in the order of its logits, then of its tokens.  x [B, V], scores [B] on the CPU; NaN and infinities are no candidates."""
+    out = []
+    for b in sorted(range(len(scores)), key=lambda b: (-scores[b], b)):
+        best = np.argsort(-x[b], kind="stable")[:keep]
+        out += [(b, int(j)) for j in best if np.isfinite(x[b, j])]
+    out = (out + [(-1, -1)] * keep)[:keep]
+    return [b for b, _ in out], [j for _, j in out]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,V,keep", [(1, 131072, 4), (2, 40000, 4), (1, 131072, 16), (3, 100000, 12), (8, 131072, 64), (5, 30011, 33)])
+@pytest.mark.parametrize("scores", [[-1e12 - 1e9 * b for b in range(8)], [-1e30] * 8, [-1e30, -3e12, -1e30, -2e20, -1e12, -3e38, -5e25, 7e14]], ids=["far", "off", "mixed"])
+def test_logits_of_a_beam_are_compared_whatever_its_score(workspace, dtype, B, V, keep, scores):
+    """Scores in which logits vanish: within a beam the best logits come first, wherever in the row they lie (the rows are slices of several
+    workgroups), and equal ones by token.  Few candidates, some hundreds and thousands are put together in ways of their own."""
+    g = torch.Generator().manual_seed(B * V + keep)
+    x = torch.randn((2 * B, V), generator=g, dtype=torch.float64).to(dtype)
+    x[:, V - 5 * keep:] += 3.0                        # the best are late
+    x[0, :V // 2 * 2:2] = x[0, 1::2]                  # and, in one row, all are there twice
+    for b in range(1, 2 * B, 2):
+        x[b, torch.randperm(V, generator=g)[keep // 2:]] = -float("inf")   # fewer of this beam than are kept
+    s = torch.tensor([scores[:B]] * 2, dtype=torch.float32)
+    # ended beams, and none of them
+    for ended in (None, (torch.arange(2 * B).view(2, B) % 4 == 1).int()):
+        got = jp.beam_select(x.to(DEV), s.to(DEV), keep, workspace, **({} if ended is None else dict(end_token=7, ended=ended.to(DEV))))
+        for i in range(2):
+            rows = f64(x)[i * B:i * B + B].copy()
+            for b in range(B):
+                if ended is not None and ended[i, b]:
+                    rows[b] = -np.inf
+                    rows[b, 7] = 0.0
+            parents, tokens = beams_apart(rows, s[i].tolist(), keep)
+            assert got.parents[i].tolist() == [p if p < 0 else p + i * B for p in parents]
+            assert got.tokens[i].tolist() == tokens
+            there = [p >= 0 for p in parents]
+            want = np.array([s[i, p].item() for p in parents], np.float64)[there]
+            assert (np.abs(f64(got.scores)[i][there] - want) <= 2.0 ** -24 * np.abs(want) + 400).all()   # (no logit is that far from the sum)
+
+
+@gpu
+@pytest.mark.parametrize("B,V,keep", [(1, 131072, 4), (1, 131072, 16), (3, 100000, 12), (8, 131072, 64)])
+def test_logits_that_vanish_in_a_sum_are_compared(workspace, B, V, keep):
+    """Logits that differ by less than 64 bits of a score hold, all over a row, among others far below them."""
+    g = torch.Generator().manual_seed(V + keep)
+    x = torch.randn((B, V), generator=g) - 30.0
+    for b in range(B):
+        x[b, torch.randperm(V, generator=g)[:100]] = torch.arange(100, dtype=torch.float32).add(1)[torch.randperm(100, generator=g)] * 1e-18
+    s = torch.tensor([[-3.0 - 2.0 * b for b in range(B)]])   # (a beam's logits among the best lie within 1 of each other)
+    got = jp.beam_select(x.to(DEV), s.to(DEV), keep, workspace)
+    parents, tokens = beams_apart(f64(x), s[0].tolist(), keep)
+    assert got.parents[0].tolist() == parents and got.tokens[0].tolist() == tokens
+
+
 @gpu
 def test_selection_in_graphs_and_on_other_streams(workspace):
     cases = [make_logits(2, 4, 32000, torch.float32, 1), make_logits(9, 3, 5000, torch.bfloat16, 2)]
