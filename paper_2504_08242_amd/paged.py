@@ -339,7 +339,7 @@ def extend(lengths, n_new, owned, table, free_blocks, free_count, page_size, max
     return Step(row_start, positions, slots, new_lengths, new_owned, new_count, status)
 
 
-def append(k, v, slots, k_pool, v_pool, positions=None, rope_theta=None, q=None, q_out=None, scales=None, stream=None):
+def append(k, v, slots, k_pool, v_pool, positions=None, rope_theta=None, q=None, q_out=None, stream=None, scales=None):
     """Rows k, v [rows, n_kv_heads, head_dim] into their slots (jup_paged_append), k rotated at ``positions`` if rope_theta is
     given; q [rows, n_heads, head_dim] is rotated into q_out (may be q; default: a new tensor), which is returned.  scales: of a pool in 8
     bits (jup_paged_append8): the rows are quantised as they are written."""
@@ -400,7 +400,7 @@ def read(slots, k_pool, v_pool, scales=None, k_out=None, v_out=None, stream=None
     return k_out, v_out
 
 
-def attention(q, k_pool, v_pool, table, row_start, lengths, max_new, workspace=None, scale=None, out=None, scales=None, stream=None):
+def attention(q, k_pool, v_pool, table, row_start, lengths, max_new, workspace=None, scale=None, out=None, stream=None, scales=None):
     """Attention of the rows q [rows, n_heads, head_dim] of a ragged batch over the pages (jup_paged_attention): out, of q's
     shape (default: a new tensor, whose rows outside the batch are not set).  lengths count the new tokens.  max_new: the most new tokens
     a request is expected to have.  workspace: a ``Workspace`` (not needed by float32 pools); scale: 1 / sqrt(head_dim) if None; scales: of a
@@ -428,7 +428,7 @@ def attention(q, k_pool, v_pool, table, row_start, lengths, max_new, workspace=N
     return out
 
 
-def prefill(stage, hidden_in, step, k_pools, v_pools, table, max_new, workspace=None, hidden_out=None, scales=None, stream=None):
+def prefill(stage, hidden_in, step, k_pools, v_pools, table, max_new, workspace=None, hidden_out=None, stream=None, scales=None):
     """A ``binding.Stage`` over the rows hidden_in [rows, d_model] of a ragged batch (jup_stage_prefill_paged): hidden_out (default: a new
     tensor).  step: what ``extend`` returned; k_pools, v_pools [n_layers, n_blocks, n_heads, page_size, head_dim]; scales: of pools in 8
     bits, [n_layers, n_blocks, n_heads, page_size] each (jup_stage_prefill_paged8)."""

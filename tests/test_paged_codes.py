@@ -5,6 +5,7 @@ fp32 roundings on the way, 2^-22 of 448 steps of e4m3's least size, or of 127.  
 rounded once, 2^-8 of it, the result once more; fp32 sums).
 """
 import ctypes
+import inspect
 
 import numpy as np
 import pytest
@@ -114,6 +115,14 @@ def test_calls_of_nothing_launch_nothing():
     assert L.jup_paged_read8(p, x, ctypes.byref(read_args(k=None, v=None, slots=None)), None) == 0
     assert L.jup_paged_copy(p, x, ctypes.byref(copy_args(n_copies=0, copy_from=None, copy_to=None)), None) == 0
     assert L.jup_paged_copy(p, x, ctypes.byref(copy_args(n_layers=0)), None) == 0
+
+
+@pytest.mark.parametrize("call,names", [
+    (jp.append, "k v slots k_pool v_pool positions rope_theta q q_out stream"), (jp.attention, "q k_pool v_pool table row_start lengths max_new workspace scale out stream"),
+    (jp.prefill, "stage hidden_in step k_pools v_pools table max_new workspace hidden_out stream")])
+def test_arguments_of_calls_over_other_pools_keep_their_places(call, names):
+    """What a call over values takes by its place is where it was before there were scales."""
+    assert list(inspect.signature(call).parameters) == names.split() + ["scales"]
 
 
 @gpu
