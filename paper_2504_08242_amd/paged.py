@@ -432,12 +432,9 @@ def prefill(stage, hidden_in, step, k_pools, v_pools, table, max_new, workspace=
     """A ``binding.Stage`` over the rows hidden_in [rows, d_model] of a ragged batch (jup_stage_prefill_paged): hidden_out (default: a new
     tensor).  step: what ``extend`` returned; k_pools, v_pools [n_layers, n_blocks, n_heads, page_size, head_dim]; scales: of pools in 8
     bits, [n_layers, n_blocks, n_heads, page_size] each (jup_stage_prefill_paged8)."""
-    if k_pools.dim() != 5 or v_pools.shape != k_pools.shape or k_pools.shape[0] != stage.cfg["n_layers"] or (
-            k_pools.shape[0] > 1 and v_pools.stride(0) != k_pools.stride(0)):
-        raise ValueError(f"k_pools and v_pools must be tensors [{stage.cfg['n_layers']}, n_blocks, n_heads, page_size, head_dim] of the same strides")
-    if k_pools.shape[0] == 0:
-        raise ValueError("a stage without layers has no pools")
     layer_stride = _layers(k_pools, v_pools, scales)
+    if k_pools.shape[0] != stage.cfg["n_layers"]:
+        raise ValueError(f"k_pools and v_pools have {k_pools.shape[0]} layers, the stage {stage.cfg['n_layers']}")
     packed, code_scales, dtype, at, _, _ = _pool(k_pools, v_pools, scales, True)
     n, rows, width = step.lengths.numel(), hidden_in.shape[0], stage.cfg["d_model"]
     for name, t in (("hidden_in", hidden_in), ("hidden_out", hidden_in if hidden_out is None else hidden_out)):
