@@ -160,8 +160,9 @@ JUP_API jup_status_t jup_paged_attention(const jup_paged_pool_t *pool, const jup
  * The same for pools in 8 bits.  Append: k is rotated in fp32 and quantised without another rounding; of two rows with the same slot the codes may
  * be one's and the scale the other's.  Attention: the scale of a key multiplies its score, that of a value its probability, and the product is what is
  * rounded to bf16 (where max_new * n_heads / n_kv_heads is at most 16, twice: what the first rounding loses too); codes are exact in bf16.  A score or a
- * value of a key that a row does not see does not reach it, whatever codes and scales hold; nor does a value whose probability is 0 in fp32.  JUP_I8
- * codes of -128 and JUP_E4M3 codes that are no numbers, which jup_paged_append8() does not write, count as what they are.  Errors: JUP_EINVAL, JUP_EDEVICE.
+ * value of a key that a row does not see does not reach it, whatever codes and scales hold.  A key that it sees, and whose codes or scales are no finite
+ * numbers, may make all of the row NaN however small the key's probability is.  JUP_I8 codes of -128 and JUP_E4M3 codes that are no numbers, which
+ * jup_paged_append8() does not write, count as what they are.  Errors: JUP_EINVAL, JUP_EDEVICE.
  */
 JUP_API jup_status_t jup_paged_append8(const jup_paged_pool_t *pool, const jup_paged_scales_t *scales, const jup_paged_append_t *args, void *stream);
 JUP_API jup_status_t jup_paged_attention8(const jup_paged_pool_t *pool, const jup_paged_scales_t *scales, const jup_paged_attention_t *args, void *stream);
