@@ -59,7 +59,7 @@ typedef struct {
  * 128 values x_i of a head:
  *     m = max(2^-100, max_i |x_i|),  scale = m / T,  code_i = the one nearest to x_i * (T / m), ties to even
  * in fp32, with T = 127 (JUP_I8) or 448 (JUP_E4M3): a value is off by at most scale / 2 (JUP_I8), or the larger of 2^-4 of itself and
- * scale * 2^-10 (JUP_E4M3).  A head with an infinity or a NaN gets scale NaN and codes 0.
+ * scale * 2^-10 (JUP_E4M3), and by 2^-22 m, the three roundings in fp32.  A head with an infinity or a NaN gets scale NaN and codes 0.
  * Such pools need head_dim 128, tensors that are 16-byte aligned, strides of codes that are multiples of 16 and strides of scales that
  * are multiples of 4; the rows that go with them (q, k, v and results) are JUP_BF16.
  */
@@ -257,8 +257,8 @@ JUP_API jup_status_t jup_verify_drafts(const jup_verify_drafts_t *args, void *st
  * (beam b, token j) with score  scores[b] + logits[b][j] - log sum_k exp(logits[b][k]),  of a beam that has ended (ended[b] not 0)
  * the one candidate (b, end_token) with scores[b].  The n_keep best of them come out, best first; equal scores: the lower beam, then the
  * lower token.  Within a beam logits are compared, then tokens, however far from them its score is; else scores in 64 bits, where of two beams'
- * that are alike to 2^-44 of themselves either may come first;
- * exponentials are fp32 with their sums in 64: a score is off by about 2^-23.
+ * that are alike to 2^-44 of themselves either may come first.  Exponentials are fp32 with their sums in 64, the logarithm and the score too: a score is off
+ * by at most 2^-21 + 2^-22 ln(vocab), mostly far less, and by the rounding of new_scores, 2^-24 of it.
  *   logits          [n_seqs * n_beams][vocab], rows row_stride apart; logits_dtype JUP_F32 or JUP_BF16.  One that is NaN or +infinity
  *                   counts as -infinity, and is no candidate
  *   scores          [n_seqs * n_beams]: sums of log probabilities.  A beam whose score is not finite has no candidates

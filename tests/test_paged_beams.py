@@ -275,6 +275,23 @@ def test_logits_that_vanish_in_a_sum_are_compared(workspace, B, V, keep):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [32000, 131072, 1 << 20])
+@pytest.mark.parametrize("first", [True, False])
+def test_scores_of_rows_whose_sum_lies_far_below_the_largest_logit(workspace, dtype, V, first):
+    """One logit, and all others the same distance d below it, so that what the rounding of d and of d log2(e) loses does not average out: d 2^-24 each,
+    and d 2^-26 of log2(e) itself.  The mean of d over the probabilities is ln V at most; an exponential is 2^-23 off and sums of eight 2^-22."""
+    for d in (3.3, 6.7, 9.1, 10.1, 11.3, 12.7):
+        x = torch.full((2, V), -d).to(dtype)
+        x[:, 5 if first else V - 3] = 0.0
+        got = jp.beam_select(x.to(DEV), torch.tensor([[-1.0, -40.0]], device=DEV), 1, workspace)
+        d = -float(x[0, 0])
+        want = -1.0 - np.log1p((V - 1) * np.exp(-d))
+        assert got.tokens.tolist() == [[5 if first else V - 3]]
+        assert abs(float(got.scores) - want) <= 2.0 ** -21 + 2.0 ** -22 * np.log(V) + 2.0 ** -24 * abs(want)
+
+
+@gpu
 def test_selection_in_graphs_and_on_other_streams(workspace):
     cases = [make_logits(2, 4, 32000, torch.float32, 1), make_logits(9, 3, 5000, torch.bfloat16, 2)]
     want = [jp.beam_select(x, s, 4, workspace) for x, s in cases]
