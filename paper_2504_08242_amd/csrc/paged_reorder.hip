@@ -185,7 +185,9 @@ __global__ __launch_bounds__(kPart) void reorder_small(const jup_paged_reorder_t
 }
 
 // Three launches: maps of a byte per block in the workspace, so that marking one needs no atomic (maps of bits with atomics: 15.7 µs for the rows of 512
-// beams, 3.1 so).  512 beams of 64 requests: 5.0 + 3.3 + 3.2 µs, trips to memory behind one another.
+// beams, 3.1 so).  512 beams of 64 requests in a pool of 3387 blocks: 5.0 + 3.3 + 3.2 µs, trips to memory behind one another.  The maps are cleared by
+// many workgroups and gone through by one, 64 KB of them at a time, so that large pools take their own time, whatever the tables: all three launches, in
+// place / with a new stack, take 8.7 / 10.2 µs in a pool of 3900 blocks, 9.1 / 10.5 of 32768, 19 / 21 of 2^18, 54 / 56 of 2^20, 197 / 206 of 2^22.
 struct Maps {
     int* first;
     unsigned char *before, *after;
@@ -281,7 +283,9 @@ hipError_t launch_paged_reorder(const jup_paged_reorder_t& a, hipStream_t s) {
     char* at = (char*)a.workspace + kCountBytes;
     int* first = (int*)at;
     // One workgroup for it all, a wave per row: up to 64 rows, 16384 table entries and 2^15 blocks.  Four beams of one request take 6.1 µs; with another
-    // plan, which took them 6.7, 10.7 in three launches (and the host two launches more).
+    // plan, which took them 6.7, 10.7 in three launches (and the host two launches more).  In place they take 5.2 µs in any such pool, 8.4 in one of 32769
+    // blocks; a new stack is copied by the same workgroup, 4 bytes per thread at a time: 6.5 µs with 200 blocks, 7.6 with 8192, 10.7 with 32768 (lost
+    // by the rule: 9.8 with 32769).
     if (a.n_in + a.n_out <= kSmallRows && (long long)a.n_in * a.table_width + (long long)a.n_out * a.new_table_width <= kSmallEntries && a.n_free <= kSmallWords * 32) {
         hipLaunchKernelGGL(reorder_small, dim3(1), dim3(kPart), 0, s, a, shift, first);
         return hipGetLastError();
