@@ -304,7 +304,9 @@ JUP_API jup_status_t jup_beam_select(const jup_beam_select_t *args, void *stream
  *                     4  more copies than there are free blocks
  *                   Then the new requests are empty (lengths and owned 0, tables and copies -1) and the stack is as before: the
  *                   old tables still hold.
- * Entries of a table that are no blocks are copied as they are and never go back.  n_in, n_out <= JUP_PAGED_MAX_SEQS.
+ * Entries of a table that are no blocks are copied as they are and never go back.  Where the partly filled page is none, copies of it are due all the
+ * same: copy_from is that entry, the page in copy_to is the new request's, and as jup_paged_copy() does nothing for it, holds what it held.
+ * n_in, n_out <= JUP_PAGED_MAX_SEQS.
  * workspace: as in jup_paged_attention().  Errors: JUP_EINVAL, JUP_EDEVICE.
  */
 typedef struct {
