@@ -530,7 +530,7 @@ hipError_t launch_beam_select(const jup_beam_select_t& a, hipStream_t s) {
         // Slices of whole steps, of 4096 logits at least: as many as give the chip 1024 workgroups (512 rows of 131072 with 512, 1024 and 2048
         // workgroups: 59, 51 and 60 µs), 512 where more than eight are kept, as every wave begins with a list of that many (32 rows of 131072, 16 kept: 25
         // and 33), and no more than the last workgroup can look at at once, where that is four at least (one request of eight beams and 131072 tokens 17 µs
-        // in place of 23, of 16 beams and 32000 21 in place of 28).
+        // in place of 23, of 16 beams and 32000 22 in place of 28).
         const long long wanted = a.n_keep > 8 ? 512 : 1024, fit = kThreads * kEach / (a.n_beams * a.n_keep);
         long long most = rows >= wanted ? 1 : wanted / rows;
         if (fit >= 4 && most > fit) most = fit;
