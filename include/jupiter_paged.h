@@ -158,8 +158,9 @@ JUP_API jup_status_t jup_paged_attention(const jup_paged_pool_t *pool, const jup
 
 /*
  * The same for pools in 8 bits.  Append: k is rotated in fp32 and quantised without another rounding; of two rows with the same slot the codes may
- * be one's and the scale the other's.  Attention: the scale of a key multiplies its score, that of a value its probability, and the product is what is
- * rounded to bf16 (where max_new * n_heads / n_kv_heads is at most 16, twice: what the first rounding loses too); codes are exact in bf16.  A score or a
+ * be one's and the scale the other's.  Attention: the scale of a key multiplies its score, that of a value its probability, and the product meets the value
+ * as two numbers of bf16, which hold it to 2^-15; as one, rounded, 2^-8, in calls of long chunks and prompts (of G = n_heads / n_kv_heads: max_new * G
+ * above 96, and (n_rows * G / 32 + n_seqs) * n_kv_heads above 1536).  Codes are exact in bf16.  A score or a
  * value of a key that a row does not see does not reach it, whatever codes and scales hold.  A key that it sees, and whose codes or scales are no finite
  * numbers, may make all of the row NaN however small the key's probability is.  JUP_I8 codes of -128 and JUP_E4M3 codes that are no numbers, which
  * jup_paged_append8() does not write, count as what they are.  Errors: JUP_EINVAL, JUP_EDEVICE.

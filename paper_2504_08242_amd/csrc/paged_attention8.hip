@@ -2,9 +2,12 @@
 // paged_work.h.
 //
 // Codes are exact in bf16, so products are those of bf16 operands.  Scores are sums over a key's codes times the key's scale; a value's scale goes
-// with its probability, s_j p_j, which is rounded to bf16 as the operand of the second product: 2^-8 of it, as in a cache of bf16 values.  Tiles
-// of 16 rows, which wait for memory, take what that rounding loses as a second operand (2^-16 is left): results are then as far from the
-// formula as their own rounding, 1.6e-3 in place of 2.3e-3 of the whole, and calls take 1 to 3 % longer (64 requests of one token 72.6 and 73.7 µs).
+// with its probability, s_j p_j, as an operand of the second product, which is bf16.  Tiles of up to 32 rows take it as two: its first eight bits, cut
+// off, and the rest of it, which is exact in fp32, rounded (2^-15 is left).  Results are then as far from the formula as their own rounding, 1.66e-3 of the
+// whole; with one rounded operand 2.2e-3 to 2.5e-3, and up to 1.54 times as far as that rounding for a few short int8 prompts.  In µs, one operand / two: 512
+// int8 tokens behind 1536 42.1 / 46.0 (with the first operand rounded, and the rest looked at for infinities, 48.7), 768 66 / 70, a prompt of 1024 32.7 / 34.1, 64
+// behind 576 11.6 / 12.0, 16 requests of five with four heads to a key head 18.0 / 18.3.  Tall tiles (attention_many) round one operand, 2^-8 of it, as they
+// do over bf16 values: with two, four prompts of 700 to 4100 tokens take 401 in place of 337.
 #include "paged_many.h"
 
 namespace jup {
@@ -240,17 +243,19 @@ __global__ __launch_bounds__(64 * NW, (Few8<QW, NW>::kGroups * NW / 4)) void att
         const float alpha = grow ? __builtin_amdgcn_exp2f(m_run - m_safe) : 1.0f;
         const bool rescale = grow && m_run != -INFINITY;
         float ps = 0.f;
-        bf16x8 pf[NS / 8], rest;
+        u32x4 pf[NS / 8], rest[NS / 8];  // the operands of the second product
 #pragma unroll
-        for (int r = 0; r < NS; ++r) {
-            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[r], a.scale_log2e, -m_safe));
-            ps += p;
-            const float x = scaled(p, vs[r]);
-            pf[r >> 3][r & 7] = (__bf16)x;  // the operand of the second product: 2^-8 of each
-            if constexpr (QW == 16) {  // and what that loses as another one (not of an infinity)
-                const float lost = x - (float)(__bf16)x;
-                rest[r & 7] = (__bf16)(fabsf(lost) < INFINITY ? lost : 0.f);
+        for (int r = 0; r < NS; r += 2) {
+            float x[2], hi[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[r + e], a.scale_log2e, -m_safe));
+                ps += p;
+                x[e] = scaled(p, vs[r + e]);
+                hi[e] = __uint_as_float(__float_as_uint(x[e]) & 0xFFFF0000u);
             }
+            pf[r >> 3][(r & 7) / 2] = __builtin_amdgcn_perm(__float_as_uint(x[1]), __float_as_uint(x[0]), 0x07060302);
+            rest[r >> 3][(r & 7) / 2] = pack_bf16x2(x[0] - hi[0], x[1] - hi[1]);
         }
         l_run = l_run * alpha + ps;
         m_run = m_new;
@@ -276,8 +281,8 @@ __global__ __launch_bounds__(64 * NW, (Few8<QW, NW>::kGroups * NW / 4)) void att
             // QW = 32: feature block f / 2, key half f % 2; QW = 16: feature block f, all 32 keys
             const u32x2 codes = read_tr8(my_place + (QW == 16 ? v_lane ^ (16 * f) : (v_lane ^ (32 * (f / 2))) + (f % 2) * 2048));
             const bf16x8 v = operand<CODE>(codes[0], codes[1]);
-            if constexpr (QW == 16) oacc[f] = mfma16(v, rest, mfma16(v, pf[0], oacc[f]));
-            else oacc[f / 2] = mfma32(v, pf[f % 2], oacc[f / 2]);
+            if constexpr (QW == 16) oacc[f] = mfma16(v, __builtin_bit_cast(bf16x8, rest[0]), mfma16(v, __builtin_bit_cast(bf16x8, pf[0]), oacc[f]));
+            else oacc[f / 2] = mfma32(v, __builtin_bit_cast(bf16x8, rest[f % 2]), mfma32(v, __builtin_bit_cast(bf16x8, pf[f % 2]), oacc[f / 2]));
         }
         here = next;
         if (P == 2) next = third;
@@ -311,8 +316,8 @@ __global__ __launch_bounds__(64 * NW, (Few8<QW, NW>::kGroups * NW / 4)) void att
 }
 
 // Codes become bf16 values once per workgroup of attention_many and once per wave of attention_few8, but there the waves do not meet: tiles of 32 rows are
-// faster up to three rounds of them.  In µs, attention_few8 and attention_many, int8: 512 tokens behind 1536 on 32 heads 43 / 46 (e4m3 36 / 45), 768
-// behind 1536 66 / 81 (58 / 81), prompts of 1024 33 / 36, of 1200 on 40 heads (1520 tiles) 51 / 50, of 2048 (2600 tiles) 113 / 95.
+// faster up to three rounds of them.  In µs, attention_few8 and attention_many, int8: 300 tokens behind 1536 on 32 heads 41 / 51, 512 45 / 45 (e4m3 39 / 45),
+// 768 70 / 81 (62 / 81), prompts of 800 26 / 29, of 1024 34 / 36, of 1200 on 40 heads (1520 tiles) 54 / 50 (lost by the rule), of 2048 (2600 tiles) 120 / 95.
 constexpr int kFewTiles8 = 1536;
 
 template <int CODE>

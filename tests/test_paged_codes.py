@@ -371,6 +371,24 @@ def test_attention_over_codes(workspace, kind, heads, kv_heads, page, requests):
 
 @gpu
 @kinds
+@pytest.mark.parametrize("heads,kv_heads,requests", [(4, 4, [(200, 1), (37, 3)]), (8, 1, [(0, 13), (0, 18)]), (32, 32, [(0, 23), (0, 73)]), (4, 2, [(100, 40), (0, 30)]),
+                                                     (40, 8, [(0, 16), (0, 19)]), (64, 64, [(30, 70), (0, 90), (0, 60)]), (2, 2, [(3000, 60)]), (16, 1, [(1500, 2)])])
+def test_tiles_of_few_rows_lose_nothing_to_probabilities_of_fewer_bits(workspace, kind, heads, kv_heads, requests):
+    """In tiles of up to 32 rows a probability times its value's scale goes into the product as two numbers: its first 8 bits, cut off, which leaves less than
+    2^-7 of it, and the rest, rounded, 2^-8 of that.  What is left is 2^-15, fp32 sums and the rounding of the result."""
+    b = Batch8(kind, heads, kv_heads, 16, requests)
+    got = b.run(workspace)
+    k, v = (whole(x, s, kind) for x, s in zip((b.k, b.v), b.scales))
+    want, size, most = ref.attention(f64(b.q)[:b.rows], k, v, b.table, b.row_start, b.lengths, b.scale, b.page)
+    keys = max(b.lengths)
+    small = (keys + 2 * 128 * most + 32) * 2.0 ** -24
+    least = keys * 2.0 ** -126 * np.abs(v[np.isfinite(v)]).max(initial=1.0)
+    off = np.abs(f64(got)[:b.rows] - want) - ((2.0 ** -15 + small) * size + BF16 * np.abs(want) + least)
+    assert (off <= 0).all(), float(off.max())
+
+
+@gpu
+@kinds
 @pytest.mark.parametrize("heads,kv_heads,page,requests", MANY_HEADS)
 def test_attention_of_many_heads(workspace, kind, heads, kv_heads, page, requests):
     b = Batch8(kind, heads, kv_heads, page, requests)
